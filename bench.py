@@ -377,7 +377,7 @@ def main_3d(args, wl):
     value = kept_flops / (ms_step * 1e-3) / 1e12
     achieved = kept_flops / (run_ms * 1e-3) / 1e12
     bq, bkv, bkc = prep_bytes_3d(wl, "q"), prep_bytes_3d(wl, "kv"), prep_bytes_3d(wl, "kv_chunk")
-    digest = src_digest("attn.hip")
+    digest = src_digest("attn_core.h", "attn.hip")
     out = {
         "metric": "sparse AR attention kept-block TFLOP/s (3-D blocks: prep + select + sparse attention + untile "
                   "per call)",
@@ -557,7 +557,7 @@ def main():
     value = kept_flops / (ms_step * 1e-3) / 1e12
     achieved = kept_flops / (run_ms * 1e-3) / 1e12
     hbm_sel_bytes = 2.0 * B * H * (Lq + (wl.Lk - Lq - wl.n_text)) * d + mask_np.size * (1 + 4) + counts.numel() * 4
-    digest = src_digest("attn.hip")
+    digest = src_digest("attn_core.h", "attn.hip")
     traffic = traffic_from_profile("attn_fwd", wl.name, digest, kept_flops)
 
     out = {

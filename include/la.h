@@ -308,6 +308,47 @@ la_status la_untile_o_3d(const la_grid3d* grid, const void* o_tiled, const float
                          float* lse, void* stream);
 
 /* ------------------------------------------------------------------------------
+ * Packed sequences: attention over whole prompts, and over a cache in 4 bits.
+ *
+ * Tokens of S sequences of different lengths lie behind one another, q and o [Tq, Hq, d], k and v
+ * [Tk, Hkv, d] in bf16 with the strides below (d contiguous); query head h reads key head
+ * h / (Hq / Hkv).  Sequence s has the rows [cu_q[s], cu_q[s + 1]) of q and o.  The starts and
+ * lengths are int32 device arrays and are read by the kernels.  They have to ascend from 0; starts
+ * are clamped to the rows there are, and a sequence that would end before it starts has no rows, so
+ * no value of them reads or writes outside the tensors.
+ * Rows that no sequence covers (behind the last one) are not written.
+ * Causal: query i of lq sees key n of lk where n <= i + lk - lq (the last query sees the last key).
+ * A query that sees no key gives o = 0 and lse = -inf.  Values of keys outside the sequence do not
+ * matter, whatever they hold; a key that some query of the sequence sees has to be finite.
+ * -------------------------------------------------------------------------- */
+typedef struct la_seqs {
+  int32_t S;                 /* sequences (>= 0) */
+  int32_t Tq, Tk;            /* rows of q and o, and of k and v (>= 0) */
+  int32_t Hq, Hkv;           /* heads: Hq a multiple of Hkv */
+  int32_t d;                 /* 64 or 128 */
+  int32_t causal;            /* 0 or 1 */
+  int64_t q_token, q_head;   /* strides in elements, multiples of 8: a token's >= d and < 2^24, */
+  int64_t o_token, o_head;   /* a head's >= 0 (0: the heads share one row; not for o) */
+  int64_t k_token, k_head;
+  int64_t v_token, v_head;
+} la_seqs;
+
+/* Bytes of scratch that la_prompt_attn needs (partial results of work that is split between
+ * workgroups); 0 for an invalid la_seqs, and where there is nothing to do. */
+size_t la_prompt_ws_bytes(const la_seqs* seqs);
+
+/* Attention over whole prompts: softmax(q k^T scale) v of every sequence over its own keys.
+ *   cu_q, cu_k  int32 [S + 1]: first row of every sequence in q and in k; cu_k may be cu_q.
+ *   scale       <= 0 selects 1/sqrt(d).
+ *   o           bf16, strides o_token and o_head;  lse  float [Tq, Hq] or NULL: natural-log sum of
+ *               exp(logits).
+ * Softmax in fp32, products in bf16 with fp32 accumulation.  Kernel launches only (two): a caller
+ * may capture the call; calls that may overlap need a ws each. */
+la_status la_prompt_attn(const la_seqs* seqs, const void* q, const void* k, const void* v,
+                         const int32_t* cu_q, const int32_t* cu_k, float scale, void* o, float* lse,
+                         void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------
  * The scalar policy around the path: adaptive context management (Sec. 3.1) and the
  * denoising cache (Sec. 3.2).  Only the latent dynamics runs on the GPU; the other
  * calls are host-only scalar rules (no GPU, no stream), exact in double precision.

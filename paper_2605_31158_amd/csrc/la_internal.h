@@ -83,6 +83,14 @@ int mse_blocks(int64_t n, int bf16);
 hipError_t launch_latent_mse(const void* a, const void* b, int64_t n, int bf16, double* out, void* ws,
                              hipStream_t st);
 
+// Attention over packed sequences (seq_walk.h has the shapes that the kernels take).
+struct SeqGeom;
+struct SeqIo;
+struct CacheGeom;
+hipError_t launch_prompt_attn(const SeqGeom& g, const SeqIo& io, int d, int P, hipStream_t st);
+// Attention over a 4-bit cache: sequences of many query rows, and of few.
+hipError_t launch_cache_rows(const SeqGeom& g, const SeqIo& io, const CacheGeom& cg, int d, int P, hipStream_t st);
+
 // CUs of the current device, 0 when HIP cannot say.  A constant of the device, asked for once per
 // device: four launches of a step need it.
 int device_cu_count();

@@ -43,6 +43,13 @@ class Grid3D(ctypes.Structure):
         return "Grid3D(" + ", ".join(f"{n}={getattr(self, n)}" for n, _ in self._fields_) + ")"
 
 
+class Seqs(ctypes.Structure):
+    """la_seqs: packed sequences and the strides of their tensors."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("S", "Tq", "Tk", "Hq", "Hkv", "d", "causal")] + \
+               [(n, ctypes.c_int64) for n in ("q_token", "q_head", "o_token", "o_head", "k_token", "k_head", "v_token",
+                                              "v_head")]
+
+
 LA_PART_TEXT, LA_PART_CONTEXT, LA_PART_CHUNK, LA_PART_ALL = 1, 2, 4, 7
 
 _lib = None
@@ -50,6 +57,7 @@ _fns = {}          # the functions of _lib by name
 _P = ctypes.c_void_p
 _SP = ctypes.POINTER(Shape)
 _GP = ctypes.POINTER(Grid3D)
+_QP = ctypes.POINTER(Seqs)
 
 _SIGNATURES = {
     "la_workspace_bytes": (ctypes.c_size_t, [_SP]),
@@ -73,6 +81,8 @@ _SIGNATURES = {
                                                 ctypes.c_size_t, _P]),
     "la_sparse_attn_plan_valid": (ctypes.c_int, [_SP, _P, _P, _P, _P, ctypes.c_size_t, _P]),
     "la_untile_o_3d": (ctypes.c_int, [_GP, _P, _P, _P, _P, _P]),
+    "la_prompt_ws_bytes": (ctypes.c_size_t, [_QP]),
+    "la_prompt_attn": (ctypes.c_int, [_QP, _P, _P, _P, _P, _P, ctypes.c_float, _P, _P, _P, ctypes.c_size_t, _P]),
     "la_latent_mse": (ctypes.c_int, [_P, _P, ctypes.c_int64, ctypes.c_int32, _P, _P, ctypes.c_size_t, _P]),
     "la_dynamics_ema": (ctypes.c_int, [ctypes.c_double, _P, ctypes.c_double, _P]),
     "la_temporal_window": (ctypes.c_int, [ctypes.c_double, ctypes.c_double, ctypes.c_int32, _P]),
@@ -513,6 +523,99 @@ def sparse_attn_3d(g: Grid3D, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
     o_t, lse_t = res if want_lse else (res, None)
     o, lse = untile_o_3d(g, o_t, lse_t)
     return o, lse, mask, counts, idx
+
+
+# ----------------------------------------------------------------------------------------------
+# packed sequences
+
+def _check_rows(name, t: torch.Tensor, device=None, heads=None, d=None, tokens=None):
+    """A bf16 GPU tensor [tokens, heads, d] with contiguous rows and strides that are multiples of 8."""
+    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+        raise TypeError(f"{name} must be a GPU tensor")
+    if t.dtype != torch.bfloat16 or t.dim() != 3:
+        raise TypeError(f"{name} must be a bfloat16 [tokens, heads, d] tensor")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    if (tokens is not None and t.shape[0] != tokens) or (heads is not None and t.shape[1] != heads) or \
+            (d is not None and t.shape[2] != d):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, inconsistent with the other operands")
+    if t.numel() and (t.stride(2) != 1 or (t.shape[0] > 1 and t.stride(0) % 8) or (t.shape[1] > 1 and t.stride(1) % 8)):
+        raise ValueError(f"{name} must have contiguous rows, and strides that are multiples of 8")
+
+
+def _strides(t: torch.Tensor):
+    """(token, head) strides in elements; those of an extent of one, which mean nothing, as a packed tensor's."""
+    T, H, d = t.shape
+    head = t.stride(1) if H > 1 else d
+    return (t.stride(0) if T > 1 else H * d), head
+
+
+def _check_ints(name, t: torch.Tensor, device, shape):
+    if not isinstance(t, torch.Tensor) or t.device != device or t.dtype != torch.int32 or tuple(t.shape) != shape \
+            or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 {list(shape)} tensor on {device}")
+
+
+def _on_device_of(t: torch.Tensor, fn: str, *args):
+    """_call with t's device as the current one (the launches go there)."""
+    if torch.cuda.current_device() == t.get_device():
+        _call(fn, *args)
+    else:
+        with torch.cuda.device(t.device):
+            _call(fn, *args)
+
+
+def _outputs(q, want_lse, out, lse_out):
+    T, Hq, d = q.shape
+    if out is None:
+        out = torch.empty((T, Hq, d), dtype=torch.bfloat16, device=q.device)
+    else:
+        _check_rows("out", out, q.device, Hq, d, T)
+    if lse_out is None:
+        lse_out = torch.empty((T, Hq), dtype=torch.float32, device=q.device) if want_lse else None
+    elif lse_out.dtype != torch.float32 or tuple(lse_out.shape) != (T, Hq) or not lse_out.is_contiguous() \
+            or lse_out.device != q.device:
+        raise ValueError(f"lse_out must be a contiguous float32 {[T, Hq]} tensor on {q.device}")
+    return out, lse_out
+
+
+def _scratch(need, device, ws):
+    """(workspace, bytes) of a call that needs `need` bytes."""
+    if ws is None:
+        if need == 0:
+            return None, 0
+        ws = torch.empty(need, dtype=torch.uint8, device=device)
+    elif ws.device != device or not ws.is_contiguous():
+        raise ValueError(f"ws must be a contiguous tensor on {device}")
+    return ws, ws.numel() * ws.element_size()
+
+
+def prompt_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor,
+                cu_k: Optional[torch.Tensor] = None, causal: bool = True, scale: Optional[float] = None,
+                want_lse: bool = False, ws: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                lse_out: Optional[torch.Tensor] = None):
+    """Attention of packed sequences over their own keys -> o bf16 [Tq, Hq, d] (and lse fp32 [Tq, Hq]).
+
+    q [Tq, Hq, d]; k, v [Tk, Hkv, d] in bf16, Hq a multiple of Hkv; token and head strides are free
+    (multiples of 8).  cu_q, cu_k int32 [S + 1] on the GPU: the first row of every sequence (cu_k None:
+    cu_q).  Causal: the last query of a sequence sees its last key.  Rows behind the last sequence are
+    not written (a new output holds anything there)."""
+    _check_rows("q", q)
+    Tq, Hq, d = q.shape
+    _check_rows("k", k, q.device, d=d)
+    Tk, Hkv, _ = k.shape
+    _check_rows("v", v, q.device, Hkv, d, Tk)
+    if cu_k is None:
+        cu_k = cu_q
+    S = cu_q.numel() - 1
+    _check_ints("cu_q", cu_q, q.device, (S + 1,))
+    _check_ints("cu_k", cu_k, q.device, (S + 1,))
+    o, lse = _outputs(q, want_lse, out, lse_out)
+    seqs = Seqs(S, Tq, Tk, Hq, Hkv, d, 1 if causal else 0, *_strides(q), *_strides(o), *_strides(k), *_strides(v))
+    ws, nbytes = _scratch(int(lib().la_prompt_ws_bytes(ctypes.byref(seqs))), q.device, ws)
+    _on_device_of(q, "la_prompt_attn", ctypes.byref(seqs), _ptr(q), _ptr(k), _ptr(v), _ptr(cu_q), _ptr(cu_k),
+                  scale if scale is not None else 0.0, _ptr(o), _ptr(lse), _ptr(ws), nbytes, _stream(q))
+    return o if lse is None else (o, lse)
 
 
 # ----------------------------------------------------------------------------------------------
