@@ -348,6 +348,54 @@ la_status la_prompt_attn(const la_seqs* seqs, const void* q, const void* k, cons
                          const int32_t* cu_q, const int32_t* cu_k, float scale, void* o, float* lse,
                          void* ws, size_t ws_bytes, void* stream);
 
+/* A cache of keys and values in 4 bits, in pages that the sequences share.
+ *   Values are e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6, and their negatives) times a power of two that the 32
+ *   values of a block of a row share: 4.25 bits per value.  The power is the smallest under which the
+ *   block's largest value is rounded by no more than half a step (held to 2^-125 .. 2^125); values are
+ *   rounded to nearest, ties to the even code.  A block with a value that is not finite reads as NaN.
+ *   cache  uint8 [n_pages, Hkv, la_kv4_page_bytes(d, page)], 16-byte aligned: per page and key head
+ *            K codes [page][d / 2]              two values to a byte, the lower 4 bits first;
+ *            K scales [d / 32][page]            2^(byte - 127), 255 = NaN;
+ *            V codes [page / 4][16][4][d / 32]  quads of tokens: chunk c (values c d / 16 ..) of each in turn;
+ *            V scales [d / 32][page].
+ *   table  int32 [S, max_pages]: token n of sequence s lies on page table[s][n / page].  A page number
+ *          outside [0, n_pages) is a page that does not exist: tokens on it are not written, and are
+ *          read, by la_kv4_attn too, as rows of zeros.
+ *   lens   int32 [S]: tokens of each sequence, the new ones included. */
+typedef struct la_kv4 {
+  int32_t n_pages;           /* >= 1 */
+  int32_t page;              /* tokens of a page: a power of two, 16 to 1024 */
+  int32_t max_pages;         /* pages of a row of the table, >= 1; a sequence ends at max_pages * page tokens */
+} la_kv4;
+
+/* Bytes of one key head's part of a page, page (d + d / 16); 0 for an unsupported d or page. */
+size_t la_kv4_page_bytes(int32_t d, int32_t page);
+
+/* Enters rows of k and v into the cache.
+ *   k, v  bf16 [Tk, Hkv, d] (la_seqs: S, Tk, Hkv, d and their strides are read; the rest is not).
+ *   cu    int32 [S + 1]: rows [cu[s], cu[s + 1]) are the last tokens of sequence s, so that the last
+ *         row is token lens[s] - 1.  Tokens before 0 or past the table are dropped.
+ * Two rows must not go to one place (a page that two sequences share is entered by one of them). */
+la_status la_kv4_append(const la_seqs* seqs, const la_kv4* kv, const void* k, const void* v, const int32_t* cu,
+                        const int32_t* lens, const int32_t* table, void* cache, void* stream);
+
+/* The values that the last cu[s + 1] - cu[s] tokens of every sequence stand for, into rows of k and v:
+ * la_kv4_append's places, read back (exactly: every value of the cache is a bf16 value).  Tokens that
+ * have no place come as zeros; rows of no sequence are not written. */
+la_status la_kv4_read(const la_seqs* seqs, const la_kv4* kv, const void* cache, const int32_t* cu,
+                      const int32_t* lens, const int32_t* table, void* k, void* v, void* stream);
+
+/* Bytes of scratch that la_kv4_attn needs; 0 for invalid arguments, and where there is nothing to do. */
+size_t la_kv4_ws_bytes(const la_seqs* seqs, const la_kv4* kv, int32_t max_q);
+
+/* Attention of every sequence's queries over its cache: la_prompt_attn with the keys and values that
+ * the cache stands for (k and v of la_seqs and Tk are not read).  With causal = 1 the last query sees
+ * the last of lens[s] tokens.
+ *   max_q  no sequence has more query rows; those of one that has are not written. */
+la_status la_kv4_attn(const la_seqs* seqs, const la_kv4* kv, int32_t max_q, const void* q, const void* cache,
+                      const int32_t* cu_q, const int32_t* lens, const int32_t* table, float scale, void* o,
+                      float* lse, void* ws, size_t ws_bytes, void* stream);
+
 /* ------------------------------------------------------------------------------
  * The scalar policy around the path: adaptive context management (Sec. 3.1) and the
  * denoising cache (Sec. 3.2).  Only the latent dynamics runs on the GPU; the other

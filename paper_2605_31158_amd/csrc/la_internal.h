@@ -89,6 +89,13 @@ struct SeqIo;
 struct CacheGeom;
 hipError_t launch_prompt_attn(const SeqGeom& g, const SeqIo& io, int d, int P, hipStream_t st);
 // Attention over a 4-bit cache: sequences of many query rows, and of few.
+hipError_t launch_cache_tokens(const SeqGeom& g, const SeqIo& io, const CacheGeom& cg, int d, int rows, int P,
+                               hipStream_t st);
+hipError_t launch_cache_merge(const SeqGeom& g, const SeqIo& io, int d, int rows, int P, hipStream_t st);
+hipError_t launch_kv4_append(const la_seqs& s, const CacheGeom& cg, const void* k, const void* v, const int32_t* cu,
+                             const int32_t* lens, void* pages, hipStream_t st);
+hipError_t launch_kv4_read(const la_seqs& s, const CacheGeom& cg, const int32_t* cu, const int32_t* lens, void* k,
+                           void* v, hipStream_t st);
 hipError_t launch_cache_rows(const SeqGeom& g, const SeqIo& io, const CacheGeom& cg, int d, int P, hipStream_t st);
 
 // CUs of the current device, 0 when HIP cannot say.  A constant of the device, asked for once per

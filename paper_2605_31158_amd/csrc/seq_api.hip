@@ -99,11 +99,70 @@ SeqIo seq_io(const la_seqs& s, const void* q, void* o, float* lse, float scale) 
   return io;
 }
 
-// Workgroups that the device runs at once: CUs rounded down to a multiple of 8 (the XCDs).
-int device_workgroups() {
-  const int cus = device_cu_count();
-  const int p = cus / 8 * 8;
-  return p < 8 ? 8 : (p > kMaxWorkgroups ? kMaxWorkgroups : p);
+// Workgroups that the device runs at once, `per_cu` to a CU: CUs rounded down to a multiple of 8 (the XCDs).
+int device_workgroups(int per_cu) {
+  const int p = device_cu_count() / 8 * 8;
+  return (p < 8 ? 8 : (p > kMaxWorkgroups ? kMaxWorkgroups : p)) * per_cu;
+}
+
+bool bad_kv4(const la_kv4* kv) {
+  return kv->n_pages < 1 || kv->max_pages < 1 || kv->page < 16 || kv->page > 1024 || (kv->page & (kv->page - 1));
+}
+
+CacheGeom cache_geom(const la_seqs& s, const la_kv4& kv, const void* cache, const int32_t* table) {
+  CacheGeom cg{(const uint8_t*)cache, table, kv.n_pages, kv.max_pages, 0, s.Hkv};
+  while ((1 << cg.log_p) < kv.page) ++cg.log_p;
+  return cg;
+}
+
+// How a call over a cache is made: sequences of at most lq_token query tokens by token_attn_kernel with
+// `rows` packed rows, those of more by seq_attn_kernel.
+constexpr int kTokenRows = 64;
+constexpr int kTokenPerCu = 2;
+struct CachePlan {
+  int lq_token, rows;
+  bool many;               // there may be sequences of more tokens
+  SeqGeom token, many_rows;
+  int p_token, p_many;     // workgroups (before the device's limit)
+  size_t bytes;
+};
+
+CachePlan cache_plan(const la_seqs& s, const la_kv4& kv, int max_q) {
+  CachePlan c{};
+  const int G = s.Hq / s.Hkv;
+  const int64_t cap64 = (int64_t)kv.max_pages * kv.page;
+  const int cap = cap64 < 0x7fffff00 ? (int)cap64 : 0x7fffff00;
+  c.lq_token = G >= kTokenRows ? 1 : kTokenRows / G;
+  c.many = max_q > c.lq_token;
+  c.rows = (int64_t)(c.many ? c.lq_token : max_q) * G <= 16 ? 16 : 32;
+  c.token = seq_geom(s, c.rows, cap);
+  c.token.lq_max = c.many ? c.lq_token : max_q;
+  c.p_token = workgroups(c.token, cap, kMaxWorkgroups * kTokenPerCu);
+  c.bytes = part_layout(c.p_token, c.rows, s.d, nullptr).bytes;
+  if (c.many) {
+    c.many_rows = seq_geom(s, kRows, cap);
+    c.many_rows.lq_min = c.lq_token + 1;
+    c.many_rows.lq_max = max_q;
+    c.p_many = workgroups(c.many_rows, cap, kMaxWorkgroups);
+    const size_t b = part_layout(c.p_many, kRows, s.d, nullptr).bytes;
+    if (b > c.bytes) c.bytes = b;
+  }
+  return c;
+}
+
+la_status check_cache_rows(const la_seqs* s, const la_kv4* kv, const void* k, const void* v, const int32_t* cu,
+                           const int32_t* lens, const int32_t* table, const void* cache, bool written) {
+  la_status st = check_seqs(s);
+  if (st != LA_OK) return st;
+  if (!kv) return LA_ERR_ARG;
+  if (bad_kv4(kv)) return LA_ERR_SHAPE;
+  if (s->S == 0 || s->Tk == 0) return LA_OK;
+  if (bad_strides(s->k_token, s->k_head, s->d, written) || bad_strides(s->v_token, s->v_head, s->d, written))
+    return LA_ERR_SHAPE;
+  if (!k || !v || !cu || !lens || !table || !cache) return LA_ERR_ARG;
+  if (misaligned(k) || misaligned(v) || misaligned(cache)) return LA_ERR_ARG;
+  if (((uintptr_t)cu | (uintptr_t)lens | (uintptr_t)table) & 3u) return LA_ERR_ARG;
+  return LA_OK;
 }
 
 }  // namespace
@@ -141,8 +200,69 @@ la_status la_prompt_attn(const la_seqs* seqs, const void* q, const void* k, cons
   io.k = (const uint16_t*)k;
   io.v = (const uint16_t*)v;
   set_parts(&io, w);
-  const int have = device_workgroups();
+  const int have = device_workgroups(1);
   const hipError_t e = launch_prompt_attn(g, io, seqs->d, most < have ? most : have, (hipStream_t)stream);
+  return e == hipSuccess ? LA_OK : LA_ERR_HIP;
+}
+
+size_t la_kv4_page_bytes(int32_t d, int32_t page) {
+  const la_kv4 kv{1, page, 1};
+  if ((d != 64 && d != 128) || bad_kv4(&kv)) return 0;
+  return (size_t)page * (d + d / 16);
+}
+
+la_status la_kv4_append(const la_seqs* seqs, const la_kv4* kv, const void* k, const void* v, const int32_t* cu,
+                        const int32_t* lens, const int32_t* table, void* cache, void* stream) {
+  const la_status st = check_cache_rows(seqs, kv, k, v, cu, lens, table, cache, false);
+  if (st != LA_OK || seqs->S == 0 || seqs->Tk == 0) return st;
+  const CacheGeom cg = cache_geom(*seqs, *kv, cache, table);
+  const hipError_t e = launch_kv4_append(*seqs, cg, k, v, cu, lens, cache, (hipStream_t)stream);
+  return e == hipSuccess ? LA_OK : LA_ERR_HIP;
+}
+
+la_status la_kv4_read(const la_seqs* seqs, const la_kv4* kv, const void* cache, const int32_t* cu, const int32_t* lens,
+                      const int32_t* table, void* k, void* v, void* stream) {
+  const la_status st = check_cache_rows(seqs, kv, k, v, cu, lens, table, cache, true);
+  if (st != LA_OK || seqs->S == 0 || seqs->Tk == 0) return st;
+  const CacheGeom cg = cache_geom(*seqs, *kv, cache, table);
+  const hipError_t e = launch_kv4_read(*seqs, cg, cu, lens, k, v, (hipStream_t)stream);
+  return e == hipSuccess ? LA_OK : LA_ERR_HIP;
+}
+
+size_t la_kv4_ws_bytes(const la_seqs* seqs, const la_kv4* kv, int32_t max_q) {
+  if (check_seqs(seqs) != LA_OK || !kv || bad_kv4(kv) || max_q < 1 || seqs->S == 0 || seqs->Tq == 0) return 0;
+  return cache_plan(*seqs, *kv, max_q).bytes;
+}
+
+la_status la_kv4_attn(const la_seqs* seqs, const la_kv4* kv, int32_t max_q, const void* q, const void* cache,
+                      const int32_t* cu_q, const int32_t* lens, const int32_t* table, float scale, void* o, float* lse,
+                      void* ws, size_t ws_bytes, void* stream) {
+  la_status st = check_seqs(seqs);
+  if (st != LA_OK) return st;
+  if (!kv || max_q < 0 || isnan(scale) || isinf(scale)) return LA_ERR_ARG;
+  if (bad_kv4(kv)) return LA_ERR_SHAPE;
+  if (seqs->S == 0 || seqs->Tq == 0 || max_q == 0) return LA_OK;
+  if (bad_strides(seqs->q_token, seqs->q_head, seqs->d, false) || bad_strides(seqs->o_token, seqs->o_head, seqs->d, true))
+    return LA_ERR_SHAPE;
+  if (!q || !o || !cache || !cu_q || !lens || !table) return LA_ERR_ARG;
+  if (misaligned(q) || misaligned(o) || misaligned(cache)) return LA_ERR_ARG;
+  if (((uintptr_t)cu_q | (uintptr_t)lens | (uintptr_t)table | (uintptr_t)lse) & 3u) return LA_ERR_ARG;
+  CachePlan c = cache_plan(*seqs, *kv, max_q);
+  if (!ws || ws_bytes < c.bytes || ((uintptr_t)ws & 255u)) return LA_ERR_WORKSPACE;
+  const CacheGeom cg = cache_geom(*seqs, *kv, cache, table);
+  SeqIo io = seq_io(*seqs, q, o, lse, scale);
+  c.token.cu_q = c.many_rows.cu_q = cu_q;
+  c.token.ks = c.many_rows.ks = lens;
+  // one after the other on the stream, so they may use the same scratch
+  set_parts(&io, part_layout(c.p_token, c.rows, seqs->d, ws));
+  int have = device_workgroups(kTokenPerCu);
+  hipError_t e = launch_cache_tokens(c.token, io, cg, seqs->d, c.rows, c.p_token < have ? c.p_token : have,
+                                     (hipStream_t)stream);
+  if (e == hipSuccess && c.many) {
+    set_parts(&io, part_layout(c.p_many, kRows, seqs->d, ws));
+    have = device_workgroups(1);
+    e = launch_cache_rows(c.many_rows, io, cg, seqs->d, c.p_many < have ? c.p_many : have, (hipStream_t)stream);
+  }
   return e == hipSuccess ? LA_OK : LA_ERR_HIP;
 }
 

@@ -451,6 +451,18 @@ hipError_t launch_prompt_attn(const SeqGeom& g, const SeqIo& io, int d, int P, h
   return d == 128 ? launch_rows<128, false>(g, io, none, P, st) : launch_rows<64, false>(g, io, none, P, st);
 }
 
+hipError_t launch_cache_merge(const SeqGeom& g, const SeqIo& io, int d, int rows, int P, hipStream_t st) {
+  const dim3 grid(P, rows / 16);
+  if (d == 128) {
+    if (rows == 16) hipLaunchKernelGGL((seq_merge_kernel<128, 16, true>), grid, dim3(256), 0, st, g, io, P);
+    else hipLaunchKernelGGL((seq_merge_kernel<128, 32, true>), grid, dim3(256), 0, st, g, io, P);
+  } else {
+    if (rows == 16) hipLaunchKernelGGL((seq_merge_kernel<64, 16, true>), grid, dim3(256), 0, st, g, io, P);
+    else hipLaunchKernelGGL((seq_merge_kernel<64, 32, true>), grid, dim3(256), 0, st, g, io, P);
+  }
+  return hipGetLastError();
+}
+
 hipError_t launch_cache_rows(const SeqGeom& g, const SeqIo& io, const CacheGeom& cg, int d, int P, hipStream_t st) {
   return d == 128 ? launch_rows<128, true>(g, io, cg, P, st) : launch_rows<64, true>(g, io, cg, P, st);
 }

@@ -50,6 +50,11 @@ class Seqs(ctypes.Structure):
                                               "v_head")]
 
 
+class Kv4(ctypes.Structure):
+    """la_kv4: the pages of a 4-bit cache."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_pages", "page", "max_pages")]
+
+
 LA_PART_TEXT, LA_PART_CONTEXT, LA_PART_CHUNK, LA_PART_ALL = 1, 2, 4, 7
 
 _lib = None
@@ -58,6 +63,7 @@ _P = ctypes.c_void_p
 _SP = ctypes.POINTER(Shape)
 _GP = ctypes.POINTER(Grid3D)
 _QP = ctypes.POINTER(Seqs)
+_KP = ctypes.POINTER(Kv4)
 
 _SIGNATURES = {
     "la_workspace_bytes": (ctypes.c_size_t, [_SP]),
@@ -83,6 +89,12 @@ _SIGNATURES = {
     "la_untile_o_3d": (ctypes.c_int, [_GP, _P, _P, _P, _P, _P]),
     "la_prompt_ws_bytes": (ctypes.c_size_t, [_QP]),
     "la_prompt_attn": (ctypes.c_int, [_QP, _P, _P, _P, _P, _P, ctypes.c_float, _P, _P, _P, ctypes.c_size_t, _P]),
+    "la_kv4_page_bytes": (ctypes.c_size_t, [ctypes.c_int32, ctypes.c_int32]),
+    "la_kv4_append": (ctypes.c_int, [_QP, _KP, _P, _P, _P, _P, _P, _P, _P]),
+    "la_kv4_read": (ctypes.c_int, [_QP, _KP, _P, _P, _P, _P, _P, _P, _P]),
+    "la_kv4_ws_bytes": (ctypes.c_size_t, [_QP, _KP, ctypes.c_int32]),
+    "la_kv4_attn": (ctypes.c_int, [_QP, _KP, ctypes.c_int32, _P, _P, _P, _P, _P, ctypes.c_float, _P, _P, _P,
+                                   ctypes.c_size_t, _P]),
     "la_latent_mse": (ctypes.c_int, [_P, _P, ctypes.c_int64, ctypes.c_int32, _P, _P, ctypes.c_size_t, _P]),
     "la_dynamics_ema": (ctypes.c_int, [ctypes.c_double, _P, ctypes.c_double, _P]),
     "la_temporal_window": (ctypes.c_int, [ctypes.c_double, ctypes.c_double, ctypes.c_int32, _P]),
@@ -615,6 +627,90 @@ def prompt_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.T
     ws, nbytes = _scratch(int(lib().la_prompt_ws_bytes(ctypes.byref(seqs))), q.device, ws)
     _on_device_of(q, "la_prompt_attn", ctypes.byref(seqs), _ptr(q), _ptr(k), _ptr(v), _ptr(cu_q), _ptr(cu_k),
                   scale if scale is not None else 0.0, _ptr(o), _ptr(lse), _ptr(ws), nbytes, _stream(q))
+    return o if lse is None else (o, lse)
+
+
+def kv4_cache(n_pages: int, Hkv: int, d: int, page: int = 64, device="cuda") -> torch.Tensor:
+    """An empty 4-bit cache: uint8 [n_pages, Hkv, page (d + d / 16)], `page` tokens to a page (a power of
+    two, 16 to 1024)."""
+    nbytes = int(lib().la_kv4_page_bytes(d, page))
+    if nbytes == 0:
+        raise ValueError(f"no 4-bit cache for d = {d} and pages of {page} tokens")
+    return torch.zeros((n_pages, Hkv, nbytes), dtype=torch.uint8, device=device)
+
+
+def _check_cache(cache, lens, table, cu, d):
+    """The la_kv4 of a cache, its page lengths and its table; raises for what does not fit."""
+    if not isinstance(cache, torch.Tensor) or cache.device.type != "cuda":
+        raise TypeError("cache must be a GPU tensor")
+    if cache.dtype != torch.uint8 or cache.dim() != 3 or not cache.is_contiguous():
+        raise TypeError("cache must be a contiguous uint8 [n_pages, Hkv, page bytes] tensor")
+    page, rest = divmod(cache.shape[2], d + d // 16)
+    if rest or lib().la_kv4_page_bytes(d, page) != cache.shape[2]:
+        raise ValueError(f"a cache of {cache.shape[2]} bytes a page is none for heads of {d}")
+    if not isinstance(table, torch.Tensor) or table.dim() != 2:
+        raise ValueError("table must be an int32 [S, max_pages] tensor")
+    S = table.shape[0]
+    _check_ints("table", table, cache.device, (S, table.shape[1]))
+    _check_ints("lens", lens, cache.device, (S,))
+    _check_ints("cu", cu, cache.device, (S + 1,))
+    return Kv4(cache.shape[0], page, table.shape[1])
+
+
+def kv4_append(cache: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: torch.Tensor, lens: torch.Tensor,
+               table: torch.Tensor) -> None:
+    """Enters k, v (bf16 [T, Hkv, d], free strides) into a 4-bit cache: rows [cu[s], cu[s + 1]) are the
+    last tokens of sequence s, which has lens[s] with them, on the pages table[s].  cu int32 [S + 1],
+    lens int32 [S], table int32 [S, max_pages], all on the GPU."""
+    _check_rows("k", k)
+    T, Hkv, d = k.shape
+    _check_rows("v", v, k.device, Hkv, d, T)
+    kv = _check_cache(cache, lens, table, cu, d)
+    if cache.device != k.device or cache.shape[1] != Hkv:
+        raise ValueError(f"cache of {cache.shape[1]} heads on {cache.device}, k of {Hkv} on {k.device}")
+    seqs = Seqs(table.shape[0], 0, T, Hkv, Hkv, d, 0, 0, 0, 0, 0, *_strides(k), *_strides(v))
+    _on_device_of(k, "la_kv4_append", ctypes.byref(seqs), ctypes.byref(kv), _ptr(k), _ptr(v), _ptr(cu), _ptr(lens),
+                  _ptr(table), _ptr(cache), _stream(k))
+
+
+def kv4_read(cache: torch.Tensor, cu: torch.Tensor, lens: torch.Tensor, table: torch.Tensor, tokens: int, d: int,
+             out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None):
+    """The values that the last cu[s + 1] - cu[s] tokens of every sequence stand for -> (k, v) bf16
+    [tokens, Hkv, d] (or the given pair, of any strides): what kv4_append entered there, rounded."""
+    kv = _check_cache(cache, lens, table, cu, d)
+    Hkv = cache.shape[1]
+    if out is None:
+        k, v = (torch.empty((tokens, Hkv, d), dtype=torch.bfloat16, device=cache.device) for _ in range(2))
+    else:
+        k, v = out
+    for name, t in (("k", k), ("v", v)):
+        _check_rows(name, t, cache.device, Hkv, d, tokens)
+    seqs = Seqs(table.shape[0], 0, tokens, Hkv, Hkv, d, 0, 0, 0, 0, 0, *_strides(k), *_strides(v))
+    _on_device_of(cache, "la_kv4_read", ctypes.byref(seqs), ctypes.byref(kv), _ptr(cache), _ptr(cu), _ptr(lens),
+                  _ptr(table), _ptr(k), _ptr(v), _stream(cache))
+    return k, v
+
+
+def kv4_attn(q: torch.Tensor, cache: torch.Tensor, cu_q: torch.Tensor, lens: torch.Tensor, table: torch.Tensor,
+             max_q: int, causal: bool = True, scale: Optional[float] = None, want_lse: bool = False,
+             ws: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+             lse_out: Optional[torch.Tensor] = None):
+    """Attention of packed queries over a 4-bit cache -> o bf16 [Tq, Hq, d] (and lse fp32 [Tq, Hq]).
+
+    q [Tq, Hq, d] in bf16 with free strides; sequence s has the rows [cu_q[s], cu_q[s + 1]), at most max_q
+    of them (1: the next token of every sequence), and lens[s] tokens in the cache (see kv4_append).
+    Causal: the last query of a sequence sees the last token, its queries being the last tokens."""
+    _check_rows("q", q)
+    Tq, Hq, d = q.shape
+    kv = _check_cache(cache, lens, table, cu_q, d)
+    if cache.device != q.device:
+        raise ValueError(f"cache is on {cache.device}, q on {q.device}")
+    o, lse = _outputs(q, want_lse, out, lse_out)
+    seqs = Seqs(table.shape[0], Tq, 0, Hq, cache.shape[1], d, 1 if causal else 0, *_strides(q), *_strides(o), 0, 0, 0, 0)
+    ws, nbytes = _scratch(int(lib().la_kv4_ws_bytes(ctypes.byref(seqs), ctypes.byref(kv), max_q)), q.device, ws)
+    _on_device_of(q, "la_kv4_attn", ctypes.byref(seqs), ctypes.byref(kv), max_q, _ptr(q), _ptr(cache), _ptr(cu_q),
+                  _ptr(lens), _ptr(table), scale if scale is not None else 0.0, _ptr(o), _ptr(lse), _ptr(ws), nbytes,
+                  _stream(q))
     return o if lse is None else (o, lse)
 
 

@@ -70,3 +70,87 @@ def test_binding_refuses_cpu_tensors():
     cu = torch.zeros(2, dtype=torch.int32)
     with pytest.raises(TypeError):
         la.prompt_attn(q, q, q, cu)
+
+
+def kv4(**kw):
+    f = dict(n_pages=10, page=64, max_pages=4)
+    f.update(kw)
+    return la.Kv4(f["n_pages"], f["page"], f["max_pages"])
+
+
+def append(s, c, k=P, v=P, cu=P, lens=P, table=P, cache=P):
+    return la.lib().la_kv4_append(None if s is None else ctypes.byref(s), None if c is None else ctypes.byref(c), k, v, cu,
+                                  lens, table, cache, None)
+
+
+def read(s, c, k=P, v=P, cu=P, lens=P, table=P, cache=P):
+    return la.lib().la_kv4_read(None if s is None else ctypes.byref(s), None if c is None else ctypes.byref(c), cache, cu,
+                                lens, table, k, v, None)
+
+
+def attn(s, c, max_q=1, q=P, cache=P, cu=P, lens=P, table=P, scale=0.0, o=P, lse=None, ws=P, nbytes=1 << 40):
+    return la.lib().la_kv4_attn(None if s is None else ctypes.byref(s), None if c is None else ctypes.byref(c), max_q, q,
+                                cache, cu, lens, table, ctypes.c_float(scale), o, lse, ws, nbytes, None)
+
+
+BAD_KV4 = [dict(n_pages=0), dict(page=8), dict(page=48), dict(page=2048), dict(page=0), dict(max_pages=0)]
+
+
+@cpu_only
+@pytest.mark.parametrize("bad", BAD_KV4, ids=str)
+def test_kv4_shapes_refused(bad):
+    for call in (append, read, attn):
+        assert call(seqs(), kv4(**bad)) == la.LA_ERR_SHAPE, call
+    assert la.lib().la_kv4_ws_bytes(ctypes.byref(seqs()), ctypes.byref(kv4(**bad)), 1) == 0
+
+
+@cpu_only
+def test_kv4_arguments_refused():
+    s, c = seqs(), kv4()
+    for call in (append, read, attn):
+        assert call(None, c) == la.LA_ERR_ARG
+        assert call(s, None) == la.LA_ERR_ARG
+        assert call(seqs(d=96), c) == la.LA_ERR_SHAPE
+        assert call(seqs(Hkv=3), c) == la.LA_ERR_SHAPE
+        for name in ("cu", "lens", "table", "cache"):
+            assert call(s, c, **{name: None}) == la.LA_ERR_ARG, (call, name)
+        assert call(s, c, cache=ODD) == la.LA_ERR_ARG
+        for name in ("cu", "lens", "table"):
+            assert call(s, c, **{name: ctypes.c_void_p(4098)}) == la.LA_ERR_ARG, (call, name)
+    for call in (append, read):
+        for name in ("k", "v"):
+            assert call(s, c, **{name: None}) == la.LA_ERR_ARG
+            assert call(s, c, **{name: ODD}) == la.LA_ERR_ARG
+        assert call(seqs(k_token=64), c) == la.LA_ERR_SHAPE
+        assert call(seqs(v_head=4), c) == la.LA_ERR_SHAPE
+        assert call(seqs(Tk=0), c, k=None, v=None) == la.LA_OK
+        assert call(seqs(S=0), c, k=None, v=None) == la.LA_OK
+    assert read(seqs(v_head=0), c) == la.LA_ERR_SHAPE            # rows that are written lie apart
+    for name in ("q", "o"):
+        assert attn(s, c, **{name: None}) == la.LA_ERR_ARG
+        assert attn(s, c, **{name: ODD}) == la.LA_ERR_ARG
+    assert attn(seqs(q_token=64), c) == la.LA_ERR_SHAPE
+    assert attn(seqs(o_head=0), c) == la.LA_ERR_SHAPE
+    assert attn(s, c, max_q=-1) == la.LA_ERR_ARG
+    assert attn(s, c, scale=float("nan")) == la.LA_ERR_ARG
+    assert attn(s, c, lse=ctypes.c_void_p(4097)) == la.LA_ERR_ARG
+    for max_q in (1, 17, 100):
+        need = la.lib().la_kv4_ws_bytes(ctypes.byref(s), ctypes.byref(c), max_q)
+        assert need > 0
+        assert attn(s, c, max_q, ws=None) == la.LA_ERR_WORKSPACE
+        assert attn(s, c, max_q, nbytes=need - 1) == la.LA_ERR_WORKSPACE
+        assert attn(s, c, max_q, ws=ctypes.c_void_p(4096 + 64)) == la.LA_ERR_WORKSPACE
+    for empty in (dict(S=0), dict(Tq=0)):
+        assert attn(seqs(**empty), c, q=None, o=None, ws=None, nbytes=0) == la.LA_OK
+    assert attn(s, c, max_q=0, ws=None, nbytes=0) == la.LA_OK
+
+
+def test_kv4_page_bytes():
+    f = la.lib().la_kv4_page_bytes
+    assert f(128, 16) == 16 * 136 and f(64, 1024) == 1024 * 68
+    assert f(96, 64) == 0 and f(128, 24) == 0 and f(128, 8) == 0 and f(128, 2048) == 0
+    with pytest.raises(ValueError):
+        la.kv4_cache(1, 1, 80, 64, device="cpu")
+    with pytest.raises(TypeError):
+        la.kv4_read(la.kv4_cache(1, 1, 64, 64, device="cpu"), torch.zeros(2, dtype=torch.int32),
+                    torch.zeros(1, dtype=torch.int32), torch.zeros((1, 1), dtype=torch.int32), 1, 64)
