@@ -56,6 +56,9 @@ typedef enum la_status {
   LA_ERR_HIP = 4         /* a HIP launch failed */
 } la_status;
 
+/* Element types, where a call takes more than bf16. */
+typedef enum la_dtype { LA_DTYPE_F32 = 0, LA_DTYPE_BF16 = 1 } la_dtype;
+
 /* Problem shape.
  *   B, H        batch and heads (>= 1); every (b, h) is independent (Sec. 3.3:
  *               pooling and selection run per attention head).
@@ -308,6 +311,35 @@ la_status la_untile_o_3d(const la_grid3d* grid, const void* o_tiled, const float
                          float* lse, void* stream);
 
 /* ------------------------------------------------------------------------------
+ * Rotary positions: what turns queries and keys by their tokens' positions before an attention call.
+ * Pair j of a head's first `rot` values is turned by positions[axis of j][token] * freqs[j] radians,
+ *   (a, b) -> amplitude (a cos - b sin, b cos + a sin);
+ * the pairs are (j, j + rot / 2), or with interleaved = 1 (2 j, 2 j + 1); the values from `rot` on are
+ * copied.  Angles are computed in 64 bits, so far positions keep their precision; a negative position
+ * turns back, and turning by -p undoes (and is the gradient of) turning by p at amplitude 1.
+ * -------------------------------------------------------------------------- */
+typedef struct la_rope_shape {
+  int32_t B, L;              /* sequences of L tokens that share their positions (packed tokens: B = 1) */
+  int32_t Hq, Hk;            /* heads of q and of k; 0: that tensor is not given */
+  int32_t d;                 /* 64 or 128 */
+  int32_t rot;               /* values of a head that are turned: a multiple of 16, 16 to d */
+  int32_t interleaved;       /* 0 or 1 */
+  int32_t dtype;             /* la_dtype of q and k and their outputs */
+  int32_t axes;              /* rows of positions, 1 to 3 */
+  int32_t section[3];        /* pairs of each axis, in the order of the pairs; they add up to rot / 2 */
+  int64_t q_batch, q_token, q_head, qo_batch, qo_token, qo_head;    /* strides in elements, multiples of 8 */
+  int64_t k_batch, k_token, k_head, ko_batch, ko_token, ko_head;
+} la_rope_shape;
+
+/*   q, k       rows of d contiguous values with the strides above, 16-byte aligned
+ *   q_out, k_out  the same; each may be its input (with its strides)
+ *   positions  int32 [axes, L] (device);  freqs  double [rot / 2] (device): radians per position.
+ * One kernel launch.  LA_ERR_SHAPE for shapes and strides that do not fit, LA_ERR_ARG for pointers, a
+ * bad dtype and an amplitude that is not finite. */
+la_status la_rope(const la_rope_shape* shape, const void* q, void* q_out, const void* k, void* k_out,
+                  const int32_t* positions, const double* freqs, float amplitude, void* stream);
+
+/* ------------------------------------------------------------------------------
  * Packed sequences: attention over whole prompts, and over a cache in 4 bits.
  *
  * Tokens of S sequences of different lengths lie behind one another, q and o [Tq, Hq, d], k and v
@@ -403,8 +435,6 @@ la_status la_kv4_attn(const la_seqs* seqs, const la_kv4* kv, int32_t max_q, cons
  * Camera-pose similarities are inputs: the paper instantiates them with an FOV
  * overlap measure it does not define.
  * -------------------------------------------------------------------------- */
-typedef enum la_dtype { LA_DTYPE_F32 = 0, LA_DTYPE_BF16 = 1 } la_dtype;
-
 /* Workspace bytes of la_latent_mse (fp64 partial sums; 256-byte aligned). */
 #define LA_LATENT_MSE_WS_BYTES 8192
 

@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import torch
 
@@ -43,6 +43,13 @@ class Grid3D(ctypes.Structure):
         return "Grid3D(" + ", ".join(f"{n}={getattr(self, n)}" for n, _ in self._fields_) + ")"
 
 
+class RopeShape(ctypes.Structure):
+    """la_rope_shape."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "L", "Hq", "Hk", "d", "rot", "interleaved", "dtype", "axes")] + \
+               [("section", ctypes.c_int32 * 3)] + \
+               [(f"{t}_{n}", ctypes.c_int64) for t in ("q", "qo", "k", "ko") for n in ("batch", "token", "head")]
+
+
 class Seqs(ctypes.Structure):
     """la_seqs: packed sequences and the strides of their tensors."""
     _fields_ = [(n, ctypes.c_int32) for n in ("S", "Tq", "Tk", "Hq", "Hkv", "d", "causal")] + \
@@ -64,6 +71,7 @@ _SP = ctypes.POINTER(Shape)
 _GP = ctypes.POINTER(Grid3D)
 _QP = ctypes.POINTER(Seqs)
 _KP = ctypes.POINTER(Kv4)
+_RP = ctypes.POINTER(RopeShape)
 
 _SIGNATURES = {
     "la_workspace_bytes": (ctypes.c_size_t, [_SP]),
@@ -87,6 +95,7 @@ _SIGNATURES = {
                                                 ctypes.c_size_t, _P]),
     "la_sparse_attn_plan_valid": (ctypes.c_int, [_SP, _P, _P, _P, _P, ctypes.c_size_t, _P]),
     "la_untile_o_3d": (ctypes.c_int, [_GP, _P, _P, _P, _P, _P]),
+    "la_rope": (ctypes.c_int, [_RP, _P, _P, _P, _P, _P, _P, ctypes.c_float, _P]),
     "la_prompt_ws_bytes": (ctypes.c_size_t, [_QP]),
     "la_prompt_attn": (ctypes.c_int, [_QP, _P, _P, _P, _P, _P, ctypes.c_float, _P, _P, _P, ctypes.c_size_t, _P]),
     "la_kv4_page_bytes": (ctypes.c_size_t, [ctypes.c_int32, ctypes.c_int32]),
@@ -517,13 +526,43 @@ def bind_3d(g: Grid3D, q, k, v, q_t, k_t, v_t, qbar, kbar, mask, counts, idx, kv
     return prep_q, prep_kv, select, plan, run, merge, untile
 
 
+def grid3d_positions(g: Grid3D, frames=None, device="cuda"):
+    """Positions (frame, row, column) of the linear-order tokens of a grid, int32 [3, n]: (of the queries, of
+    the keys).  frames: the positions of the T_ctx + T_q frames (retrieved frames need not be neighbours of the
+    chunk); None numbers them from 0.  Text tokens have the position 0 on every axis (they are not turned)."""
+    T = g.T_ctx + g.T_q
+    f = torch.arange(T) if frames is None else torch.as_tensor(frames)
+    if tuple(f.shape) != (T,):
+        raise ValueError(f"frames must hold {T} positions")
+    p = torch.stack(torch.meshgrid(f.to(torch.int32), torch.arange(g.Hs, dtype=torch.int32),
+                                   torch.arange(g.Ws, dtype=torch.int32), indexing="ij")).flatten(1)
+    k = torch.cat([torch.zeros((3, g.n_text), dtype=torch.int32), p], 1)
+    return p[:, g.T_ctx * g.Hs * g.Ws:].contiguous().to(device), k.to(device)
+
+
+class Rope(NamedTuple):
+    """How a path turns its queries and keys (see rope): frequencies, pairs of each axis, and positions."""
+    freqs: torch.Tensor
+    sections: Tuple[int, ...]
+    q_positions: torch.Tensor
+    k_positions: torch.Tensor
+    interleaved: bool = True
+    amplitude: float = 1.0
+
+
 def sparse_attn_3d(g: Grid3D, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, tau: Optional[float] = None,
                    keep_blocks: Optional[int] = None, scale: Optional[float] = None, want_lse: bool = False,
-                   kvalid: Optional[torch.Tensor] = None):
+                   kvalid: Optional[torch.Tensor] = None, rotary: Optional[Rope] = None):
     """The whole 3-D path on linear-order inputs: Q-Prep, KV-Prep, selection from the pooled means,
-    attention over the tiled buffers with the padding masked, Untile Scatter.  Returns
-    (o linear, lse linear or None, mask over the tiled blocks, counts, idx)."""
+    attention over the tiled buffers with the padding masked, Untile Scatter.  rotary: q and k are turned by
+    their positions first (grid3d_positions).  Returns (o linear, lse linear or None, mask over the tiled
+    blocks, counts, idx)."""
     shape = grid3d_shape(g)
+    if rotary is not None:
+        q = rope(q, rotary.q_positions, rotary.freqs, interleaved=rotary.interleaved, sections=rotary.sections,
+                 amplitude=rotary.amplitude)
+        k = rope(k, rotary.k_positions, rotary.freqs, interleaved=rotary.interleaved, sections=rotary.sections,
+                 amplitude=rotary.amplitude)
     if kvalid is None:
         kvalid = torch.from_numpy(grid3d_valid(g)[1]).to(q.device)
     q_t, qbar = prep_q_3d(g, q)
@@ -535,6 +574,110 @@ def sparse_attn_3d(g: Grid3D, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
     o_t, lse_t = res if want_lse else (res, None)
     o, lse = untile_o_3d(g, o_t, lse_t)
     return o, lse, mask, counts, idx
+
+
+# ----------------------------------------------------------------------------------------------
+# rotary positions
+
+LA_DTYPE_F32, LA_DTYPE_BF16 = 0, 1
+_DTYPES = {torch.float32: LA_DTYPE_F32, torch.bfloat16: LA_DTYPE_BF16}
+
+
+def rope_frequencies(rot: int, base: float = 10000.0, sections: Optional[Tuple[int, ...]] = None,
+                     scaling: Optional[str] = None, factor: float = 1.0, trained: int = 0, turns=(1.0, 32.0),
+                     device="cuda") -> torch.Tensor:
+    """Radians per position of the rot / 2 pairs, float64: base^(-2 j / rot), or with `sections` (the pairs of
+    each axis, adding up to rot / 2) a ladder base^(-i / n) of its own for every axis of n pairs.
+
+    scaling  for contexts `factor` times as long as the trained ones:
+      "linear"  every frequency divided by factor (positions interpolated);
+      "base"    base multiplied by factor^(rot / (rot - 2)): the slowest pair is interpolated, the fastest kept;
+      "ramp"    pairs that make fewer than turns[0] turns over the `trained` positions are interpolated, those of
+                more than turns[1] are kept, and between them the two are mixed linearly in the turns."""
+    if rot < 2 or rot % 2:
+        raise ValueError("rot must be a positive even number")
+    if base <= 0 or factor <= 0:
+        raise ValueError("base and factor must be positive")
+    if scaling == "base":
+        if rot == 2 or sections is not None:
+            raise ValueError("base scaling needs one axis of more than one pair")
+        base = base * factor ** (rot / (rot - 2))
+    parts = tuple(sections) if sections is not None else (rot // 2,)
+    if sum(parts) != rot // 2 or min(parts) < 0:
+        raise ValueError("sections must add up to rot / 2")
+    f = torch.cat([float(base) ** (-torch.arange(n, dtype=torch.float64) / max(n, 1)) for n in parts])
+    if scaling == "linear":
+        f = f / factor
+    elif scaling == "ramp":
+        if trained < 1 or not turns[0] < turns[1]:
+            raise ValueError("ramp scaling needs the trained length, and turns in ascending order")
+        keep = ((trained * f / 6.283185307179586 - turns[0]) / (turns[1] - turns[0])).clamp(0.0, 1.0)
+        f = f * (keep + (1.0 - keep) / factor)
+    elif scaling not in (None, "base"):
+        raise ValueError(f"unknown scaling {scaling!r}")
+    return f.to(device)
+
+
+def _rope_rows(name, t, like=None):
+    """(B, L, H, d) and (batch, token, head) strides of [tokens, heads, d] or [B, heads, L, d] rows."""
+    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+        raise TypeError(f"{name} must be a GPU tensor")
+    if t.dtype not in _DTYPES or t.dim() not in (3, 4):
+        raise TypeError(f"{name} must be a float32 or bfloat16 [tokens, heads, d] or [B, heads, L, d] tensor")
+    if like is not None and (t.dim() != like.dim() or t.dtype != like.dtype or t.device != like.device):
+        raise ValueError(f"{name} differs in form, type or device from q")
+    if t.dim() == 3:
+        (L, H, d), B, (st, sh, sd), sb = t.shape, 1, t.stride(), 0
+    else:
+        (B, H, L, d), (sb, sh, st, sd) = t.shape, t.stride()
+    if t.numel() and sd != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    # strides of an extent of one mean nothing
+    strides = (sb if B > 1 else 8, st if L > 1 else 8, sh if H > 1 else 8)
+    if t.numel() and any(s % 8 for s in strides):
+        raise ValueError(f"{name} must have strides that are multiples of 8")
+    return (B, L, H, d), strides
+
+
+def rope(q: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, k: Optional[torch.Tensor] = None,
+         interleaved: bool = False, sections: Optional[Tuple[int, ...]] = None, amplitude: float = 1.0,
+         out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
+    """Queries (and keys) turned by their tokens' positions -> the same shape and type (a pair with k).
+
+    q, k  bf16 or fp32, [tokens, heads, d] or [B, heads, L, d], any strides that are multiples of 8.
+    positions  int32 [tokens] (or [L], shared by the batch), or with sections [axes, tokens]: the pairs of
+    each axis, e.g. those of (frame, row, column).  freqs  float64 [rot / 2] (rope_frequencies): the first rot
+    values of a head are turned, the others copied.  interleaved: pairs (2 j, 2 j + 1) instead of
+    (j, j + rot / 2).  out and k_out may be q and k."""
+    (B, L, Hq, d), qs = _rope_rows("q", q)
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    oshape, os = _rope_rows("out", out, q)
+    if oshape != (B, L, Hq, d):
+        raise ValueError(f"out has shape {tuple(out.shape)}, q has {tuple(q.shape)}")
+    Hk, ks, kos = 0, (0, 0, 0), (0, 0, 0)
+    if k is not None:
+        kshape, ks = _rope_rows("k", k, q)
+        if k_out is None:
+            k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
+        koshape, kos = _rope_rows("k_out", k_out, q)
+        Hk = kshape[2]
+        if kshape != (B, L, Hk, d) or koshape != kshape:
+            raise ValueError(f"k has shape {tuple(k.shape)} and k_out {tuple(k_out.shape)}, q has {tuple(q.shape)}")
+    axes = 1 if sections is None else len(sections)
+    if not isinstance(freqs, torch.Tensor) or freqs.device != q.device or freqs.dtype != torch.float64 \
+            or freqs.dim() != 1 or not freqs.is_contiguous():
+        raise ValueError(f"freqs must be a contiguous float64 [rot / 2] tensor on {q.device}")
+    pairs = freqs.shape[0]
+    if not 1 <= axes <= 3 or (sections is not None and sum(sections) != pairs):
+        raise ValueError("sections must be the pairs of one to three axes, rot / 2 in all")
+    _check_ints("positions", positions, q.device, (L,) if sections is None else (axes, L))
+    section = (tuple(sections) if sections is not None else (pairs,)) + (0,) * (3 - axes)
+    shape = RopeShape(B, L, Hq, Hk, d, 2 * pairs, 1 if interleaved else 0, _DTYPES[q.dtype], axes,
+                      (ctypes.c_int32 * 3)(*section), *qs, *os, *ks, *kos)
+    _on_device_of(q, "la_rope", ctypes.byref(shape), _ptr(q), _ptr(out), _ptr(k), _ptr(k_out), _ptr(positions),
+                  _ptr(freqs), amplitude, _stream(q))
+    return out if k is None else (out, k_out)
 
 
 # ----------------------------------------------------------------------------------------------
@@ -717,7 +860,6 @@ def kv4_attn(q: torch.Tensor, cache: torch.Tensor, cu_q: torch.Tensor, lens: tor
 # ----------------------------------------------------------------------------------------------
 # scalar policy (Sec. 3.1, Sec. 3.2)
 
-LA_DTYPE_F32, LA_DTYPE_BF16 = 0, 1
 LATENT_MSE_WS_BYTES = 8192
 
 
