@@ -27,9 +27,10 @@ la_status check_seqs(const la_seqs* s) {
 
 constexpr int kRows = 256;              // packed rows of a workgroup (seq_attn.hip)
 constexpr uint32_t kMinShare = 256;     // keys
+constexpr uint32_t kRowsExtra = 512, kTokenExtra = 384;    // what starting and ending a unit costs, in keys
 constexpr int kMaxWorkgroups = 256;
 
-SeqGeom seq_geom(const la_seqs& s, int rows, int kcap) {
+SeqGeom seq_geom(const la_seqs& s, int rows, int kcap, uint32_t extra) {
   SeqGeom g{};
   g.S = s.S;
   g.Tq = s.Tq;
@@ -43,6 +44,7 @@ SeqGeom seq_geom(const la_seqs& s, int rows, int kcap) {
   g.GS = ceil_div(g.G, g.GH);
   g.TB = rows / g.GH;
   g.causal = s.causal;
+  g.extra = extra;
   g.min_share = kMinShare;
   return g;
 }
@@ -51,7 +53,7 @@ SeqGeom seq_geom(const la_seqs& s, int rows, int kcap) {
 // at most kcap keys, kall in all).
 int workgroups(const SeqGeom& g, int64_t kall, int most) {
   const double units = (double)g.Hkv * g.GS * ((double)g.Tq / g.TB + (g.S < g.Tq ? g.S : g.Tq));
-  const double shares = ceil(units * (double)(kall > 0 ? kall : 1) / g.min_share);
+  const double shares = ceil(units * ((double)kall + g.extra) / g.min_share);
   const int want = shares < most ? (int)shares : most;
   return (want + 7) / 8 * 8;
 }
@@ -135,12 +137,12 @@ CachePlan cache_plan(const la_seqs& s, const la_kv4& kv, int max_q) {
   c.lq_token = G >= kTokenRows ? 1 : kTokenRows / G;
   c.many = max_q > c.lq_token;
   c.rows = (int64_t)(c.many ? c.lq_token : max_q) * G <= 16 ? 16 : 32;
-  c.token = seq_geom(s, c.rows, cap);
+  c.token = seq_geom(s, c.rows, cap, kTokenExtra);
   c.token.lq_max = c.many ? c.lq_token : max_q;
   c.p_token = workgroups(c.token, cap, kMaxWorkgroups * kTokenPerCu);
   c.bytes = part_layout(c.p_token, c.rows, s.d, nullptr).bytes;
   if (c.many) {
-    c.many_rows = seq_geom(s, kRows, cap);
+    c.many_rows = seq_geom(s, kRows, cap, kRowsExtra);
     c.many_rows.lq_min = c.lq_token + 1;
     c.many_rows.lq_max = max_q;
     c.p_many = workgroups(c.many_rows, cap, kMaxWorkgroups);
@@ -171,7 +173,7 @@ extern "C" {
 
 size_t la_prompt_ws_bytes(const la_seqs* seqs) {
   if (check_seqs(seqs) != LA_OK || seqs->S == 0 || seqs->Tq == 0) return 0;
-  const SeqGeom g = seq_geom(*seqs, kRows, seqs->Tk);
+  const SeqGeom g = seq_geom(*seqs, kRows, seqs->Tk, kRowsExtra);
   return part_layout(workgroups(g, seqs->Tk, kMaxWorkgroups), kRows, seqs->d, nullptr).bytes;
 }
 
@@ -190,7 +192,7 @@ la_status la_prompt_attn(const la_seqs* seqs, const void* q, const void* k, cons
   if (!q || !o || !cu_q || !cu_k || (seqs->Tk > 0 && (!k || !v))) return LA_ERR_ARG;
   if (misaligned(q) || misaligned(o) || misaligned(k) || misaligned(v)) return LA_ERR_ARG;
   if (((uintptr_t)cu_q | (uintptr_t)cu_k | (uintptr_t)lse) & 3u) return LA_ERR_ARG;
-  SeqGeom g = seq_geom(*seqs, kRows, seqs->Tk);
+  SeqGeom g = seq_geom(*seqs, kRows, seqs->Tk, kRowsExtra);
   g.cu_q = cu_q;
   g.ks = cu_k;
   const int most = workgroups(g, seqs->Tk, kMaxWorkgroups);

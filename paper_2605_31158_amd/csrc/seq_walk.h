@@ -3,12 +3,13 @@
 // A unit is a run of at most TB query tokens of one sequence with the GH query heads of one head
 // group: R = TB GH packed rows (row r is token r / GH, head r % GH), which all read the same keys.
 // A head group is the G query heads of a key head, or, where G > R, a part of at most R of them.
-// A unit weighs the keys that its last token sees (at least 1, so that a row that sees nothing is
-// written too).  The units, in the order (sequence, head group, run of tokens), are laid end to end
-// on one line of weights, and workgroup l of P takes the stretch [l share, (l + 1) share): equal
-// shares whatever the lengths are, with no plan in memory and no launch for one.  A stretch covers
-// the end of one unit, whole units and the start of another; positions inside a unit are rounded up
-// to tiles of 64 keys, on both sides of a cut alike, so every tile belongs to exactly one piece.
+// A unit weighs the keys that its last token sees, and `extra` for what it costs to start and to end
+// one (a row that sees nothing is written too).  The units, in the order (sequence, head group, run of
+// tokens), are laid end to end on one line of weights, and workgroup l of P takes the stretch
+// [l share, (l + 1) share): equal shares whatever the lengths are, with no plan in memory and no launch
+// for one.  A stretch covers the end of one unit, whole units and the start of another; a place inside
+// a unit, less the extra, is rounded up to tiles of 64 keys, on both sides of a cut alike, so every
+// tile belongs to exactly one piece.
 //
 // Where a unit starts on the line has a closed form (causal runs of a sequence weigh off + TB,
 // off + 2 TB, ..), so a wave finds its first unit with one scan over the sequences and a 64-way
@@ -27,7 +28,8 @@ struct SeqGeom {
   int Hq, Hkv, G, GH, GS;  // query heads, key heads, Hq / Hkv, heads of a group, groups of a key head
   int TB;                  // tokens of a unit
   int causal;
-  uint32_t min_share;      // keys; more than two tiles, so that a share inside a unit is never empty
+  uint32_t extra;          // weight of a unit beside its keys, >= 1
+  uint32_t min_share;      // more than two tiles, so that a share among a unit's keys is never empty
 };
 
 struct Seq {
@@ -66,11 +68,12 @@ __device__ __forceinline__ Seq load_seq(const SeqGeom& g, int s) {
 
 // Weight of the runs before run b (b < the sequence's runs), for one head group.
 __device__ __forceinline__ uint64_t weight_before(const SeqGeom& g, const Seq& q, int b) {
-  if (!g.causal) return (uint64_t)b * (uint32_t)max(1, q.lk);
+  const uint64_t extra = (uint64_t)b * g.extra;
+  if (!g.causal) return extra + (uint64_t)b * (uint32_t)q.lk;
   const int off = q.lk - q.lq;                         // token i sees the keys up to i + off
-  const int b0 = off < 0 ? min(b, -off / g.TB) : 0;    // runs whose last token sees nothing weigh 1
+  const int b0 = off < 0 ? min(b, -off / g.TB) : 0;    // runs whose last token sees nothing
   const int64_t n = b - b0;
-  return (uint64_t)(b0 + n * off + (int64_t)g.TB * (n * (b0 + 1 + (int64_t)b) / 2));
+  return extra + (uint64_t)(n * off + (int64_t)g.TB * (n * (b0 + 1 + (int64_t)b) / 2));
 }
 
 // Keys that the last token of run b sees.
@@ -84,7 +87,7 @@ __device__ __forceinline__ int runs_of(const SeqGeom& g, const Seq& q) { return 
 // Weight of all runs of a sequence, for one head group.
 __device__ __forceinline__ uint64_t seq_weight(const SeqGeom& g, const Seq& q) {
   const int nb = runs_of(g, q);
-  return nb == 0 ? 0 : weight_before(g, q, nb - 1) + (uint32_t)max(1, q.lk);
+  return nb == 0 ? 0 : weight_before(g, q, nb - 1) + (uint32_t)q.lk + g.extra;
 }
 
 // A wave's place on the line; everything in it is uniform.
@@ -174,13 +177,13 @@ struct Piece {
 __device__ __forceinline__ Piece walk_piece(const SeqGeom& g, const Walk& w, uint64_t* unit_end) {
   Piece p;
   p.keys = run_keys(g, w.q, w.b);
-  const uint32_t weight = (uint32_t)max(1, p.keys);
-  *unit_end = w.unit0 + weight;
+  *unit_end = w.unit0 + (uint32_t)p.keys + g.extra;
   const uint32_t xa = (uint32_t)(w.pos - w.unit0);
   const uint32_t xb = (uint32_t)((w.end < *unit_end ? w.end : *unit_end) - w.unit0);
-  p.ta = __builtin_amdgcn_readfirstlane((int)((xa + 63u) >> 6));
-  p.tb = __builtin_amdgcn_readfirstlane((int)((xb + 63u) >> 6));
-  p.n = (int)((weight + 63u) >> 6);
+  p.n = p.keys == 0 ? 1 : (int)(((uint32_t)p.keys + 63u) >> 6);
+  p.ta = __builtin_amdgcn_readfirstlane(xa <= g.extra ? 0 : (int)((xa - g.extra + 63u) >> 6));
+  p.tb = w.end >= *unit_end ? p.n : (xb <= g.extra ? 0 : (int)((xb - g.extra + 63u) >> 6));
+  p.tb = __builtin_amdgcn_readfirstlane(p.tb);
   return p;
 }
 

@@ -619,24 +619,28 @@ def rope_frequencies(rot: int, base: float = 10000.0, sections: Optional[Tuple[i
 
 
 def _rope_rows(name, t, like=None):
-    """(B, L, H, d) and (batch, token, head) strides of [tokens, heads, d] or [B, heads, L, d] rows."""
-    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+    """((B, L, H, d), (batch, token, head) strides) of [tokens, heads, d] or [B, heads, L, d] rows."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a GPU tensor")
-    if t.dtype not in _DTYPES or t.dim() not in (3, 4):
+    n = t.dim()
+    if t.dtype not in _DTYPES or (n != 3 and n != 4):
         raise TypeError(f"{name} must be a float32 or bfloat16 [tokens, heads, d] or [B, heads, L, d] tensor")
-    if like is not None and (t.dim() != like.dim() or t.dtype != like.dtype or t.device != like.device):
+    if like is not None and (n != like.dim() or t.dtype is not like.dtype or t.get_device() != like.get_device()):
         raise ValueError(f"{name} differs in form, type or device from q")
-    if t.dim() == 3:
-        (L, H, d), B, (st, sh, sd), sb = t.shape, 1, t.stride(), 0
+    if n == 3:
+        (L, H, d), B, (st, sh, sd), sb = t.shape, 1, t.stride(), 8
     else:
         (B, H, L, d), (sb, sh, st, sd) = t.shape, t.stride()
-    if t.numel() and sd != 1:
-        raise ValueError(f"{name} must have contiguous rows")
     # strides of an extent of one mean nothing
-    strides = (sb if B > 1 else 8, st if L > 1 else 8, sh if H > 1 else 8)
-    if t.numel() and any(s % 8 for s in strides):
-        raise ValueError(f"{name} must have strides that are multiples of 8")
-    return (B, L, H, d), strides
+    if B <= 1:
+        sb = 8
+    if L <= 1:
+        st = 8
+    if H <= 1:
+        sh = 8
+    if (sd != 1 or (sb | st | sh) % 8) and B * L * H * d:
+        raise ValueError(f"{name} must have contiguous rows, and strides that are multiples of 8")
+    return (B, L, H, d), (sb, st, sh)
 
 
 def rope(q: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, k: Optional[torch.Tensor] = None,
@@ -649,100 +653,117 @@ def rope(q: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, k: Optio
     each axis, e.g. those of (frame, row, column).  freqs  float64 [rot / 2] (rope_frequencies): the first rot
     values of a head are turned, the others copied.  interleaved: pairs (2 j, 2 j + 1) instead of
     (j, j + rot / 2).  out and k_out may be q and k."""
-    (B, L, Hq, d), qs = _rope_rows("q", q)
+    qshape, qs = _rope_rows("q", q)
+    B, L, Hq, d = qshape
+    packed = q.dim() == 3
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
-    oshape, os = _rope_rows("out", out, q)
-    if oshape != (B, L, Hq, d):
-        raise ValueError(f"out has shape {tuple(out.shape)}, q has {tuple(q.shape)}")
+        os = (8, max(Hq, 1) * d, d) if packed else (Hq * L * d, d, max(L, 1) * d)
+    else:
+        oshape, os = _rope_rows("out", out, q)
+        if oshape != qshape:
+            raise ValueError(f"out has shape {tuple(out.shape)}, q has {tuple(q.shape)}")
     Hk, ks, kos = 0, (0, 0, 0), (0, 0, 0)
     if k is not None:
         kshape, ks = _rope_rows("k", k, q)
+        Hk = kshape[2]
+        if kshape != (B, L, Hk, d):
+            raise ValueError(f"k has shape {tuple(k.shape)}, q has {tuple(q.shape)}")
         if k_out is None:
             k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
-        koshape, kos = _rope_rows("k_out", k_out, q)
-        Hk = kshape[2]
-        if kshape != (B, L, Hk, d) or koshape != kshape:
-            raise ValueError(f"k has shape {tuple(k.shape)} and k_out {tuple(k_out.shape)}, q has {tuple(q.shape)}")
+            kos = (8, max(Hk, 1) * d, d) if packed else (Hk * L * d, d, max(L, 1) * d)
+        else:
+            koshape, kos = _rope_rows("k_out", k_out, q)
+            if koshape != kshape:
+                raise ValueError(f"k_out has shape {tuple(k_out.shape)}, k has {tuple(k.shape)}")
     axes = 1 if sections is None else len(sections)
-    if not isinstance(freqs, torch.Tensor) or freqs.device != q.device or freqs.dtype != torch.float64 \
+    dev = q.get_device()
+    if not isinstance(freqs, torch.Tensor) or freqs.get_device() != dev or freqs.dtype is not torch.float64 \
             or freqs.dim() != 1 or not freqs.is_contiguous():
         raise ValueError(f"freqs must be a contiguous float64 [rot / 2] tensor on {q.device}")
     pairs = freqs.shape[0]
     if not 1 <= axes <= 3 or (sections is not None and sum(sections) != pairs):
         raise ValueError("sections must be the pairs of one to three axes, rot / 2 in all")
-    _check_ints("positions", positions, q.device, (L,) if sections is None else (axes, L))
-    section = (tuple(sections) if sections is not None else (pairs,)) + (0,) * (3 - axes)
+    _check_ints("positions", positions, dev, (L,) if sections is None else (axes, L))
     shape = RopeShape(B, L, Hq, Hk, d, 2 * pairs, 1 if interleaved else 0, _DTYPES[q.dtype], axes,
-                      (ctypes.c_int32 * 3)(*section), *qs, *os, *ks, *kos)
-    _on_device_of(q, "la_rope", ctypes.byref(shape), _ptr(q), _ptr(out), _ptr(k), _ptr(k_out), _ptr(positions),
-                  _ptr(freqs), amplitude, _stream(q))
+                      (pairs,) if sections is None else tuple(sections), *qs, *os, *ks, *kos)
+    _on_device(dev, "la_rope", ctypes.byref(shape), q.data_ptr(), out.data_ptr(), _ptr(k), _ptr(k_out),
+               positions.data_ptr(), freqs.data_ptr(), amplitude, _stream(q))
     return out if k is None else (out, k_out)
 
 
 # ----------------------------------------------------------------------------------------------
 # packed sequences
 
-def _check_rows(name, t: torch.Tensor, device=None, heads=None, d=None, tokens=None):
-    """A bf16 GPU tensor [tokens, heads, d] with contiguous rows and strides that are multiples of 8."""
-    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+def _rows(name, t: torch.Tensor, dev=None, heads=None, d=None, tokens=None):
+    """(tokens, heads, d, token stride, head stride) of a bf16 GPU tensor [tokens, heads, d] with contiguous
+    rows and strides that are multiples of 8; raises for anything else, and for another device, number of
+    heads, head dimension or number of tokens than given.  The strides of an extent of one, which mean
+    nothing, are given as a packed tensor's."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a GPU tensor")
-    if t.dtype != torch.bfloat16 or t.dim() != 3:
+    if t.dtype is not torch.bfloat16 or t.dim() != 3:
         raise TypeError(f"{name} must be a bfloat16 [tokens, heads, d] tensor")
-    if device is not None and t.device != device:
-        raise ValueError(f"{name} is on {t.device}, not on {device}")
-    if (tokens is not None and t.shape[0] != tokens) or (heads is not None and t.shape[1] != heads) or \
-            (d is not None and t.shape[2] != d):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, inconsistent with the other operands")
-    if t.numel() and (t.stride(2) != 1 or (t.shape[0] > 1 and t.stride(0) % 8) or (t.shape[1] > 1 and t.stride(1) % 8)):
+    if dev is not None and t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, other operands are on device {dev}")
+    T, H, D = t.shape
+    if (tokens is not None and T != tokens) or (heads is not None and H != heads) or (d is not None and D != d):
+        raise ValueError(f"{name} has shape {(T, H, D)}, inconsistent with the other operands")
+    st, sh, sd = t.stride()
+    if H <= 1:
+        sh = D
+    if T <= 1:
+        st = max(H, 1) * D
+    if (sd != 1 or (st | sh) % 8) and T * H * D:
         raise ValueError(f"{name} must have contiguous rows, and strides that are multiples of 8")
+    return T, H, D, st, sh
 
 
-def _strides(t: torch.Tensor):
-    """(token, head) strides in elements; those of an extent of one, which mean nothing, as a packed tensor's."""
-    T, H, d = t.shape
-    head = t.stride(1) if H > 1 else d
-    return (t.stride(0) if T > 1 else H * d), head
-
-
-def _check_ints(name, t: torch.Tensor, device, shape):
-    if not isinstance(t, torch.Tensor) or t.device != device or t.dtype != torch.int32 or tuple(t.shape) != shape \
+def _check_ints(name, t: torch.Tensor, dev, shape):
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.int32 or t.shape != shape or t.get_device() != dev \
             or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous int32 {list(shape)} tensor on {device}")
+        raise ValueError(f"{name} must be a contiguous int32 {list(shape)} tensor on GPU {dev}")
 
 
-def _on_device_of(t: torch.Tensor, fn: str, *args):
-    """_call with t's device as the current one (the launches go there)."""
-    if torch.cuda.current_device() == t.get_device():
+# 0.1 us; torch.cuda.current_device() looks whether CUDA is initialised first and takes 0.5
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _on_device(dev: int, fn: str, *args):
+    """_call with device `dev` as the current one (the launches go there)."""
+    if _current_device() == dev:
         _call(fn, *args)
     else:
-        with torch.cuda.device(t.device):
+        with torch.cuda.device(dev):
             _call(fn, *args)
 
 
-def _outputs(q, want_lse, out, lse_out):
-    T, Hq, d = q.shape
+def _outputs(q, dev, T, Hq, d, want_lse, out, lse_out):
+    """(o, its token and head stride, lse or None)."""
     if out is None:
-        out = torch.empty((T, Hq, d), dtype=torch.bfloat16, device=q.device)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        st, sh = Hq * d, d
     else:
-        _check_rows("out", out, q.device, Hq, d, T)
+        _, _, _, st, sh = _rows("out", out, dev, Hq, d, T)
     if lse_out is None:
-        lse_out = torch.empty((T, Hq), dtype=torch.float32, device=q.device) if want_lse else None
-    elif lse_out.dtype != torch.float32 or tuple(lse_out.shape) != (T, Hq) or not lse_out.is_contiguous() \
-            or lse_out.device != q.device:
-        raise ValueError(f"lse_out must be a contiguous float32 {[T, Hq]} tensor on {q.device}")
-    return out, lse_out
+        if want_lse:
+            lse_out = torch.empty((T, Hq), dtype=torch.float32, device=q.device)
+    elif lse_out.dtype is not torch.float32 or lse_out.shape != (T, Hq) or not lse_out.is_contiguous() \
+            or lse_out.get_device() != dev:
+        raise ValueError(f"lse_out must be a contiguous float32 {[T, Hq]} tensor on GPU {dev}")
+    return out, st, sh, lse_out
 
 
-def _scratch(need, device, ws):
-    """(workspace, bytes) of a call that needs `need` bytes."""
+def _scratch(need, q, dev, ws):
+    """(pointer, bytes, tensor) of the workspace of a call that needs `need` bytes."""
     if ws is None:
         if need == 0:
-            return None, 0
-        ws = torch.empty(need, dtype=torch.uint8, device=device)
-    elif ws.device != device or not ws.is_contiguous():
-        raise ValueError(f"ws must be a contiguous tensor on {device}")
-    return ws, ws.numel() * ws.element_size()
+            return None, 0, None
+        ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+        return ws.data_ptr(), need, ws
+    if ws.get_device() != dev or not ws.is_contiguous():
+        raise ValueError(f"ws must be a contiguous tensor on GPU {dev}")
+    return ws.data_ptr(), ws.numel() * ws.element_size(), ws
 
 
 def prompt_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor,
@@ -755,21 +776,20 @@ def prompt_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.T
     (multiples of 8).  cu_q, cu_k int32 [S + 1] on the GPU: the first row of every sequence (cu_k None:
     cu_q).  Causal: the last query of a sequence sees its last key.  Rows behind the last sequence are
     not written (a new output holds anything there)."""
-    _check_rows("q", q)
-    Tq, Hq, d = q.shape
-    _check_rows("k", k, q.device, d=d)
-    Tk, Hkv, _ = k.shape
-    _check_rows("v", v, q.device, Hkv, d, Tk)
+    Tq, Hq, d, qt, qh = _rows("q", q)
+    dev = q.get_device()
+    Tk, Hkv, _, kt, kh = _rows("k", k, dev, d=d)
+    _, _, _, vt, vh = _rows("v", v, dev, Hkv, d, Tk)
     if cu_k is None:
         cu_k = cu_q
     S = cu_q.numel() - 1
-    _check_ints("cu_q", cu_q, q.device, (S + 1,))
-    _check_ints("cu_k", cu_k, q.device, (S + 1,))
-    o, lse = _outputs(q, want_lse, out, lse_out)
-    seqs = Seqs(S, Tq, Tk, Hq, Hkv, d, 1 if causal else 0, *_strides(q), *_strides(o), *_strides(k), *_strides(v))
-    ws, nbytes = _scratch(int(lib().la_prompt_ws_bytes(ctypes.byref(seqs))), q.device, ws)
-    _on_device_of(q, "la_prompt_attn", ctypes.byref(seqs), _ptr(q), _ptr(k), _ptr(v), _ptr(cu_q), _ptr(cu_k),
-                  scale if scale is not None else 0.0, _ptr(o), _ptr(lse), _ptr(ws), nbytes, _stream(q))
+    _check_ints("cu_q", cu_q, dev, (S + 1,))
+    _check_ints("cu_k", cu_k, dev, (S + 1,))
+    o, ot, oh, lse = _outputs(q, dev, Tq, Hq, d, want_lse, out, lse_out)
+    seqs = ctypes.byref(Seqs(S, Tq, Tk, Hq, Hkv, d, 1 if causal else 0, qt, qh, ot, oh, kt, kh, vt, vh))
+    wp, nbytes, ws = _scratch(lib().la_prompt_ws_bytes(seqs), q, dev, ws)
+    _on_device(dev, "la_prompt_attn", seqs, q.data_ptr(), k.data_ptr(), v.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(),
+               scale if scale is not None else 0.0, o.data_ptr(), _ptr(lse), wp, nbytes, _stream(q))
     return o if lse is None else (o, lse)
 
 
@@ -783,21 +803,23 @@ def kv4_cache(n_pages: int, Hkv: int, d: int, page: int = 64, device="cuda") -> 
 
 
 def _check_cache(cache, lens, table, cu, d):
-    """The la_kv4 of a cache, its page lengths and its table; raises for what does not fit."""
-    if not isinstance(cache, torch.Tensor) or cache.device.type != "cuda":
+    """(key heads, the la_kv4 of a cache and its table, sequences); raises for what does not fit."""
+    if not isinstance(cache, torch.Tensor) or not cache.is_cuda:
         raise TypeError("cache must be a GPU tensor")
-    if cache.dtype != torch.uint8 or cache.dim() != 3 or not cache.is_contiguous():
+    if cache.dtype is not torch.uint8 or cache.dim() != 3 or not cache.is_contiguous():
         raise TypeError("cache must be a contiguous uint8 [n_pages, Hkv, page bytes] tensor")
-    page, rest = divmod(cache.shape[2], d + d // 16)
-    if rest or lib().la_kv4_page_bytes(d, page) != cache.shape[2]:
-        raise ValueError(f"a cache of {cache.shape[2]} bytes a page is none for heads of {d}")
+    n, Hkv, nbytes = cache.shape
+    page, rest = divmod(nbytes, d + d // 16)
+    if rest or page < 16 or page & (page - 1):
+        raise ValueError(f"a cache of {nbytes} bytes a page is none for heads of {d}")
     if not isinstance(table, torch.Tensor) or table.dim() != 2:
         raise ValueError("table must be an int32 [S, max_pages] tensor")
-    S = table.shape[0]
-    _check_ints("table", table, cache.device, (S, table.shape[1]))
-    _check_ints("lens", lens, cache.device, (S,))
-    _check_ints("cu", cu, cache.device, (S + 1,))
-    return Kv4(cache.shape[0], page, table.shape[1])
+    dev = cache.get_device()
+    S, most = table.shape
+    _check_ints("table", table, dev, (S, most))
+    _check_ints("lens", lens, dev, (S,))
+    _check_ints("cu", cu, dev, (S + 1,))
+    return Hkv, ctypes.byref(Kv4(n, page, most)), S
 
 
 def kv4_append(cache: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: torch.Tensor, lens: torch.Tensor,
@@ -805,32 +827,31 @@ def kv4_append(cache: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: torch.
     """Enters k, v (bf16 [T, Hkv, d], free strides) into a 4-bit cache: rows [cu[s], cu[s + 1]) are the
     last tokens of sequence s, which has lens[s] with them, on the pages table[s].  cu int32 [S + 1],
     lens int32 [S], table int32 [S, max_pages], all on the GPU."""
-    _check_rows("k", k)
-    T, Hkv, d = k.shape
-    _check_rows("v", v, k.device, Hkv, d, T)
-    kv = _check_cache(cache, lens, table, cu, d)
-    if cache.device != k.device or cache.shape[1] != Hkv:
-        raise ValueError(f"cache of {cache.shape[1]} heads on {cache.device}, k of {Hkv} on {k.device}")
-    seqs = Seqs(table.shape[0], 0, T, Hkv, Hkv, d, 0, 0, 0, 0, 0, *_strides(k), *_strides(v))
-    _on_device_of(k, "la_kv4_append", ctypes.byref(seqs), ctypes.byref(kv), _ptr(k), _ptr(v), _ptr(cu), _ptr(lens),
-                  _ptr(table), _ptr(cache), _stream(k))
+    T, H, d, kt, kh = _rows("k", k)
+    dev = k.get_device()
+    _, _, _, vt, vh = _rows("v", v, dev, H, d, T)
+    Hkv, kv, S = _check_cache(cache, lens, table, cu, d)
+    if cache.get_device() != dev or Hkv != H:
+        raise ValueError(f"cache of {Hkv} heads on {cache.device}, k of {H} on {k.device}")
+    _on_device(dev, "la_kv4_append", ctypes.byref(Seqs(S, 0, T, H, H, d, 0, 0, 0, 0, 0, kt, kh, vt, vh)), kv, k.data_ptr(),
+               v.data_ptr(), cu.data_ptr(), lens.data_ptr(), table.data_ptr(), cache.data_ptr(), _stream(k))
 
 
 def kv4_read(cache: torch.Tensor, cu: torch.Tensor, lens: torch.Tensor, table: torch.Tensor, tokens: int, d: int,
              out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None):
     """The values that the last cu[s + 1] - cu[s] tokens of every sequence stand for -> (k, v) bf16
     [tokens, Hkv, d] (or the given pair, of any strides): what kv4_append entered there, rounded."""
-    kv = _check_cache(cache, lens, table, cu, d)
-    Hkv = cache.shape[1]
+    H, kv, S = _check_cache(cache, lens, table, cu, d)
+    dev = cache.get_device()
     if out is None:
-        k, v = (torch.empty((tokens, Hkv, d), dtype=torch.bfloat16, device=cache.device) for _ in range(2))
+        k, v = torch.empty((2, tokens, H, d), dtype=torch.bfloat16, device=cache.device).unbind(0)
     else:
         k, v = out
-    for name, t in (("k", k), ("v", v)):
-        _check_rows(name, t, cache.device, Hkv, d, tokens)
-    seqs = Seqs(table.shape[0], 0, tokens, Hkv, Hkv, d, 0, 0, 0, 0, 0, *_strides(k), *_strides(v))
-    _on_device_of(cache, "la_kv4_read", ctypes.byref(seqs), ctypes.byref(kv), _ptr(cache), _ptr(cu), _ptr(lens),
-                  _ptr(table), _ptr(k), _ptr(v), _stream(cache))
+    _, _, _, kt, kh = _rows("k", k, dev, H, d, tokens)
+    _, _, _, vt, vh = _rows("v", v, dev, H, d, tokens)
+    _on_device(dev, "la_kv4_read", ctypes.byref(Seqs(S, 0, tokens, H, H, d, 0, 0, 0, 0, 0, kt, kh, vt, vh)), kv,
+               cache.data_ptr(), cu.data_ptr(), lens.data_ptr(), table.data_ptr(), k.data_ptr(), v.data_ptr(),
+               _stream(cache))
     return k, v
 
 
@@ -843,17 +864,16 @@ def kv4_attn(q: torch.Tensor, cache: torch.Tensor, cu_q: torch.Tensor, lens: tor
     q [Tq, Hq, d] in bf16 with free strides; sequence s has the rows [cu_q[s], cu_q[s + 1]), at most max_q
     of them (1: the next token of every sequence), and lens[s] tokens in the cache (see kv4_append).
     Causal: the last query of a sequence sees the last token, its queries being the last tokens."""
-    _check_rows("q", q)
-    Tq, Hq, d = q.shape
-    kv = _check_cache(cache, lens, table, cu_q, d)
-    if cache.device != q.device:
+    Tq, Hq, d, qt, qh = _rows("q", q)
+    dev = q.get_device()
+    Hkv, kv, S = _check_cache(cache, lens, table, cu_q, d)
+    if cache.get_device() != dev:
         raise ValueError(f"cache is on {cache.device}, q on {q.device}")
-    o, lse = _outputs(q, want_lse, out, lse_out)
-    seqs = Seqs(table.shape[0], Tq, 0, Hq, cache.shape[1], d, 1 if causal else 0, *_strides(q), *_strides(o), 0, 0, 0, 0)
-    ws, nbytes = _scratch(int(lib().la_kv4_ws_bytes(ctypes.byref(seqs), ctypes.byref(kv), max_q)), q.device, ws)
-    _on_device_of(q, "la_kv4_attn", ctypes.byref(seqs), ctypes.byref(kv), max_q, _ptr(q), _ptr(cache), _ptr(cu_q),
-                  _ptr(lens), _ptr(table), scale if scale is not None else 0.0, _ptr(o), _ptr(lse), _ptr(ws), nbytes,
-                  _stream(q))
+    o, ot, oh, lse = _outputs(q, dev, Tq, Hq, d, want_lse, out, lse_out)
+    seqs = ctypes.byref(Seqs(S, Tq, 0, Hq, Hkv, d, 1 if causal else 0, qt, qh, ot, oh, 0, 0, 0, 0))
+    wp, nbytes, ws = _scratch(lib().la_kv4_ws_bytes(seqs, kv, max_q), q, dev, ws)
+    _on_device(dev, "la_kv4_attn", seqs, kv, max_q, q.data_ptr(), cache.data_ptr(), cu_q.data_ptr(), lens.data_ptr(),
+               table.data_ptr(), scale if scale is not None else 0.0, o.data_ptr(), _ptr(lse), wp, nbytes, _stream(q))
     return o if lse is None else (o, lse)
 
 
