@@ -34,13 +34,13 @@ struct RopeArgs {
 template <bool BF16>
 struct Chunk {
   u32x4 w[BF16 ? 1 : 2];
-  __device__ __forceinline__ void load(const void* p, int64_t at) {
-    const u32x4* s = (const u32x4*)((const char*)p + at * (BF16 ? 2 : 4));
+  __device__ __forceinline__ void load(const char* p) {
+    const u32x4* s = (const u32x4*)p;
 #pragma unroll
     for (int i = 0; i < (BF16 ? 1 : 2); ++i) w[i] = __builtin_nontemporal_load(s + i);
   }
-  __device__ __forceinline__ void store(void* p, int64_t at) const {
-    u32x4* d = (u32x4*)((char*)p + at * (BF16 ? 2 : 4));
+  __device__ __forceinline__ void store(char* p) const {
+    u32x4* d = (u32x4*)p;
 #pragma unroll
     for (int i = 0; i < (BF16 ? 1 : 2); ++i) d[i] = w[i];
   }
@@ -72,79 +72,84 @@ template <int D, bool BF16, bool NEIGHBOURS>
 __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
   constexpr int LANES = D / 16;                              // of a row
   constexpr int HEADS = kRopeThreads / (LANES * kRopeTokens);  // rows of a token at a time
-  constexpr int UNROLL = 4;
+  constexpr int UNROLL = 4, SIZE = BF16 ? 2 : 4;
   __shared__ float cs[kRopeTokens][D / 2], sn[kRopeTokens][D / 2];
-  const int pairs = a.rot / 2, t0 = blockIdx.x * kRopeTokens, b = blockIdx.y;
-  for (int i = threadIdx.x; i < kRopeTokens * pairs; i += kRopeThreads) {
-    const int j = i % pairs, tt = i / pairs;
-    const int axis = j < a.s0 ? 0 : (j < a.s1 ? 1 : 2);
-    const int p = a.pos[(int64_t)axis * a.L + min(t0 + tt, a.L - 1)];
-    const double turns = (double)p * a.freqs[j] * 0.15915494309189533577;
-    float s, c;
-    sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
-    cs[tt][j] = c * a.amplitude;
-    sn[tt][j] = s * a.amplitude;
-  }
-  __syncthreads();
+  const int pairs = a.rot / 2, t0 = blockIdx.x * kRopeTokens, b = blockIdx.y, H = a.Hq + a.Hk;
   const int lane = threadIdx.x % LANES, hl = threadIdx.x / LANES % HEADS, tt = threadIdx.x / (LANES * HEADS);
   const int t = t0 + tt;
-  if (t >= a.L) return;
-  // this lane's two chunks of 8 values, and the pairs of them
+  // this lane's two chunks of 8 values, and whether they turn
   const bool turn = NEIGHBOURS ? 16 * lane < a.rot : lane < a.rot / 16;
   const int o1 = NEIGHBOURS ? 16 * lane : (turn ? 8 * lane : 16 * lane);
   const int o2 = !NEIGHBOURS && turn ? pairs + 8 * lane : o1 + 8;
+  const char* const qs = (const char*)a.q + (b * a.q_b + t * a.q_t) * SIZE;
+  const char* const ks = (const char*)a.k + (b * a.k_b + t * a.k_t) * SIZE;
+  char* const qd = (char*)a.qo + (b * a.qo_b + t * a.qo_t) * SIZE;
+  char* const kd = (char*)a.ko + (b * a.ko_b + t * a.ko_t) * SIZE;
+  Chunk<BF16> x[UNROLL], y[UNROLL];
+  // rows h0, h0 + HEADS, ..: the queries' heads, then the keys'
+  auto load = [&](int h0) {
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+      const int h = h0 + u * HEADS;
+      if (h < H && t < a.L) {
+        const char* p = h < a.Hq ? qs + h * a.q_h * SIZE : ks + (h - a.Hq) * a.k_h * SIZE;
+        x[u].load(p + o1 * SIZE);
+        y[u].load(p + o2 * SIZE);
+      }
+    }
+  };
+  load(hl);
+  for (int i = threadIdx.x; i < kRopeTokens * pairs; i += kRopeThreads) {
+    const int j = i % pairs, ti = i / pairs;
+    const int axis = j < a.s0 ? 0 : (j < a.s1 ? 1 : 2);
+    const int p = a.pos[(int64_t)axis * a.L + min(t0 + ti, a.L - 1)];
+    const double turns = (double)p * a.freqs[j] * 0.15915494309189533577;
+    float s, c;
+    sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
+    cs[ti][j] = c * a.amplitude;
+    sn[ti][j] = s * a.amplitude;
+  }
+  __syncthreads();
+  if (t >= a.L) return;
   float c[8], s[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     c[e] = turn ? cs[tt][8 * lane + e] : 1.f;
     s[e] = turn ? sn[tt][8 * lane + e] : 0.f;
   }
-  auto rows = [&](const void* src, void* dst, int H, int64_t sb, int64_t st, int64_t sh, int64_t db, int64_t dt,
-                  int64_t dh) {
-    const int64_t from = b * sb + (int64_t)t * st, to = b * db + (int64_t)t * dt;
-    for (int h0 = hl; h0 < H; h0 += UNROLL * HEADS) {
-      Chunk<BF16> x[UNROLL], y[UNROLL];
+  for (int h0 = hl; h0 < H; h0 += UNROLL * HEADS) {
+    if (h0 != hl) load(h0);
 #pragma unroll
-      for (int u = 0; u < UNROLL; ++u) {
-        const int h = h0 + u * HEADS;
-        if (h < H) {
-          x[u].load(src, from + h * sh + o1);
-          y[u].load(src, from + h * sh + o2);
-        }
-      }
+    for (int u = 0; u < UNROLL; ++u) {
+      const int h = h0 + u * HEADS;
+      if (h >= H) break;
+      if (turn) {
+        float p[8], r[8], pn[8], rn[8];
+        x[u].get(p);
+        y[u].get(r);
+        if (NEIGHBOURS) {
 #pragma unroll
-      for (int u = 0; u < UNROLL; ++u) {
-        const int h = h0 + u * HEADS;
-        if (h >= H) break;
-        if (turn) {
-          float p[8], r[8], pn[8], rn[8];
-          x[u].get(p);
-          y[u].get(r);
-          if (NEIGHBOURS) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              pn[2 * e] = p[2 * e] * c[e] - p[2 * e + 1] * s[e];
-              pn[2 * e + 1] = p[2 * e + 1] * c[e] + p[2 * e] * s[e];
-              rn[2 * e] = r[2 * e] * c[4 + e] - r[2 * e + 1] * s[4 + e];
-              rn[2 * e + 1] = r[2 * e + 1] * c[4 + e] + r[2 * e] * s[4 + e];
-            }
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              pn[e] = p[e] * c[e] - r[e] * s[e];
-              rn[e] = r[e] * c[e] + p[e] * s[e];
-            }
+          for (int e = 0; e < 4; ++e) {
+            pn[2 * e] = p[2 * e] * c[e] - p[2 * e + 1] * s[e];
+            pn[2 * e + 1] = p[2 * e + 1] * c[e] + p[2 * e] * s[e];
+            rn[2 * e] = r[2 * e] * c[4 + e] - r[2 * e + 1] * s[4 + e];
+            rn[2 * e + 1] = r[2 * e + 1] * c[4 + e] + r[2 * e] * s[4 + e];
           }
-          x[u].set(pn);
-          y[u].set(rn);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            pn[e] = p[e] * c[e] - r[e] * s[e];
+            rn[e] = r[e] * c[e] + p[e] * s[e];
+          }
         }
-        x[u].store(dst, to + h * dh + o1);
-        y[u].store(dst, to + h * dh + o2);
+        x[u].set(pn);
+        y[u].set(rn);
       }
+      char* d = h < a.Hq ? qd + h * a.qo_h * SIZE : kd + (h - a.Hq) * a.ko_h * SIZE;
+      x[u].store(d + o1 * SIZE);
+      y[u].store(d + o2 * SIZE);
     }
-  };
-  rows(a.q, a.qo, a.Hq, a.q_b, a.q_t, a.q_h, a.qo_b, a.qo_t, a.qo_h);
-  rows(a.k, a.ko, a.Hk, a.k_b, a.k_t, a.k_h, a.ko_b, a.ko_t, a.ko_h);
+  }
 }
 
 template <int D, bool BF16>

@@ -123,7 +123,7 @@ constexpr int kTokenRows = 64;
 constexpr int kTokenPerCu = 2;
 struct CachePlan {
   int lq_token, rows;
-  bool many;               // there may be sequences of more tokens
+  bool few, many;          // there may be sequences of at most, and of more than, lq_token tokens
   SeqGeom token, many_rows;
   int p_token, p_many;     // workgroups (before the device's limit)
   size_t bytes;
@@ -135,7 +135,11 @@ CachePlan cache_plan(const la_seqs& s, const la_kv4& kv, int max_q) {
   const int64_t cap64 = (int64_t)kv.max_pages * kv.page;
   const int cap = cap64 < 0x7fffff00 ? (int)cap64 : 0x7fffff00;
   c.lq_token = G >= kTokenRows ? 1 : kTokenRows / G;
+  if (max_q > s.Tq) max_q = s.Tq;
   c.many = max_q > c.lq_token;
+  // a single sequence has all rows, so that it is one of many (or, where rows behind it are spare, may be
+  // made like one); saves two launches, 9 us
+  c.few = !(c.many && s.S == 1);
   c.rows = (int64_t)(c.many ? c.lq_token : max_q) * G <= 16 ? 16 : 32;
   c.token = seq_geom(s, c.rows, cap, kTokenExtra);
   c.token.lq_max = c.many ? c.lq_token : max_q;
@@ -143,7 +147,7 @@ CachePlan cache_plan(const la_seqs& s, const la_kv4& kv, int max_q) {
   c.bytes = part_layout(c.p_token, c.rows, s.d, nullptr).bytes;
   if (c.many) {
     c.many_rows = seq_geom(s, kRows, cap, kRowsExtra);
-    c.many_rows.lq_min = c.lq_token + 1;
+    c.many_rows.lq_min = c.few ? c.lq_token + 1 : 1;
     c.many_rows.lq_max = max_q;
     c.p_many = workgroups(c.many_rows, cap, kMaxWorkgroups);
     const size_t b = part_layout(c.p_many, kRows, s.d, nullptr).bytes;
@@ -257,12 +261,14 @@ la_status la_kv4_attn(const la_seqs* seqs, const la_kv4* kv, int32_t max_q, cons
   c.token.ks = c.many_rows.ks = lens;
   // one after the other on the stream, so they may use the same scratch
   set_parts(&io, part_layout(c.p_token, c.rows, seqs->d, ws));
-  int have = device_workgroups(kTokenPerCu);
-  hipError_t e = launch_cache_tokens(c.token, io, cg, seqs->d, c.rows, c.p_token < have ? c.p_token : have,
-                                     (hipStream_t)stream);
+  hipError_t e = hipSuccess;
+  if (c.few) {
+    const int have = device_workgroups(kTokenPerCu);
+    e = launch_cache_tokens(c.token, io, cg, seqs->d, c.rows, c.p_token < have ? c.p_token : have, (hipStream_t)stream);
+  }
   if (e == hipSuccess && c.many) {
     set_parts(&io, part_layout(c.p_many, kRows, seqs->d, ws));
-    have = device_workgroups(1);
+    const int have = device_workgroups(1);
     e = launch_cache_rows(c.many_rows, io, cg, seqs->d, c.p_many < have ? c.p_many : have, (hipStream_t)stream);
   }
   return e == hipSuccess ? LA_OK : LA_ERR_HIP;

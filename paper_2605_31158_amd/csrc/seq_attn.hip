@@ -212,6 +212,38 @@ __device__ __forceinline__ void start_rows(PieceState<D>& st, WaveCtx& w, const 
   st.seen = __builtin_amdgcn_readfirstlane(seen);
 }
 
+// The wave's row c of query column qt as bf16, 16 bytes (8 values) at a time: word i of lane group lg
+// belongs to column out_col(i, lg).  The accumulators give a lane 4 neighbouring values; it exchanges
+// every second quad with the next lane group's.  (Stored 8 bytes at a time, 16 rows of 32 bytes to an
+// instruction, a unit's 64 KB take 3 us more to issue, a third of what starting and ending it costs.)
+template <int D>
+__device__ __forceinline__ int out_col(int i, int lg) {
+  return Mma<D>::MR == 16 ? 32 * i + 16 * (lg & 1) + 8 * (lg >> 1) : 16 * i + 8 * lg;
+}
+template <int D>
+__device__ __forceinline__ void out_words(const typename Mma<D>::Acc (*oacc)[Mma<D>::QT], int qt, float inv, u32x4* y) {
+  using X = Mma<D>;
+  // quad n of the lane: values n MR .. (MR = 16), or 8 n .. (32), plus 4 lg
+  auto quad = [&](int n) {
+    const int e = 4 * n;
+    const typename X::Acc a = oacc[e / X::AR][qt] * inv;
+    return u32x2{pack_bf16x2(a[e % X::AR], a[e % X::AR + 1]), pack_bf16x2(a[e % X::AR + 2], a[e % X::AR + 3])};
+  };
+#pragma unroll
+  for (int i = 0; i < D / (8 * X::NG); ++i) {
+    const u32x2 a = quad(2 * i), b = quad(2 * i + 1);
+    u32x2 lo, hi;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const auto s = X::MR == 16 ? __builtin_amdgcn_permlane16_swap(a[w], b[w], false, false)
+                                 : __builtin_amdgcn_permlane32_swap(a[w], b[w], false, false);
+      lo[w] = (uint32_t)s[0];
+      hi[w] = (uint32_t)s[1];
+    }
+    y[i] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+  }
+}
+
 // Ends a piece: bf16 rows (and lse) where the piece is the whole unit, else the partial.
 template <int D>
 __device__ __forceinline__ void end_rows(const PieceState<D>& st, const SeqGeom& g, const SeqIo& io, const Walk& wk,
@@ -219,7 +251,7 @@ __device__ __forceinline__ void end_rows(const PieceState<D>& st, const SeqGeom&
   using X = Mma<D>;
   const bool whole = pc.ta == 0 && pc.tb == pc.n;
   const int slot = slot0 + (pc.ta == 0 ? 1 : 0);
-  if (!whole && threadIdx.x == 0) io.cut[slot] = int4{wk.s, wk.hg, wk.b, 1};
+  if (!whole && threadIdx.x == 0) io.cut[slot] = unit_record(g, wk);
 #pragma unroll
   for (int qt = 0; qt < X::QT; ++qt) {
     float l = st.l_run[qt];
@@ -227,17 +259,13 @@ __device__ __forceinline__ void end_rows(const PieceState<D>& st, const SeqGeom&
     l += __shfl_xor(l, 32);
     const int r = r_off + X::MR * qt + c;
     const Row row = unit_row(g, wk.q, wk.hg, wk.b, r);
+    u32x4 y[D / (8 * X::NG)];
+    if (whole) out_words<D>(st.oacc, qt, l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l), y);   // a NaN stays one
     if (!row.ok) {
     } else if (whole) {
-      const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l);   // a NaN stays one
-      uint16_t* dst = io.o + (int64_t)(wk.q.q0 + row.token) * io.o_tok + (int64_t)row.head * io.o_head + 4 * lg;
+      uint16_t* dst = io.o + (int64_t)(wk.q.q0 + row.token) * io.o_tok + (int64_t)row.head * io.o_head;
 #pragma unroll
-      for (int dt = 0; dt < D / X::MR; ++dt) {
-        const typename X::Acc x = st.oacc[dt][qt] * inv;
-#pragma unroll
-        for (int i = 0; i < X::AR; i += 4)
-          *(u32x2*)(dst + X::MR * dt + X::acc_row(i)) = u32x2{pack_bf16x2(x[i], x[i + 1]), pack_bf16x2(x[i + 2], x[i + 3])};
-      }
+      for (int i = 0; i < D / (8 * X::NG); ++i) *(u32x4*)(dst + out_col<D>(i, lg)) = y[i];
       if (io.lse && lg == 0)
         io.lse[(int64_t)(wk.q.q0 + row.token) * g.Hq + row.head] =
             l == 0.f ? -INFINITY : (st.m_run[qt] + log2f(l)) * 0.69314718055994531f;
@@ -363,34 +391,30 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 // over the pieces in the order of the stretches.  Workgroup (l, y) joins rows [16 y, 16 y + 16) of
 // the unit that stretch l starts and does not end, if there is one: its first piece lies in slot
 // 2 l + 1, the others in the slots 2 l' of the stretches that follow.
-template <int D, int R, bool CACHE>
-__global__ __launch_bounds__(256) void seq_merge_kernel(SeqGeom g, SeqIo io, int P) {
+template <int D, int R>
+__global__ __launch_bounds__(256) void seq_merge_kernel(SeqIo io, int GH, int Hq, int P) {
   constexpr int TPR = 16;                             // threads of a row
   constexpr int W = D / TPR;
   const int l0 = blockIdx.x;
+  const int lane = threadIdx.x & 63;
   const int4 u = io.cut[2 * l0 + 1];
+  const int4 x0 = io.cut[2 * min(l0 + 1 + lane, P - 1)];
   if (u.w == 0) return;
   // pieces that follow: as long as slot 2 l' names the same unit
-  const int lane = threadIdx.x & 63;
   int n = 0;
   for (;;) {
     const int l = l0 + 1 + n + lane;
-    bool same = false;
-    if (l < P) {
-      const int4 x = io.cut[2 * l];
-      same = x.w != 0 && x.x == u.x && x.y == u.y && x.z == u.z;
-    }
-    const uint64_t not_same = ~__ballot(same);
-    if (not_same) {
-      n += __builtin_ctzll(not_same);
+    const int4 x = n == 0 ? x0 : io.cut[2 * min(l, P - 1)];
+    const uint64_t other = ~__ballot(l < P && x.w != 0 && x.x == u.x && x.z == u.z);
+    if (other) {
+      n += __builtin_ctzll(other);
       break;
     }
     n += 64;
   }
   const int r = blockIdx.y * 16 + threadIdx.x / TPR, part = threadIdx.x % TPR;
-  const Seq q = load_seq<CACHE>(g, u.x);
-  const Row row = unit_row(g, q, u.y, u.z, r);
-  if (!row.ok) return;
+  const int token = r / GH, head = r - token * GH;    // as unit_row
+  if (token >= u.y || head >= u.w) return;
   float m = -INFINITY, l = 0.f, acc[W];
 #pragma unroll
   for (int e = 0; e < W; ++e) acc[e] = 0.f;
@@ -426,15 +450,19 @@ __global__ __launch_bounds__(256) void seq_merge_kernel(SeqGeom g, SeqIo io, int
     m = mx;
   }
   const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l);
-  uint16_t* dst = io.o + (int64_t)(q.q0 + row.token) * io.o_tok + (int64_t)row.head * io.o_head + part * W;
+  uint16_t* dst = io.o + (int64_t)(u.x + token) * io.o_tok + (int64_t)(u.z + head) * io.o_head + part * W;
   uint32_t y[W / 2];
 #pragma unroll
   for (int e = 0; e < W / 2; ++e) y[e] = pack_bf16x2(acc[2 * e] * inv, acc[2 * e + 1] * inv);
 #pragma unroll
   for (int e = 0; e < W / 4; ++e) *(u32x2*)(dst + 4 * e) = u32x2{y[2 * e], y[2 * e + 1]};
   if (io.lse && part == 0)
-    io.lse[(int64_t)(q.q0 + row.token) * g.Hq + row.head] =
-        l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+    io.lse[(int64_t)(u.x + token) * Hq + u.z + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+}
+
+template <int D, int R>
+void launch_merge(const SeqGeom& g, const SeqIo& io, int P, hipStream_t st) {
+  hipLaunchKernelGGL((seq_merge_kernel<D, R>), dim3(P, R / 16), dim3(256), 0, st, io, g.GH, g.Hq, P);
 }
 
 }  // namespace
@@ -442,7 +470,7 @@ __global__ __launch_bounds__(256) void seq_merge_kernel(SeqGeom g, SeqIo io, int
 template <int D, bool CACHE>
 static hipError_t launch_rows(const SeqGeom& g, const SeqIo& io, const CacheGeom& cg, int P, hipStream_t st) {
   hipLaunchKernelGGL((seq_attn_kernel<D, CACHE>), dim3(P), dim3(kThreads), 0, st, g, io, cg);
-  hipLaunchKernelGGL((seq_merge_kernel<D, QR, CACHE>), dim3(P, QR / 16), dim3(256), 0, st, g, io, P);
+  launch_merge<D, QR>(g, io, P, st);
   return hipGetLastError();
 }
 
@@ -452,14 +480,8 @@ hipError_t launch_prompt_attn(const SeqGeom& g, const SeqIo& io, int d, int P, h
 }
 
 hipError_t launch_cache_merge(const SeqGeom& g, const SeqIo& io, int d, int rows, int P, hipStream_t st) {
-  const dim3 grid(P, rows / 16);
-  if (d == 128) {
-    if (rows == 16) hipLaunchKernelGGL((seq_merge_kernel<128, 16, true>), grid, dim3(256), 0, st, g, io, P);
-    else hipLaunchKernelGGL((seq_merge_kernel<128, 32, true>), grid, dim3(256), 0, st, g, io, P);
-  } else {
-    if (rows == 16) hipLaunchKernelGGL((seq_merge_kernel<64, 16, true>), grid, dim3(256), 0, st, g, io, P);
-    else hipLaunchKernelGGL((seq_merge_kernel<64, 32, true>), grid, dim3(256), 0, st, g, io, P);
-  }
+  if (d == 128) rows == 16 ? launch_merge<128, 16>(g, io, P, st) : launch_merge<128, 32>(g, io, P, st);
+  else rows == 16 ? launch_merge<64, 16>(g, io, P, st) : launch_merge<64, 32>(g, io, P, st);
   return hipGetLastError();
 }
 

@@ -322,7 +322,7 @@ __global__ __launch_bounds__(kTokenThreads, 2) void token_attn_kernel(SeqGeom g,
       }
       const bool whole = pc.ta == 0 && pc.tb == pc.n;
       const int slot = 2 * lambda + (pc.ta == 0 ? 1 : 0);
-      if (!whole && tid == 0) io.cut[slot] = int4{wk.s, wk.hg, wk.b, 1};
+      if (!whole && tid == 0) io.cut[slot] = unit_record(g, wk);
       if (!row.ok) {
       } else if (whole) {
         const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l);   // a NaN stays one

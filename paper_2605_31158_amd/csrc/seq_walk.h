@@ -9,7 +9,12 @@
 // [l share, (l + 1) share): equal shares whatever the lengths are, with no plan in memory and no launch
 // for one.  A stretch covers the end of one unit, whole units and the start of another; a place inside
 // a unit, less the extra, is rounded up to tiles of 64 keys, on both sides of a cut alike, so every
-// tile belongs to exactly one piece.
+// tile belongs to exactly one piece.  A cut costs a piece more, so a border no further than `extra` (or
+// a 64th of a share) from a unit's start or end is moved there, again on both sides alike.  The runs of a
+// causal sequence come from both ends in turn, the longest, the shortest, the second longest, ..:
+// pairs weigh the same, and where they fill the shares evenly no unit is cut at all (8192 tokens, 4
+// key heads: 512 units for 256 workgroups; in ascending order nearly every workgroup cut two, 34 MB of
+// partials written and read).
 //
 // Where a unit starts on the line has a closed form (causal runs of a sequence weigh off + TB,
 // off + 2 TB, ..), so a wave finds its first unit with one scan over the sequences and a 64-way
@@ -44,7 +49,7 @@ struct SeqIo {
   float* part_o;           // [2 P][R][d]: O of the piece that a stretch starts in (0) or ends in (1)
   float* part_m;           // [2 P][R]
   float* part_l;
-  int4* cut;               // [2 P]: (sequence, head group, run, 1) of the piece in a slot, or w = 0
+  int4* cut;               // [2 P]: the unit whose piece a slot holds (unit_record), or w = 0
   float scale_log2;
 };
 
@@ -90,11 +95,25 @@ __device__ __forceinline__ uint64_t seq_weight(const SeqGeom& g, const Seq& q) {
   return nb == 0 ? 0 : weight_before(g, q, nb - 1) + (uint32_t)q.lk + g.extra;
 }
 
+// The j-th run of a sequence on the line, and the weight of those before it.
+__device__ __forceinline__ int run_at(const SeqGeom& g, int nb, int j) {
+  return g.causal ? ((j & 1) ? j >> 1 : nb - 1 - (j >> 1)) : j;
+}
+__device__ __forceinline__ uint64_t line_before(const SeqGeom& g, const Seq& q, int nb, uint64_t all, int j) {
+  if (!g.causal) return weight_before(g, q, j);
+  const int m = j >> 1;                                // m runs of either end
+  uint64_t w = weight_before(g, q, m);
+  if (m > 0) w += all - weight_before(g, q, nb - m);
+  if (j & 1) w += (uint32_t)run_keys(g, q, nb - 1 - m) + g.extra;
+  return w;
+}
+
 // A wave's place on the line; everything in it is uniform.
 struct Walk {
   uint64_t pos, end;       // the stretch still to do
   uint64_t unit0;          // where the present unit starts
-  int s, hg, b, nb;        // sequence, head group, run, runs of the sequence
+  uint32_t snap;           // borders this near a unit's start or end lie there
+  int s, hg, j, b, nb;     // sequence, head group, place of the run among the sequence's, run, runs
   Seq q;
   __device__ __forceinline__ bool more() const { return pos < end; }
 };
@@ -111,6 +130,52 @@ __device__ __forceinline__ Seq load_seq_uniform(const SeqGeom& g, int s) {
   return q;
 }
 
+// The part of the present unit that the stretch covers: tiles [ta, tb) of n, none if ta == tb.
+struct Piece {
+  int keys;                // keys that the unit's last token sees
+  int ta, tb, n;
+};
+
+__device__ __forceinline__ Piece walk_piece(const SeqGeom& g, const Walk& w, uint64_t* unit_end) {
+  Piece p;
+  p.keys = run_keys(g, w.q, w.b);
+  *unit_end = w.unit0 + (uint32_t)p.keys + g.extra;
+  p.n = p.keys == 0 ? 1 : (int)(((uint32_t)p.keys + 63u) >> 6);
+  const uint32_t xa = (uint32_t)(w.pos - w.unit0);
+  p.ta = xa <= g.extra ? 0 : (int)((xa - g.extra + 63u) >> 6);
+  p.tb = p.n;
+  if (w.end < *unit_end) {
+    const uint32_t xb = (uint32_t)(w.end - w.unit0);
+    if (xb <= w.snap) p.tb = 0;                         // the unit is the next workgroup's
+    else if (*unit_end - w.end > w.snap) p.tb = xb <= g.extra ? 0 : (int)((xb - g.extra + 63u) >> 6);
+  }
+  p.ta = __builtin_amdgcn_readfirstlane(p.ta);
+  p.tb = __builtin_amdgcn_readfirstlane(max(p.ta, p.tb));
+  return p;
+}
+
+// On to the next unit.
+template <bool CACHE>
+__device__ __forceinline__ void walk_on(const SeqGeom& g, Walk& w, uint64_t unit_end) {
+  w.pos = w.unit0 = unit_end;
+  if (w.pos >= w.end) return;
+  if (++w.j >= w.nb) {
+    w.j = 0;
+    if (++w.hg >= g.Hkv * g.GS) {
+      w.hg = 0;
+      do {
+        if (++w.s >= g.S) {                             // not reached while pos < end
+          w.pos = w.end;
+          return;
+        }
+        w.q = load_seq_uniform<CACHE>(g, w.s);
+      } while (w.q.lq == 0);
+      w.nb = runs_of(g, w.q);
+    }
+  }
+  w.b = run_at(g, w.nb, w.j);
+}
+
 // Start of the stretch of workgroup l of P.
 template <bool CACHE>
 __device__ __forceinline__ Walk start_walk(const SeqGeom& g, int l, int P) {
@@ -118,9 +183,13 @@ __device__ __forceinline__ Walk start_walk(const SeqGeom& g, int l, int P) {
   const int NH = g.Hkv * g.GS;
   const int C = (g.S + 63) / 64;
   uint64_t sum = 0;
+  Seq mine{0, 0, 0, 0};
   for (int i = 0; i < C; ++i) {
     const int s = lane * C + i;
-    if (s < g.S) sum += seq_weight(g, load_seq<CACHE>(g, s));
+    if (s < g.S) {
+      mine = load_seq<CACHE>(g, s);
+      sum += seq_weight(g, mine);
+    }
   }
   sum *= (uint32_t)NH;
   const uint64_t incl = wave_incl_scan(sum);
@@ -130,7 +199,8 @@ __device__ __forceinline__ Walk start_walk(const SeqGeom& g, int l, int P) {
   Walk w;
   w.pos = first_lane_u64((uint64_t)(uint32_t)l * share);
   w.end = w.pos + share < total ? w.pos + share : total;
-  w.s = w.hg = w.b = w.nb = 0;
+  w.snap = (uint32_t)(share / 64 < g.extra ? share / 64 : g.extra);
+  w.s = w.hg = w.j = w.b = w.nb = 0;
   w.unit0 = 0;
   w.q = Seq{0, 0, 0, 0};
   if (w.pos >= w.end) return w;
@@ -139,7 +209,15 @@ __device__ __forceinline__ Walk start_walk(const SeqGeom& g, int l, int P) {
   const int L = __builtin_ctzll(held);
   uint64_t at = read_lane_u64(incl - sum, L);
   int s = __builtin_amdgcn_readfirstlane(L * C);
-  Seq q = load_seq_uniform<CACHE>(g, s);
+  Seq q;
+  if (C == 1) {
+    q.q0 = __builtin_amdgcn_readlane(mine.q0, L);
+    q.lq = __builtin_amdgcn_readlane(mine.lq, L);
+    q.k0 = __builtin_amdgcn_readlane(mine.k0, L);
+    q.lk = __builtin_amdgcn_readlane(mine.lk, L);
+  } else {
+    q = load_seq_uniform<CACHE>(g, s);
+  }
   uint64_t ws = seq_weight(g, q);
   while (w.pos >= at + ws * (uint32_t)NH && s + 1 < g.S) {
     at += ws * (uint32_t)NH;
@@ -151,59 +229,25 @@ __device__ __forceinline__ Walk start_walk(const SeqGeom& g, int l, int P) {
   const uint64_t rem = w.pos - at;
   const int nb = runs_of(g, q);
   int lo = 0, n = nb;
-  while (n > 1) {                                       // the run is in [lo, lo + n)
+  while (n > 1) {                                       // the run's place is in [lo, lo + n)
     const int step = (n + 63) / 64;
-    const int64_t b = (int64_t)lo + (int64_t)lane * step;
-    const bool below = b < lo + n && weight_before(g, q, (int)b) <= rem;
+    const int64_t j = (int64_t)lo + (int64_t)lane * step;
+    const bool below = j < lo + n && line_before(g, q, nb, ws, (int)j) <= rem;
     const int i = __popcll(__ballot(below)) - 1;        // lane 0 is always below
     lo += i * step;
     n = min(step, n - i * step);
   }
   w.s = __builtin_amdgcn_readfirstlane(s);
   w.hg = __builtin_amdgcn_readfirstlane(hg);
-  w.b = __builtin_amdgcn_readfirstlane(lo);
+  w.j = __builtin_amdgcn_readfirstlane(lo);
+  w.b = run_at(g, nb, w.j);
   w.nb = nb;
   w.q = q;
-  w.unit0 = first_lane_u64(at + weight_before(g, q, w.b));
+  w.unit0 = first_lane_u64(at + line_before(g, q, nb, ws, w.j));
+  const uint64_t unit_end = w.unit0 + (uint32_t)run_keys(g, q, w.b) + g.extra;
+  if (w.pos - w.unit0 <= w.snap) w.pos = w.unit0;
+  else if (unit_end - w.pos <= w.snap) walk_on<CACHE>(g, w, unit_end);
   return w;
-}
-
-// The part of the present unit that the stretch covers: tiles [ta, tb) of n, none if ta == tb.
-struct Piece {
-  int keys;                // keys that the unit's last token sees
-  int ta, tb, n;
-};
-
-__device__ __forceinline__ Piece walk_piece(const SeqGeom& g, const Walk& w, uint64_t* unit_end) {
-  Piece p;
-  p.keys = run_keys(g, w.q, w.b);
-  *unit_end = w.unit0 + (uint32_t)p.keys + g.extra;
-  const uint32_t xa = (uint32_t)(w.pos - w.unit0);
-  const uint32_t xb = (uint32_t)((w.end < *unit_end ? w.end : *unit_end) - w.unit0);
-  p.n = p.keys == 0 ? 1 : (int)(((uint32_t)p.keys + 63u) >> 6);
-  p.ta = __builtin_amdgcn_readfirstlane(xa <= g.extra ? 0 : (int)((xa - g.extra + 63u) >> 6));
-  p.tb = w.end >= *unit_end ? p.n : (xb <= g.extra ? 0 : (int)((xb - g.extra + 63u) >> 6));
-  p.tb = __builtin_amdgcn_readfirstlane(p.tb);
-  return p;
-}
-
-// On to the next unit.
-template <bool CACHE>
-__device__ __forceinline__ void walk_on(const SeqGeom& g, Walk& w, uint64_t unit_end) {
-  w.pos = w.unit0 = unit_end;
-  if (w.pos >= w.end) return;
-  if (++w.b < w.nb) return;
-  w.b = 0;
-  if (++w.hg < g.Hkv * g.GS) return;
-  w.hg = 0;
-  do {
-    if (++w.s >= g.S) {                                 // not reached while pos < end
-      w.pos = w.end;
-      return;
-    }
-    w.q = load_seq_uniform<CACHE>(g, w.s);
-  } while (w.q.lq == 0);
-  w.nb = runs_of(g, w.q);
 }
 
 // Packed row r of a unit: its token (of the sequence) and query head, or ok == false.
@@ -219,6 +263,14 @@ __device__ __forceinline__ Row unit_row(const SeqGeom& g, const Seq& q, int hg, 
   x.head = kvh * g.G + part * g.GH + j;
   x.ok = t < g.TB && x.token < q.lq && part * g.GH + j < g.G;
   return x;
+}
+
+// What a merge has to know of a unit: its first row of q and o, tokens, first head, heads.  The first and
+// the third name the unit.
+__device__ __forceinline__ int4 unit_record(const SeqGeom& g, const Walk& w) {
+  const int kvh = w.hg / g.GS, part = w.hg - kvh * g.GS;
+  return int4{w.q.q0 + w.b * g.TB, min(g.TB, w.q.lq - w.b * g.TB), kvh * g.G + part * g.GH,
+              min(g.GH, g.G - part * g.GH)};
 }
 
 // Keys that token t of the sequence sees.
