@@ -26,11 +26,11 @@ la_status check_seqs(const la_seqs* s) {
 }
 
 constexpr int kRows = 256;              // packed rows of a workgroup (seq_attn.hip)
-constexpr uint32_t kMinShare = 256;     // keys
-constexpr uint32_t kRowsExtra = 512, kTokenExtra = 384;    // what starting and ending a unit costs, in keys
+// What starting and ending a unit costs, and the smallest share of a workgroup, in keys.
+constexpr uint32_t kRowsExtra = 512, kTokenExtra = 384, kRowsShare = 512, kTokenShare = 256;
 constexpr int kMaxWorkgroups = 256;
 
-SeqGeom seq_geom(const la_seqs& s, int rows, int kcap, uint32_t extra) {
+SeqGeom seq_geom(const la_seqs& s, int rows, int kcap, uint32_t extra, uint32_t whole, uint32_t share) {
   SeqGeom g{};
   g.S = s.S;
   g.Tq = s.Tq;
@@ -45,7 +45,8 @@ SeqGeom seq_geom(const la_seqs& s, int rows, int kcap, uint32_t extra) {
   g.TB = rows / g.GH;
   g.causal = s.causal;
   g.extra = extra;
-  g.min_share = kMinShare;
+  g.whole = whole;
+  g.min_share = share;
   return g;
 }
 
@@ -141,12 +142,12 @@ CachePlan cache_plan(const la_seqs& s, const la_kv4& kv, int max_q) {
   // made like one); saves two launches, 9 us
   c.few = !(c.many && s.S == 1);
   c.rows = (int64_t)(c.many ? c.lq_token : max_q) * G <= 16 ? 16 : 32;
-  c.token = seq_geom(s, c.rows, cap, kTokenExtra);
+  c.token = seq_geom(s, c.rows, cap, kTokenExtra, 0, kTokenShare);
   c.token.lq_max = c.many ? c.lq_token : max_q;
   c.p_token = workgroups(c.token, cap, kMaxWorkgroups * kTokenPerCu);
   c.bytes = part_layout(c.p_token, c.rows, s.d, nullptr).bytes;
   if (c.many) {
-    c.many_rows = seq_geom(s, kRows, cap, kRowsExtra);
+    c.many_rows = seq_geom(s, kRows, cap, kRowsExtra, 2 * kRowsExtra, kRowsShare);
     c.many_rows.lq_min = c.few ? c.lq_token + 1 : 1;
     c.many_rows.lq_max = max_q;
     c.p_many = workgroups(c.many_rows, cap, kMaxWorkgroups);
@@ -177,7 +178,7 @@ extern "C" {
 
 size_t la_prompt_ws_bytes(const la_seqs* seqs) {
   if (check_seqs(seqs) != LA_OK || seqs->S == 0 || seqs->Tq == 0) return 0;
-  const SeqGeom g = seq_geom(*seqs, kRows, seqs->Tk, kRowsExtra);
+  const SeqGeom g = seq_geom(*seqs, kRows, seqs->Tk, kRowsExtra, 2 * kRowsExtra, kRowsShare);
   return part_layout(workgroups(g, seqs->Tk, kMaxWorkgroups), kRows, seqs->d, nullptr).bytes;
 }
 
@@ -196,7 +197,7 @@ la_status la_prompt_attn(const la_seqs* seqs, const void* q, const void* k, cons
   if (!q || !o || !cu_q || !cu_k || (seqs->Tk > 0 && (!k || !v))) return LA_ERR_ARG;
   if (misaligned(q) || misaligned(o) || misaligned(k) || misaligned(v)) return LA_ERR_ARG;
   if (((uintptr_t)cu_q | (uintptr_t)cu_k | (uintptr_t)lse) & 3u) return LA_ERR_ARG;
-  SeqGeom g = seq_geom(*seqs, kRows, seqs->Tk, kRowsExtra);
+  SeqGeom g = seq_geom(*seqs, kRows, seqs->Tk, kRowsExtra, 2 * kRowsExtra, kRowsShare);
   g.cu_q = cu_q;
   g.ks = cu_k;
   const int most = workgroups(g, seqs->Tk, kMaxWorkgroups);

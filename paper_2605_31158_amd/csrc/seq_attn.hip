@@ -388,12 +388,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 }
 
 // Joins the pieces of a unit that several stretches share: o = sum 2^(m_s - m) O_s / sum 2^(m_s - m) l_s,
-// over the pieces in the order of the stretches.  Workgroup (l, y) joins rows [16 y, 16 y + 16) of
+// over the pieces in the order of the stretches.  Workgroup (l, y) joins rows [RW y, RW y + RW) of
 // the unit that stretch l starts and does not end, if there is one: its first piece lies in slot
 // 2 l + 1, the others in the slots 2 l' of the stretches that follow.
-template <int D, int R>
-__global__ __launch_bounds__(256) void seq_merge_kernel(SeqIo io, int GH, int Hq, int P) {
-  constexpr int TPR = 16;                             // threads of a row
+// A unit of few rows is often one of many pieces (a long cache): NG groups of 256 threads take every
+// NG-th batch of them and are joined in LDS.
+template <int D, int R, int RW, int NG>
+__global__ __launch_bounds__(256 * NG) void seq_merge_kernel(SeqIo io, int GH, int Hq, int P) {
+  constexpr int TPR = 256 / RW;                       // threads of a row
   constexpr int W = D / TPR;
   const int l0 = blockIdx.x;
   const int lane = threadIdx.x & 63;
@@ -412,19 +414,20 @@ __global__ __launch_bounds__(256) void seq_merge_kernel(SeqIo io, int GH, int Hq
     }
     n += 64;
   }
-  const int r = blockIdx.y * 16 + threadIdx.x / TPR, part = threadIdx.x % TPR;
+  const int th = threadIdx.x & 255, grp = threadIdx.x >> 8;
+  const int r = blockIdx.y * RW + th / TPR, part = th % TPR;
   const int token = r / GH, head = r - token * GH;    // as unit_row
-  if (token >= u.y || head >= u.w) return;
+  const bool ok = token < u.y && head < u.w;
   float m = -INFINITY, l = 0.f, acc[W];
 #pragma unroll
   for (int e = 0; e < W; ++e) acc[e] = 0.f;
   constexpr int BATCH = 4;
-  for (int i0 = 0; i0 <= n; i0 += BATCH) {
+  for (int i0 = grp * BATCH; i0 <= n && ok; i0 += NG * BATCH) {
     float pm[BATCH], pl[BATCH];
     f32x4 po[BATCH][W / 4];
 #pragma unroll
     for (int j = 0; j < BATCH; ++j) {
-      const int i = min(i0 + j, n);                   // a repeated piece is given the weight 0 below
+      const int i = min(i0 + j, n);                   // a repeated piece is left out below
       const size_t at = (size_t)(i == 0 ? 2 * l0 + 1 : 2 * (l0 + i)) * R + r;
       pm[j] = io.part_m[at];
       pl[j] = io.part_l[at];
@@ -449,6 +452,36 @@ __global__ __launch_bounds__(256) void seq_merge_kernel(SeqIo io, int GH, int Hq
     }
     m = mx;
   }
+  if constexpr (NG > 1) {
+    __shared__ float sm[NG - 1][256][W + 3];          // W + 2 values; the row stride is odd
+    if (grp > 0) {
+      float* p = sm[grp - 1][th];
+#pragma unroll
+      for (int e = 0; e < W; ++e) p[e] = acc[e];
+      p[W] = m;
+      p[W + 1] = l;
+    }
+    __syncthreads();
+    if (grp > 0) return;
+    float mx = m;
+#pragma unroll
+    for (int k = 0; k < NG - 1; ++k) mx = fmaxf(mx, sm[k][th][W]);
+    const float base = mx == -INFINITY ? 0.f : mx;
+    const float keep = exp2f(m - base);
+    l *= keep;
+#pragma unroll
+    for (int e = 0; e < W; ++e) acc[e] *= keep;
+#pragma unroll
+    for (int k = 0; k < NG - 1; ++k) {
+      const float* p = sm[k][th];
+      const float a = exp2f(p[W] - base);
+      l += a * p[W + 1];
+#pragma unroll
+      for (int e = 0; e < W; ++e) acc[e] += a * p[e];
+    }
+    m = mx;
+  }
+  if (!ok) return;
   const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l);
   uint16_t* dst = io.o + (int64_t)(u.x + token) * io.o_tok + (int64_t)(u.z + head) * io.o_head + part * W;
   uint32_t y[W / 2];
@@ -462,7 +495,8 @@ __global__ __launch_bounds__(256) void seq_merge_kernel(SeqIo io, int GH, int Hq
 
 template <int D, int R>
 void launch_merge(const SeqGeom& g, const SeqIo& io, int P, hipStream_t st) {
-  hipLaunchKernelGGL((seq_merge_kernel<D, R>), dim3(P, R / 16), dim3(256), 0, st, io, g.GH, g.Hq, P);
+  constexpr int RW = R == 32 ? 32 : 16, NG = R <= 32 ? 4 : 1;
+  hipLaunchKernelGGL((seq_merge_kernel<D, R, RW, NG>), dim3(P, R / RW), dim3(256 * NG), 0, st, io, g.GH, g.Hq, P);
 }
 
 }  // namespace
