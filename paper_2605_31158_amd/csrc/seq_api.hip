@@ -42,6 +42,7 @@ SeqGeom seq_geom(const la_seqs& s, int rows, int kcap, uint32_t extra, uint32_t 
   g.G = s.Hq / s.Hkv;
   g.GH = g.G < rows ? g.G : rows;
   g.GS = ceil_div(g.G, g.GH);
+  g.gh_magic = (65536 + g.GH - 1) / g.GH;
   g.TB = rows / g.GH;
   g.causal = s.causal;
   g.extra = extra;

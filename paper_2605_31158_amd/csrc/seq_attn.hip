@@ -195,7 +195,7 @@ __device__ __forceinline__ void start_rows(PieceState<D>& st, WaveCtx& w, const 
     for (int dt = 0; dt < D / X::MR; ++dt)
 #pragma unroll
       for (int i = 0; i < X::AR; ++i) st.oacc[dt][qt][i] = 0.f;
-    const Row row = unit_row(g, wk.q, wk.hg, wk.b, r_off + X::MR * qt + c);
+    const Row row = unit_row(g, wk, r_off + X::MR * qt + c);
     const uint16_t* src = io.q + (int64_t)(wk.q.q0 + row.token) * io.q_tok + (int64_t)row.head * io.q_head + 8 * lg;
 #pragma unroll
     for (int ks = 0; ks < D / X::KC; ++ks) {
@@ -258,7 +258,7 @@ __device__ __forceinline__ void end_rows(const PieceState<D>& st, const SeqGeom&
     if constexpr (X::NG == 4) l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
     const int r = r_off + X::MR * qt + c;
-    const Row row = unit_row(g, wk.q, wk.hg, wk.b, r);
+    const Row row = unit_row(g, wk, r);
     u32x4 y[D / (8 * X::NG)];
     if (whole) out_words<D>(st.oacc, qt, l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l), y);   // a NaN stays one
     if (!row.ok) {
@@ -334,7 +334,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       const Piece pc = walk_piece(g, wk, &unit_end);
       const int N = pc.tb - pc.ta;
       if (N > 0) {
-        src.prime(io, wk, wk.hg / g.GS, pc.ta, pc.tb, IS_G1 ? s0 + VOFF : s0, IS_G1 ? nullptr : s1);
+        src.prime(io, wk, wk.kvh, pc.ta, pc.tb, IS_G1 ? s0 + VOFF : s0, IS_G1 ? nullptr : s1);
         start_rows<D>(st, w, g, io, wk, r_off, c, lg);
         // first tile that some row of the unit does not see whole
         const int open = g.causal ? max(0, wk.q.lk - wk.q.lq + wk.b * g.TB + 1) : wk.q.lk;

@@ -84,7 +84,7 @@ __global__ __launch_bounds__(kTokenThreads, 2) void token_attn_kernel(SeqGeom g,
     uint64_t unit_end;
     const Piece pc = walk_piece(g, wk, &unit_end);
     if (pc.tb > pc.ta) {
-      const int kvh = wk.hg / g.GS, lk = wk.q.lk;
+      const int kvh = wk.kvh, lk = wk.q.lk;
       const int32_t* row_pages = cg.table + (int64_t)wk.s * cg.max_pages;
       // Q: lane (c, g) has values (d / 4) g + 8 ks .. of row c, as its K words have
       bf16x8 qreg[KS][QT];
@@ -93,7 +93,7 @@ __global__ __launch_bounds__(kTokenThreads, 2) void token_attn_kernel(SeqGeom g,
       float m_run[QT], l_run[QT];
 #pragma unroll
       for (int qt = 0; qt < QT; ++qt) {
-        const Row row = unit_row(g, wk.q, wk.hg, wk.b, 16 * qt + c);
+        const Row row = unit_row(g, wk, 16 * qt + c);
         const uint16_t* src = io.q + (int64_t)(wk.q.q0 + row.token) * io.q_tok + (int64_t)row.head * io.q_head + (D / 4) * lg;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
@@ -301,7 +301,7 @@ __global__ __launch_bounds__(kTokenThreads, 2) void token_attn_kernel(SeqGeom g,
       __syncthreads();
       constexpr int TPR = kTokenThreads / R, W = D / TPR;      // threads of a row, values of a thread
       const int r = tid / TPR, part = tid % TPR;
-      const Row row = unit_row(g, wk.q, wk.hg, wk.b, r);
+      const Row row = unit_row(g, wk, r);
       float mx = -INFINITY;
 #pragma unroll
       for (int w = 0; w < kTokenWaves; ++w) mx = fmaxf(mx, sm_m[w][r]);

@@ -33,6 +33,7 @@ struct SeqGeom {
   int S, Tq, Kcap;         // Kcap: packed keys, or the most keys of a sequence in the cache
   int lq_min, lq_max;      // sequences with other numbers of query tokens are left out
   int Hq, Hkv, G, GH, GS;  // query heads, key heads, Hq / Hkv, heads of a group, groups of a key head
+  int gh_magic;            // r / GH of a packed row r < 256 is r gh_magic >> 16: ceil(2^16 / GH)
   int TB;                  // tokens of a unit
   int causal;
   uint32_t extra;          // weight of a unit beside its keys, >= 1
@@ -116,7 +117,8 @@ struct Walk {
   uint64_t pos, end;       // the stretch still to do
   uint64_t unit0;          // where the present unit starts
   uint32_t snap;           // borders this near a unit's start or end lie there
-  int s, hg, j, b, nb;     // sequence, head group, place of the run among the sequence's, run, runs
+  int s, kvh, part;        // sequence, key head, part of its group
+  int j, b, nb;            // place of the run among the sequence's, run, runs
   Seq q;
   __device__ __forceinline__ bool more() const { return pos < end; }
 };
@@ -164,16 +166,19 @@ __device__ __forceinline__ void walk_on(const SeqGeom& g, Walk& w, uint64_t unit
   if (w.pos >= w.end) return;
   if (++w.j >= w.nb) {
     w.j = 0;
-    if (++w.hg >= g.Hkv * g.GS) {
-      w.hg = 0;
-      do {
-        if (++w.s >= g.S) {                             // not reached while pos < end
-          w.pos = w.end;
-          return;
-        }
-        w.q = load_seq_uniform<CACHE>(g, w.s);
-      } while (w.q.lq == 0);
-      w.nb = runs_of(g, w.q);
+    if (++w.part >= g.GS) {
+      w.part = 0;
+      if (++w.kvh >= g.Hkv) {
+        w.kvh = 0;
+        do {
+          if (++w.s >= g.S) {                           // not reached while pos < end
+            w.pos = w.end;
+            return;
+          }
+          w.q = load_seq_uniform<CACHE>(g, w.s);
+        } while (w.q.lq == 0);
+        w.nb = runs_of(g, w.q);
+      }
     }
   }
   w.b = run_at(g, w.nb, w.j);
@@ -203,7 +208,7 @@ __device__ __forceinline__ Walk start_walk(const SeqGeom& g, int l, int P) {
   w.pos = first_lane_u64((uint64_t)(uint32_t)l * share);
   w.end = w.pos + share < total ? w.pos + share : total;
   w.snap = (uint32_t)(share < g.whole ? share / 2 : (share / 64 < g.extra ? share / 64 : g.extra));
-  w.s = w.hg = w.j = w.b = w.nb = 0;
+  w.s = w.kvh = w.part = w.j = w.b = w.nb = 0;
   w.unit0 = 0;
   w.q = Seq{0, 0, 0, 0};
   if (w.pos >= w.end) return w;
@@ -241,7 +246,8 @@ __device__ __forceinline__ Walk start_walk(const SeqGeom& g, int l, int P) {
     n = min(step, n - i * step);
   }
   w.s = __builtin_amdgcn_readfirstlane(s);
-  w.hg = __builtin_amdgcn_readfirstlane(hg);
+  w.kvh = __builtin_amdgcn_readfirstlane(hg / g.GS);
+  w.part = __builtin_amdgcn_readfirstlane(hg % g.GS);
   w.j = __builtin_amdgcn_readfirstlane(lo);
   w.b = run_at(g, nb, w.j);
   w.nb = nb;
@@ -258,22 +264,21 @@ struct Row {
   int token, head;
   bool ok;
 };
-__device__ __forceinline__ Row unit_row(const SeqGeom& g, const Seq& q, int hg, int b, int r) {
-  const int t = (int)((uint32_t)r / (uint32_t)g.GH), j = r - t * g.GH;
-  const int kvh = hg / g.GS, part = hg - kvh * g.GS;
+__device__ __forceinline__ int unit_head0(const SeqGeom& g, const Walk& w) { return w.kvh * g.G + w.part * g.GH; }
+__device__ __forceinline__ int unit_heads(const SeqGeom& g, const Walk& w) { return min(g.GH, g.G - w.part * g.GH); }
+__device__ __forceinline__ Row unit_row(const SeqGeom& g, const Walk& w, int r) {
+  const int t = (int)(((uint32_t)r * (uint32_t)g.gh_magic) >> 16), j = r - t * g.GH;
   Row x;
-  x.token = b * g.TB + t;
-  x.head = kvh * g.G + part * g.GH + j;
-  x.ok = t < g.TB && x.token < q.lq && part * g.GH + j < g.G;
+  x.token = w.b * g.TB + t;
+  x.head = unit_head0(g, w) + j;
+  x.ok = t < min(g.TB, w.q.lq - w.b * g.TB) && j < unit_heads(g, w);
   return x;
 }
 
 // What a merge has to know of a unit: its first row of q and o, tokens, first head, heads.  The first and
 // the third name the unit.
 __device__ __forceinline__ int4 unit_record(const SeqGeom& g, const Walk& w) {
-  const int kvh = w.hg / g.GS, part = w.hg - kvh * g.GS;
-  return int4{w.q.q0 + w.b * g.TB, min(g.TB, w.q.lq - w.b * g.TB), kvh * g.G + part * g.GH,
-              min(g.GH, g.G - part * g.GH)};
+  return int4{w.q.q0 + w.b * g.TB, min(g.TB, w.q.lq - w.b * g.TB), unit_head0(g, w), unit_heads(g, w)};
 }
 
 // Keys that token t of the sequence sees.
