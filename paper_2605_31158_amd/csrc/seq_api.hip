@@ -120,8 +120,11 @@ CacheGeom cache_geom(const la_seqs& s, const la_kv4& kv, const void* cache, cons
 }
 
 // How a call over a cache is made: sequences of at most lq_token query tokens by token_attn_kernel with
-// `rows` packed rows, those of more by seq_attn_kernel.
-constexpr int kTokenRows = 64;
+// `rows` packed rows a unit, those of more by seq_attn_kernel.  The first reads the cache once for every
+// 32 rows, the second converts a tile once for 256 but takes longer to start a unit: over 6000 tokens, 4
+// key heads of 4 query heads, 8 sequences of 128 rows 37 against 55 us, 2 of 256 rows 33 against 46, 32 of
+// 128 rows 73 against 100, 32 of 256 rows 133 against 114.
+constexpr int kTokenRows = 192;
 constexpr int kTokenPerCu = 2;
 struct CachePlan {
   int lq_token, rows;

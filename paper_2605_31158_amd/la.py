@@ -782,7 +782,7 @@ def prompt_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.T
     _, _, _, vt, vh = _rows("v", v, dev, Hkv, d, Tk)
     if cu_k is None:
         cu_k = cu_q
-    S = cu_q.numel() - 1
+    S = cu_q.numel() - 1 if isinstance(cu_q, torch.Tensor) else 0
     _check_ints("cu_q", cu_q, dev, (S + 1,))
     _check_ints("cu_k", cu_k, dev, (S + 1,))
     o, ot, oh, lse = _outputs(q, dev, Tq, Hq, d, want_lse, out, lse_out)

@@ -278,3 +278,76 @@ def test_far_pages():
         want = R.attention(q, lambda s, h: (kr[2500 * s: 2500 * s + lens[s], h], vr[2500 * s: 2500 * s + lens[s], h]), lq,
                            lens, True)
         R.check(o, None, want, f"far pages, queries {lq}")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_missing_and_far_pages_with_many_queries(d):
+    # as above, with enough query rows for the kernel that converts tiles on their way to LDS
+    page, Hkv = 16, 2
+    lens = [50, 40]
+    table = torch.tensor([[3, -1, 1, 2, 7], [0, 4, 1000000, -5, 2]], dtype=torch.int32, device="cuda")
+    cache = la.kv4_cache(5, Hkv, d, page)
+    cache.fill_(0xFF)
+    k, v = (torch.randn((90, Hkv, d), device="cuda").to(torch.bfloat16) for _ in range(2))
+    la.kv4_append(cache, k, v, R.starts(lens), ints(lens), table)
+    kr, vr = la.kv4_read(cache, R.starts(lens), ints(lens), table, 90, d)
+    lq = [230, 300]
+    q = torch.randn((sum(lq), 4, d), device="cuda").to(torch.bfloat16)
+    for causal in (False, True):
+        o, lse = la.kv4_attn(q, cache, R.starts(lq), ints(lens), table, max(lq), causal=causal, want_lse=True)
+        want = R.attention(q, lambda s, h: (kr[50 * s: 50 * s + lens[s], h // 2], vr[50 * s: 50 * s + lens[s], h // 2]),
+                           lq, lens, causal)
+        R.check(o, lse, want, f"missing pages, many queries, causal {causal}")
+    # past 32 bits of bytes
+    nbytes = 1024 * (d + d // 16)
+    n = (5 << 30) // (Hkv * nbytes)
+    cache = torch.empty((n, Hkv, nbytes), dtype=torch.uint8, device="cuda")
+    cache[-3:] = 0xFF
+    lens = [2500, 100]
+    table = torch.tensor([[n - 1, n - 2, n - 3], [5, -1, -1]], dtype=torch.int32, device="cuda")
+    k, v = (torch.randn((2600, Hkv, d), device="cuda").to(torch.bfloat16) for _ in range(2))
+    la.kv4_append(cache, k, v, R.starts(lens), ints(lens), table)
+    kr, vr = la.kv4_read(cache, R.starts(lens), ints(lens), table, 2600, d)
+    lq = [400, 40]
+    q = torch.randn((sum(lq), Hkv, d), device="cuda").to(torch.bfloat16)
+    o = la.kv4_attn(q, cache, R.starts(lq), ints(lens), table, max(lq))
+    want = R.attention(q, lambda s, h: (kr[2500 * s: 2500 * s + lens[s], h], vr[2500 * s: 2500 * s + lens[s], h]), lq, lens,
+                       True)
+    R.check(o, None, want, "far pages, many queries")
+
+
+def test_values_that_are_not_finite():
+    # a block with such a value reads as NaN, and reaches the queries that see it and no others
+    lens, d, page = [100, 100], 128, 16
+    cache, table, L, _, _ = filled(lens, 1, d, page, 9, fill=0x00)
+    k, v = (torch.randn((2, 1, d), device="cuda").to(torch.bfloat16) for _ in range(2))
+    v[1, 0, 40] = float("inf")
+    la.kv4_append(cache, k, v, R.starts([0, 2]), L, table)              # the last tokens of sequence 1
+    kr, vr = la.kv4_read(cache, R.starts([0, 2]), L, table, 2, d)
+    assert bool(torch.isnan(vr[1, 0, 32:64]).all()) and bool(torch.isfinite(vr[1, 0, :32]).all())
+    assert bool(torch.isfinite(kr).all()) and bool(torch.isfinite(vr[0]).all())
+    q = torch.randn((2, 4, d), device="cuda").to(torch.bfloat16)
+    o = la.kv4_attn(q, cache, R.starts([1, 1]), L, table, 1)
+    assert bool(torch.isfinite(o[0]).all()) and bool(torch.isnan(o[1, :, 32:64]).all())
+    assert bool(torch.isfinite(o[1, :, :32]).all()) and bool(torch.isfinite(o[1, :, 64:]).all())
+    short = L - torch.tensor([0, 1], dtype=torch.int32, device="cuda")  # the token is behind the end now
+    assert bool(torch.isfinite(la.kv4_attn(q, cache, R.starts([1, 1]), short, table, 1)).all())
+
+
+def test_random_caches():
+    gen = torch.Generator().manual_seed(7)
+    for n in range(24):
+        S = int(torch.randint(1, 7, (1,), generator=gen))
+        page = [16, 32, 64, 256][n % 4]
+        most = [1, 3, 20, 300][n % 4 if n < 16 else (n + 1) % 4]
+        lq = torch.randint(0, most + 1, (S,), generator=gen).tolist()
+        lens = torch.randint(0, 1500, (S,), generator=gen).tolist()
+        Hkv, G, d, causal = [1, 2, 3][n % 3], [1, 2, 4, 5, 20][n % 5], [64, 128][n % 2], n % 4 != 2
+        print(f"[kv4] random {n}: {lq} over {lens} G {G} Hkv {Hkv} d {d} page {page}", flush=True)
+        cache, table, L, k, v = filled(lens, Hkv, d, page, 50 + n)
+        q = (torch.randn((sum(lq), G * Hkv, d), device="cuda") * 1.5).to(torch.bfloat16)
+        o, lse = la.kv4_attn(q, cache, R.starts(lq), L, table, max(lq), causal=causal, want_lse=True)
+        at = [sum(lens[:s]) for s in range(S)]
+        want = R.attention(q, lambda s, h: (k[at[s]: at[s] + lens[s], h // G], v[at[s]: at[s] + lens[s], h // G]), lq, lens,
+                           causal)
+        R.check(o, lse, want, f"random {n}")

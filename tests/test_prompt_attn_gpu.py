@@ -185,3 +185,43 @@ def test_random_lengths():
         q, k, v = make(lq, lk, G * Hkv, Hkv, d, 100 + n)
         o, lse = la.prompt_attn(q, k, v, R.starts(lq), R.starts(lk), causal=causal, want_lse=True)
         R.check(o, lse, reference(q, k, v, lq, lk, causal), f"random {n}")
+
+
+def test_without_keys_and_shared_workspace():
+    q = torch.randn((5, 4, 64), device="cuda").to(torch.bfloat16)
+    none = torch.empty((0, 2, 64), dtype=torch.bfloat16, device="cuda")
+    o, lse = la.prompt_attn(q, none, none, R.starts([2, 3]), R.starts([0, 0]), want_lse=True)
+    assert bool((o == 0).all()) and bool((lse == -torch.inf).all())
+    assert la.prompt_attn(q[:0], none, none, R.starts([0, 0])).shape == (0, 4, 64)
+    # one workspace for several calls in turn, and captured ones among them
+    ws = torch.empty(1 << 27, dtype=torch.uint8, device="cuda")
+    sizes = [([900], 128), ([20, 300], 64), ([5] * 40, 128)]
+    made = [(*make(lq, lq, 8, 2, d, 20 + i), R.starts(lq)) for i, (lq, d) in enumerate(sizes)]
+    want = [la.prompt_attn(*m) for m in made]
+    graphs, outs = [], []
+    for m in made:
+        out = torch.empty_like(m[0])
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            la.prompt_attn(*m, ws=ws, out=out)
+        graphs.append(graph), outs.append(out)
+    for r in range(3):
+        for graph, out, w, m in zip(graphs, outs, want, made):
+            out.zero_()
+            graph.replay()
+            assert torch.equal(la.prompt_attn(*m, ws=ws), w)
+            torch.cuda.synchronize()
+            assert torch.equal(out, w), r
+
+
+def test_wide_strides():
+    # a head's rows lie 64 MB apart
+    L, H = 1 << 18, 24
+    buf = torch.empty((H, L, 128), dtype=torch.bfloat16, device="cuda")
+    q = buf[:, :70].transpose(0, 1)
+    q.copy_(torch.randn((70, H, 128), device="cuda"))
+    k, v = (torch.randn((70, 1, 128), device="cuda").to(torch.bfloat16) for _ in range(2))
+    o = la.prompt_attn(q, k, v, R.starts([70]))
+    R.check(o, None, reference(q, k, v, [70], [70], True), "wide strides")
