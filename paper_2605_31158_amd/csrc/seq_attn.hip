@@ -97,27 +97,28 @@ struct CacheTiles {
   Codes codes;
   uint32_t scales;
   int part;                // K: which quarter of the row; V: which chunk
-  uint32_t dst_off[4];
+  uint32_t dst0;
 
   __device__ __forceinline__ void init(const SeqIo&, const CacheGeom& cg_, int lw, int lane) {
     cg = cg_;
     const int gt = lw * 64 + lane;
+    // row r = at_tile + j of a V tile, or slot (d / 32) part + j of a K row, is swizzled by an exclusive or
+    // of j's bits with those of j = 0, at which `dst0` points
     if (V) {
+      constexpr int CB = 2 * Mma<D>::MR;                    // bytes that are permuted as one
       at_tile = 4 * (gt >> 4);
       part = gt & 15;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        constexpr int CB = 2 * Mma<D>::MR;                  // bytes that are permuted as one
-        const int lo = part * (D / 8), r = at_tile + j;
-        dst_off[j] = (uint32_t)(r * T::STRIDE + ((lo / CB) ^ T::vswz(r)) * CB + lo % CB);
-      }
+      const int lo = part * (D / 8);
+      dst0 = (uint32_t)(at_tile * T::STRIDE + ((lo / CB) ^ T::vswz(at_tile)) * CB + lo % CB);
     } else {
       at_tile = gt >> 2;
       part = gt & 3;
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        dst_off[j] = (uint32_t)(at_tile * T::STRIDE + (((D / 32) * part + j) ^ T::kswz(at_tile)) * 16);
+      dst0 = (uint32_t)(at_tile * T::STRIDE + (((D / 32) * part) ^ T::kswz(at_tile)) * 16);
     }
+  }
+  __device__ __forceinline__ uint32_t dst_off(int j) const {
+    return V ? (dst0 ^ (uint32_t)((D == 128 ? j : j >> 1) * 2 * Mma<D>::MR)) + (uint32_t)(j * T::STRIDE)
+             : dst0 ^ (uint32_t)(16 * j);
   }
   __device__ __forceinline__ void load_id() {
     const int idx = min((key + at_tile) >> cg.log_p, cg.max_pages - 1);
@@ -146,16 +147,16 @@ struct CacheTiles {
       for (int j = 0; j < 4; ++j) {
         const float sc = j < nv ? scale_of(scales, j) : 1.0f;
         if constexpr (D == 128) {
-          *(u32x4*)(dst + dst_off[j]) = fp4x8(j < nv ? codes[j] : 0u, sc);
+          *(u32x4*)(dst + dst_off(j)) = fp4x8(j < nv ? codes[j] : 0u, sc);
         } else {
           const uint32_t w = j < nv ? codes[j >> 1] >> (16 * (j & 1)) : 0u;
-          *(u32x2*)(dst + dst_off[j]) = u32x2{fp4x2<0>(w, sc), fp4x2<1>(w, sc)};
+          *(u32x2*)(dst + dst_off(j)) = u32x2{fp4x2<0>(w, sc), fp4x2<1>(w, sc)};
         }
       }
     } else {
       const float sc = nv ? scale_of(scales, 0) : 1.0f;
 #pragma unroll
-      for (int j = 0; j < D / 32; ++j) *(u32x4*)(dst + dst_off[j]) = fp4x8(nv ? codes[j] : 0u, sc);
+      for (int j = 0; j < D / 32; ++j) *(u32x4*)(dst + dst_off(j)) = fp4x8(nv ? codes[j] : 0u, sc);
     }
   }
   __device__ __forceinline__ void prime(const SeqIo&, const Walk& wk, int kvh_, int ta, int tb_, unsigned char* d0,
@@ -287,10 +288,23 @@ __device__ __forceinline__ void end_rows(const PieceState<D>& st, const SeqGeom&
   }
 }
 
+struct SeqArgs {
+  SeqGeom g;
+  SeqIo io;
+  CacheGeom cg;
+};
+
+// The arguments of seq_attn_kernel, read anew: 50 scalar registers that a piece needs at its ends must
+// not be held over its loop, which needs nearly all there are.
+__device__ __forceinline__ SeqArgs fresh_args() {
+  typedef const __attribute__((address_space(4))) SeqArgs CArgs;
+  CArgs* p = (CArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const SeqArgs*)p;
+}
+
 template <int D, bool CACHE>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void seq_attn_kernel(SeqGeom g,
-                                                                                                      SeqIo io,
-                                                                                                      CacheGeom cg) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void seq_attn_kernel(SeqArgs) {
   using T = Tile<D>;
   using X = Mma<D>;
   __shared__ __attribute__((aligned(1024))) unsigned char ring[6 * T::BYTES];
@@ -299,8 +313,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int P = gridDim.x;
   const int lambda = (blockIdx.x & 7) * (P >> 3) + (blockIdx.x >> 3);
   const int tid = threadIdx.x, lane = tid & 63;
-  if (tid == 0) io.cut[2 * lambda] = io.cut[2 * lambda + 1] = int4{0, 0, 0, 0};
-  Walk wk = start_walk<CACHE>(g, lambda, P);
+  Walk wk;
+  float scale_log2;
+  {
+    const SeqArgs a = fresh_args();
+    if (tid == 0) a.io.cut[2 * lambda] = a.io.cut[2 * lambda + 1] = int4{0, 0, 0, 0};
+    wk = start_walk<CACHE>(a.g, lambda, P);
+    scale_log2 = a.io.scale_log2;
+  }
   if (!wk.more()) return;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lw = wave & 3;
@@ -315,7 +335,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
               8 * (lane & 3);
   }
   w.g4 = 4 * lg;
-  w.scale_log2 = io.scale_log2;
+  w.scale_log2 = scale_log2;
   PieceState<D> st;
 
   // Iteration i of a piece's tiles (phases as in attn.hip): tile i lies in stage i % 3.  Group 0
@@ -325,20 +345,30 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     constexpr bool IS_G1 = decltype(G1)::value;
     constexpr int VOFF = 3 * T::BYTES;
     typename std::conditional<CACHE, CacheTiles<D, IS_G1>, RowTiles<D, IS_G1>>::type src;
-    src.init(io, cg, lw, lane);
+    {
+      const SeqArgs a = fresh_args();
+      src.init(a.io, a.cg, lw, lane);
+    }
     unsigned char* const s0 = ring;
     unsigned char* const s1 = ring + T::BYTES;
     unsigned char* const s2 = ring + 2 * T::BYTES;
     while (wk.more()) {
       uint64_t unit_end;
-      const Piece pc = walk_piece(g, wk, &unit_end);
+      Piece pc;
+      {
+        const SeqArgs a = fresh_args();
+        pc = walk_piece(a.g, wk, &unit_end);
+      }
       const int N = pc.tb - pc.ta;
       if (N > 0) {
-        src.prime(io, wk, wk.kvh, pc.ta, pc.tb, IS_G1 ? s0 + VOFF : s0, IS_G1 ? nullptr : s1);
-        start_rows<D>(st, w, g, io, wk, r_off, c, lg);
-        // first tile that some row of the unit does not see whole
-        const int open = g.causal ? max(0, wk.q.lk - wk.q.lq + wk.b * g.TB + 1) : wk.q.lk;
-        const int key_open = min(open, wk.q.lk) - 63;
+        int key_open;                                 // first tile that some row of the unit does not see whole
+        {
+          const SeqArgs a = fresh_args();
+          src.prime(a.io, wk, wk.kvh, pc.ta, pc.tb, IS_G1 ? s0 + VOFF : s0, IS_G1 ? nullptr : s1);
+          start_rows<D>(st, w, a.g, a.io, wk, r_off, c, lg);
+          const int open = a.g.causal ? max(0, wk.q.lk - wk.q.lq + wk.b * a.g.TB + 1) : wk.q.lk;
+          key_open = min(open, wk.q.lk) - 63;
+        }
         __builtin_amdgcn_s_waitcnt(0);
         phase_barrier();
         auto m_phase = [&](int i, const unsigned char* kcur, const unsigned char* vprev) {
@@ -376,11 +406,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
           iteration(i + 2, s2, s1, s0);
           if (i + 3 > N) break;
         }
-        end_rows<D>(st, g, io, wk, pc, 2 * lambda, r_off, c, lg);
+        const SeqArgs a = fresh_args();
+        end_rows<D>(st, a.g, a.io, wk, pc, 2 * lambda, r_off, c, lg);
         // the loads behind the piece have landed before the next one's (or the end of the workgroup)
         __builtin_amdgcn_s_waitcnt(0);
       }
-      walk_on<CACHE>(g, wk, unit_end);
+      const SeqArgs a = fresh_args();
+      walk_on<CACHE>(a.g, wk, unit_end);
     }
   };
   if (wave >= 4) run(std::true_type{});
@@ -503,7 +535,7 @@ void launch_merge(const SeqGeom& g, const SeqIo& io, int P, hipStream_t st) {
 
 template <int D, bool CACHE>
 static hipError_t launch_rows(const SeqGeom& g, const SeqIo& io, const CacheGeom& cg, int P, hipStream_t st) {
-  hipLaunchKernelGGL((seq_attn_kernel<D, CACHE>), dim3(P), dim3(kThreads), 0, st, g, io, cg);
+  hipLaunchKernelGGL((seq_attn_kernel<D, CACHE>), dim3(P), dim3(kThreads), 0, st, SeqArgs{g, io, cg});
   launch_merge<D, QR>(g, io, P, st);
   return hipGetLastError();
 }
