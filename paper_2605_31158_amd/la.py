@@ -845,10 +845,12 @@ def kv4_read(cache: torch.Tensor, cu: torch.Tensor, lens: torch.Tensor, table: t
     dev = cache.get_device()
     if out is None:
         k, v = torch.empty((2, tokens, H, d), dtype=torch.bfloat16, device=cache.device).unbind(0)
+        kt = vt = H * d
+        kh = vh = d
     else:
         k, v = out
-    _, _, _, kt, kh = _rows("k", k, dev, H, d, tokens)
-    _, _, _, vt, vh = _rows("v", v, dev, H, d, tokens)
+        _, _, _, kt, kh = _rows("k", k, dev, H, d, tokens)
+        _, _, _, vt, vh = _rows("v", v, dev, H, d, tokens)
     _on_device(dev, "la_kv4_read", ctypes.byref(Seqs(S, 0, tokens, H, H, d, 0, 0, 0, 0, 0, kt, kh, vt, vh)), kv,
                cache.data_ptr(), cu.data_ptr(), lens.data_ptr(), table.data_ptr(), k.data_ptr(), v.data_ptr(),
                _stream(cache))
