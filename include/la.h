@@ -366,7 +366,7 @@ typedef struct la_seqs {
 } la_seqs;
 
 /* Bytes of scratch that la_prompt_attn needs (partial results of work that is split between
- * workgroups); 0 for an invalid la_seqs, and where there is nothing to do. */
+ * workgroups); 0 where it needs none (few keys), and for an invalid la_seqs. */
 size_t la_prompt_ws_bytes(const la_seqs* seqs);
 
 /* Attention over whole prompts: softmax(q k^T scale) v of every sequence over its own keys.
@@ -374,7 +374,7 @@ size_t la_prompt_ws_bytes(const la_seqs* seqs);
  *   scale       <= 0 selects 1/sqrt(d).
  *   o           bf16, strides o_token and o_head;  lse  float [Tq, Hq] or NULL: natural-log sum of
  *               exp(logits).
- * Softmax in fp32, products in bf16 with fp32 accumulation.  Kernel launches only (two): a caller
+ * Softmax in fp32, products in bf16 with fp32 accumulation.  Kernel launches only (one or two): a caller
  * may capture the call; calls that may overlap need a ws each. */
 la_status la_prompt_attn(const la_seqs* seqs, const void* q, const void* k, const void* v,
                          const int32_t* cu_q, const int32_t* cu_k, float scale, void* o, float* lse,
@@ -417,7 +417,8 @@ la_status la_kv4_append(const la_seqs* seqs, const la_kv4* kv, const void* k, co
 la_status la_kv4_read(const la_seqs* seqs, const la_kv4* kv, const void* cache, const int32_t* cu,
                       const int32_t* lens, const int32_t* table, void* k, void* v, void* stream);
 
-/* Bytes of scratch that la_kv4_attn needs; 0 for invalid arguments, and where there is nothing to do. */
+/* Bytes of scratch that la_kv4_attn needs; 0 where it needs none (tables of few tokens), and for
+ * invalid arguments. */
 size_t la_kv4_ws_bytes(const la_seqs* seqs, const la_kv4* kv, int32_t max_q);
 
 /* Attention of every sequence's queries over its cache: la_prompt_attn with the keys and values that

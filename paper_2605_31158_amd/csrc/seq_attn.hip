@@ -317,7 +317,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   float scale_log2;
   {
     const SeqArgs a = fresh_args();
-    if (tid == 0) a.io.cut[2 * lambda] = a.io.cut[2 * lambda + 1] = int4{0, 0, 0, 0};
+    if (a.g.cuts && tid == 0) a.io.cut[2 * lambda] = a.io.cut[2 * lambda + 1] = int4{0, 0, 0, 0};
     wk = start_walk<CACHE>(a.g, lambda, P);
     scale_log2 = a.io.scale_log2;
   }
@@ -536,7 +536,7 @@ void launch_merge(const SeqGeom& g, const SeqIo& io, int P, hipStream_t st) {
 template <int D, bool CACHE>
 static hipError_t launch_rows(const SeqGeom& g, const SeqIo& io, const CacheGeom& cg, int P, hipStream_t st) {
   hipLaunchKernelGGL((seq_attn_kernel<D, CACHE>), dim3(P), dim3(kThreads), 0, st, SeqArgs{g, io, cg});
-  launch_merge<D, QR>(g, io, P, st);
+  if (g.cuts) launch_merge<D, QR>(g, io, P, st);
   return hipGetLastError();
 }
 

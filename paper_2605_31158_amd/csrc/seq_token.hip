@@ -76,7 +76,7 @@ __global__ __launch_bounds__(kTokenThreads, 2) void token_attn_kernel(SeqGeom g,
   const int lambda = (blockIdx.x & 7) * (P >> 3) + (blockIdx.x >> 3);
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  if (tid == 0) io.cut[2 * lambda] = io.cut[2 * lambda + 1] = int4{0, 0, 0, 0};
+  if (g.cuts && tid == 0) io.cut[2 * lambda] = io.cut[2 * lambda + 1] = int4{0, 0, 0, 0};
   Walk wk = start_walk<true>(g, lambda, P);
   const int page = 1 << cg.log_p;
 
@@ -362,7 +362,7 @@ hipError_t launch_cache_tokens(const SeqGeom& g, const SeqIo& io, const CacheGeo
   hipError_t e;
   if (rows == 16) e = d == 128 ? launch_qt<128, 1>(g, io, cg, P, st) : launch_qt<64, 1>(g, io, cg, P, st);
   else e = d == 128 ? launch_qt<128, 2>(g, io, cg, P, st) : launch_qt<64, 2>(g, io, cg, P, st);
-  return e == hipSuccess ? launch_cache_merge(g, io, d, rows, P, st) : e;
+  return e == hipSuccess && g.cuts ? launch_cache_merge(g, io, d, rows, P, st) : e;
 }
 
 }  // namespace la

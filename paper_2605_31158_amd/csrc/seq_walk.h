@@ -37,6 +37,7 @@ struct SeqGeom {
   int TB;                  // tokens of a unit
   int causal;
   uint32_t extra;          // weight of a unit beside its keys, >= 1
+  uint32_t cuts;           // 0: no unit is cut, the workgroup whose share holds its end does all of it
   uint32_t whole;          // shares below this end where the nearest unit does
   uint32_t min_share;      // more than two tiles, so that a share among a unit's keys is never empty
 };
@@ -207,7 +208,7 @@ __device__ __forceinline__ Walk start_walk(const SeqGeom& g, int l, int P) {
   Walk w;
   w.pos = first_lane_u64((uint64_t)(uint32_t)l * share);
   w.end = w.pos + share < total ? w.pos + share : total;
-  w.snap = (uint32_t)(share < g.whole ? share / 2 : (share / 64 < g.extra ? share / 64 : g.extra));
+  w.snap = !g.cuts ? ~0u : (uint32_t)(share < g.whole ? share / 2 : (share / 64 < g.extra ? share / 64 : g.extra));
   w.s = w.kvh = w.part = w.j = w.b = w.nb = 0;
   w.unit0 = 0;
   w.q = Seq{0, 0, 0, 0};

@@ -351,3 +351,29 @@ def test_random_caches():
         want = R.attention(q, lambda s, h: (k[at[s]: at[s] + lens[s], h // G], v[at[s]: at[s] + lens[s], h // G]), lq, lens,
                            causal)
         R.check(o, lse, want, f"random {n}")
+
+
+@pytest.mark.parametrize("lq", [1, 2, 70])
+@pytest.mark.parametrize("d", [64, 128])
+def test_narrow_and_wide_tables(lq, d):
+    # tables of up to 1024 tokens (512 for many queries) leave no work to be joined, wider ones may; a wider
+    # table alone changes no result beyond the roundings of both ways
+    lens = [1024, 1, 64, 500, 0, 1000] * (12 if lq < 3 else 2)
+    cache, table, L, k, v = filled(lens, 2, d, 64, 9)
+    S, n = len(lens), lq * len(lens)
+    table = table[:, :16].contiguous()
+    q = (torch.randn((n, 8, d), device="cuda") * 1.5).to(torch.bfloat16)
+    cu, at = R.starts([lq] * S), [sum(lens[:s]) for s in range(S)]
+    want = R.attention(q, lambda s, h: (k[at[s]: at[s] + lens[s], h // 4], v[at[s]: at[s] + lens[s], h // 4]), [lq] * S,
+                       lens, True)
+    for more in (0, 1, 300):
+        t = torch.cat([table, torch.full((S, more), -1, dtype=torch.int32, device="cuda")], 1).contiguous()
+        o, lse = la.kv4_attn(q, cache, cu, L, t, lq, want_lse=True)
+        R.check(o, lse, want, f"{more} more columns")
+    # a table of 512 tokens: what lies behind them is not seen
+    short = table[:, :8].contiguous()
+    lens = [min(x, 512) for x in lens]
+    want = R.attention(q, lambda s, h: (k[at[s]: at[s] + lens[s], h // 4], v[at[s]: at[s] + lens[s], h // 4]), [lq] * S,
+                       lens, True)
+    o, lse = la.kv4_attn(q, cache, cu, L, short, lq, want_lse=True)
+    R.check(o, lse, want, "512 tokens")

@@ -225,3 +225,14 @@ def test_wide_strides():
     k, v = (torch.randn((70, 1, 128), device="cuda").to(torch.bfloat16) for _ in range(2))
     o = la.prompt_attn(q, k, v, R.starts([70]))
     R.check(o, None, reference(q, k, v, [70], [70], True), "wide strides")
+
+
+@pytest.mark.parametrize("lq,lk", [([512], [512]), ([513], [513]), ([5000], [500]), ([100] * 5, [100] * 5),
+                                   ([3] * 700, [0] * 300 + [1] * 300 + [2] * 100), ([300, 800], [500, 12]),
+                                   ([300, 800], [500, 13])], ids=lambda x: f"{len(x)}x{x[0]}")
+@pytest.mark.parametrize("causal", [True, False])
+def test_few_keys(lq, lk, causal):
+    # up to 512 keys in all no work is split, whatever the number of queries and sequences
+    q, k, v = make(lq, lk, 12, 4, 64, 31)
+    o, lse = la.prompt_attn(q, k, v, R.starts(lq), R.starts(lk), causal=causal, want_lse=True)
+    R.check(o, lse, reference(q, k, v, lq, lk, causal), "few keys")

@@ -35,7 +35,7 @@ def test_prompt_shapes_refused(bad):
 
 @cpu_only
 def test_prompt_arguments_refused():
-    s = seqs()
+    s = seqs(Tk=2000)
     assert prompt(None) == la.LA_ERR_ARG
     for name in ("q", "k", "v", "o", "cu_q", "cu_k"):
         assert prompt(s, **{name: None}) == la.LA_ERR_ARG, name
@@ -62,7 +62,8 @@ def test_prompt_with_nothing_to_do():
     # scratch stops growing with the work: partials of 256 workgroups
     most = la.lib().la_prompt_ws_bytes(ctypes.byref(seqs(Tq=1 << 20, Tk=1 << 20)))
     assert 2 * 256 * 256 * 128 * 4 <= most < 2 * 256 * 256 * 131 * 4
-    assert la.lib().la_prompt_ws_bytes(ctypes.byref(seqs(S=1, Tq=1, Tk=64))) < 1 << 23
+    assert la.lib().la_prompt_ws_bytes(ctypes.byref(seqs(S=1, Tq=1, Tk=2000))) < 1 << 23
+    assert la.lib().la_prompt_ws_bytes(ctypes.byref(seqs(S=1, Tq=1, Tk=64))) == 0      # nothing is split
 
 
 def test_binding_refuses_cpu_tensors():
@@ -134,6 +135,8 @@ def test_kv4_arguments_refused():
     assert attn(s, c, max_q=-1) == la.LA_ERR_ARG
     assert attn(s, c, scale=float("nan")) == la.LA_ERR_ARG
     assert attn(s, c, lse=ctypes.c_void_p(4097)) == la.LA_ERR_ARG
+    assert la.lib().la_kv4_ws_bytes(ctypes.byref(s), ctypes.byref(c), 1) == 0           # 256 tokens: nothing is split
+    c = kv4(max_pages=100)
     for max_q in (1, 17, 100):
         need = la.lib().la_kv4_ws_bytes(ctypes.byref(s), ctypes.byref(c), max_q)
         assert need > 0
