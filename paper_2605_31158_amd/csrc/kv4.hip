@@ -10,7 +10,10 @@
 // instruction, after an exact multiplication by 2^-e.
 //
 // Both are streaming passes bound by HBM: 2 bytes per value on one side, 17/32 on the other.  A group
-// of d / 8 lanes has a token's row of one head, 16 bytes a lane; four lanes share a block's maximum.
+// of d / 8 lanes has a token's row of one head, 16 bytes a lane; four lanes share a block's maximum.  6240
+// tokens of 16 heads, d 128 (65 MB either way): 11.0 us entered, 10.7 read, 5.9 TB/s, since part of it is
+// found in the last-level cache; 64 tokens of 8 heads 3.7 us each, which is the launch and a chain of
+// loads (starts, length, page number, row).
 #include "kv4.h"
 
 namespace la {

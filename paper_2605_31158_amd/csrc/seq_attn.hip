@@ -15,6 +15,15 @@
 // Differences from attn.hip: the tiles of a piece are consecutive, so nothing is read to know the
 // next one (no records); K and V rows have a stride; and the loop ends with the piece, so a piece
 // pays one load latency of its own.
+//
+// Bound by the matrix pipeline under the card's power limit where pieces are long: 8192 causal tokens, 16
+// query heads over 4, d 128, in 213 us, 1.29 PFLOP/s of the 1.36 that a large bf16 product of random data
+// reaches here (1.63 us a tile of 256 x 64); 6240 queries over 12480 tokens of a 4-bit cache, 16 heads, in
+// 520 us, 1.23 PFLOP/s.  A piece costs about 8 us beside its tiles: the 128 KB of Q and O that every
+// workgroup moves at the same time, and the latency of the first tiles.  Sequences of 150 to 3300 tokens
+// (6, 24 heads over 8) take 124 us where their products alone take 77.  Holding the next piece's Q in LDS,
+// with its tiles issued before the results are written, was right and no faster (registers, and the
+// bytes are the same).
 #include <math.h>
 
 #include <type_traits>

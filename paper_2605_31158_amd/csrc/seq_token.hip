@@ -12,8 +12,15 @@
 //
 // A workgroup's four waves take the tiles (64 keys) of a piece in turn, each with its own (m, l, O);
 // they are joined in LDS at the end of the piece.  Pieces are shares of one line of work (seq_walk.h),
-// cut units are joined by seq_merge (seq_attn.hip).  Each wave has the next tile's codes in flight while
-// it works on one, and the page numbers of the one behind.
+// cut units are joined by seq_merge (seq_attn.hip).  Each wave issues the next tile's codes, and the page
+// numbers of the one behind, before it works on one.  (The compiler joins the paths with and without a
+// next tile and waits for the loads of the shorter one, so a wave may wait for most of what it issued;
+// loads without the branch, with waits for exactly the present tile, took the same time, 40.4 against
+// 41.0 us on 32 sequences: eight waves to a CU cover one another.)
+//
+// 32 sequences of 1000 to 16000 tokens (32 query heads over 8, d 128: 190 MB) take 49 us, 4 of them
+// before the first codes arrive and 4.5 for the join: 4.7 TB/s while it streams, a large copy's rate being
+// 5.1; with most of it in the last-level cache 41 us, 5.8 TB/s.  One sequence of 1000 tokens takes 11 us.
 #include <math.h>
 
 #include <type_traits>
