@@ -319,7 +319,8 @@ la_status la_untile_o_3d(const la_grid3d* grid, const void* o_tiled, const float
  * turns back, and turning by -p undoes (and is the gradient of) turning by p at amplitude 1.
  * -------------------------------------------------------------------------- */
 typedef struct la_rope_shape {
-  int32_t B, L;              /* sequences of L tokens that share their positions (packed tokens: B = 1) */
+  int32_t B, L;              /* sequences of L tokens (<= 2^26 - 4) that share their positions (packed tokens:
+                                B = 1) */
   int32_t Hq, Hk;            /* heads of q and of k; 0: that tensor is not given */
   int32_t d;                 /* 64 or 128 */
   int32_t rot;               /* values of a head that are turned: a multiple of 16, 16 to d */
@@ -355,7 +356,7 @@ la_status la_rope(const la_rope_shape* shape, const void* q, void* q_out, const 
  * -------------------------------------------------------------------------- */
 typedef struct la_seqs {
   int32_t S;                 /* sequences (>= 0) */
-  int32_t Tq, Tk;            /* rows of q and o, and of k and v (>= 0) */
+  int32_t Tq, Tk;            /* rows of q and o, and of k and v (>= 0); these and S at most 2^31 - 4096 */
   int32_t Hq, Hkv;           /* heads: Hq a multiple of Hkv */
   int32_t d;                 /* 64 or 128 */
   int32_t causal;            /* 0 or 1 */
@@ -397,7 +398,8 @@ la_status la_prompt_attn(const la_seqs* seqs, const void* q, const void* k, cons
 typedef struct la_kv4 {
   int32_t n_pages;           /* >= 1 */
   int32_t page;              /* tokens of a page: a power of two, 16 to 1024 */
-  int32_t max_pages;         /* pages of a row of the table, >= 1; a sequence ends at max_pages * page tokens */
+  int32_t max_pages;         /* pages of a row of the table, >= 1; a sequence ends at max_pages * page tokens, and at
+                                2^31 - 4096 */
 } la_kv4;
 
 /* Bytes of one key head's part of a page, page (d + d / 16); 0 for an unsupported d or page. */
@@ -407,7 +409,8 @@ size_t la_kv4_page_bytes(int32_t d, int32_t page);
  *   k, v  bf16 [Tk, Hkv, d] (la_seqs: S, Tk, Hkv, d and their strides are read; the rest is not).
  *   cu    int32 [S + 1]: rows [cu[s], cu[s + 1]) are the last tokens of sequence s, so that the last
  *         row is token lens[s] - 1.  Tokens before 0 or past the table are dropped.
- * Two rows must not go to one place (a page that two sequences share is entered by one of them). */
+ * Two rows must not go to one place (a page that two sequences share is entered by one of them).  Tk is
+ * at most 2^28 - 32, here and for la_kv4_read. */
 la_status la_kv4_append(const la_seqs* seqs, const la_kv4* kv, const void* k, const void* v, const int32_t* cu,
                         const int32_t* lens, const int32_t* table, void* cache, void* stream);
 

@@ -174,6 +174,7 @@ extern "C" la_status la_rope(const la_rope_shape* s, const void* q, void* q_out,
                              const int32_t* positions, const double* freqs, float amplitude, void* stream) {
   if (!s) return LA_ERR_ARG;
   if (s->B < 0 || s->L < 0 || s->Hq < 0 || s->Hk < 0 || s->B > 65535 || (s->d != 64 && s->d != 128)) return LA_ERR_SHAPE;
+  if (s->L > (1 << 26) - 4) return LA_ERR_SHAPE;    // 64 threads a token, below 2^32 in all
   if (s->rot < 16 || s->rot > s->d || s->rot % 16) return LA_ERR_SHAPE;
   if (s->interleaved != 0 && s->interleaved != 1) return LA_ERR_SHAPE;
   if (s->axes < 1 || s->axes > 3) return LA_ERR_SHAPE;

@@ -16,10 +16,18 @@ bool bad_strides(int64_t token, int64_t head, int d, bool written) {
   return token < d || token >= (int64_t(1) << 24) || head < (written ? 1 : 0) || ((token | head) & 7);
 }
 
+// The most sequences, rows and cached tokens: 64 times a tile's number, and what is read ahead of a tile (8 of
+// them), stay below 2^31.
+constexpr int kMaxTokens = 0x7ffff000;
+// The most rows of la_kv4_append and la_kv4_read: 256 threads for 16 or 32 rows, and a grid has at most
+// 2^32 - 1 threads along an axis.
+constexpr int kMaxCacheRows = (1 << 28) - 32;
+
 // Shared checks of a la_seqs; the strides of k and v only where the call has such rows.
 la_status check_seqs(const la_seqs* s) {
   if (!s) return LA_ERR_ARG;
   if (s->S < 0 || s->Tq < 0 || s->Tk < 0 || s->Hq < 1 || s->Hkv < 1 || s->Hq % s->Hkv) return LA_ERR_SHAPE;
+  if (s->S > kMaxTokens || s->Tq > kMaxTokens || s->Tk > kMaxTokens) return LA_ERR_SHAPE;
   if (s->Hq > 65535 || (s->d != 64 && s->d != 128)) return LA_ERR_SHAPE;
   if (s->causal != 0 && s->causal != 1) return LA_ERR_SHAPE;
   return LA_OK;
@@ -146,7 +154,7 @@ CachePlan cache_plan(const la_seqs& s, const la_kv4& kv, int max_q) {
   CachePlan c{};
   const int G = s.Hq / s.Hkv;
   const int64_t cap64 = (int64_t)kv.max_pages * kv.page;
-  const int cap = cap64 < 0x7fffff00 ? (int)cap64 : 0x7fffff00;
+  const int cap = cap64 < kMaxTokens ? (int)cap64 : kMaxTokens;
   c.lq_token = G >= kTokenRows ? 1 : kTokenRows / G;
   if (max_q > s.Tq) max_q = s.Tq;
   c.many = max_q > c.lq_token;
@@ -174,7 +182,7 @@ la_status check_cache_rows(const la_seqs* s, const la_kv4* kv, const void* k, co
   la_status st = check_seqs(s);
   if (st != LA_OK) return st;
   if (!kv) return LA_ERR_ARG;
-  if (bad_kv4(kv)) return LA_ERR_SHAPE;
+  if (bad_kv4(kv) || s->Tk > kMaxCacheRows) return LA_ERR_SHAPE;
   if (s->S == 0 || s->Tk == 0) return LA_OK;
   if (bad_strides(s->k_token, s->k_head, s->d, written) || bad_strides(s->v_token, s->v_head, s->d, written))
     return LA_ERR_SHAPE;

@@ -873,6 +873,7 @@ def kv4_attn(q: torch.Tensor, cache: torch.Tensor, cu_q: torch.Tensor, lens: tor
         raise ValueError(f"cache is on {cache.device}, q on {q.device}")
     o, ot, oh, lse = _outputs(q, dev, Tq, Hq, d, want_lse, out, lse_out)
     seqs = ctypes.byref(Seqs(S, Tq, 0, Hq, Hkv, d, 1 if causal else 0, qt, qh, ot, oh, 0, 0, 0, 0))
+    max_q = min(max_q, Tq)                     # a c_int32
     wp, nbytes, ws = _scratch(lib().la_kv4_ws_bytes(seqs, kv, max_q), q, dev, ws)
     _on_device(dev, "la_kv4_attn", seqs, kv, max_q, q.data_ptr(), cache.data_ptr(), cu_q.data_ptr(), lens.data_ptr(),
                table.data_ptr(), scale if scale is not None else 0.0, o.data_ptr(), _ptr(lse), wp, nbytes, _stream(q))

@@ -377,3 +377,29 @@ def test_narrow_and_wide_tables(lq, d):
                        lens, True)
     o, lse = la.kv4_attn(q, cache, cu, L, short, lq, want_lse=True)
     R.check(o, lse, want, "512 tokens")
+
+
+@pytest.mark.parametrize("lq", [1, 200])
+def test_longest_table(lq):
+    # a table of 2^31 tokens, all of its pages missing, and a length of 2^31 - 1: the sequence ends at
+    # 2^31 - 4096, every value reads as zero and every weight is one
+    cache = la.kv4_cache(1, 1, 64, 1024)
+    cache.fill_(0x22)
+    table = torch.full((2, 1 << 21), -1, dtype=torch.int32, device="cuda")
+    q = torch.randn((1 + lq, 1, 64), device="cuda").to(torch.bfloat16)
+    print(f"[kv4] 2^31 tokens, {lq} queries", flush=True)
+    o, lse = la.kv4_attn(q, cache, R.starts([1, lq]), ints([5, (1 << 31) - 1]), table, lq, want_lse=True)
+    torch.cuda.synchronize()
+    assert bool((o == 0).all())
+    seen = torch.tensor([5.0] + [2.0 ** 31 - 4096 - (lq - 1 - i) for i in range(lq)], dtype=torch.float64)
+    # a lane counts fewer than 2^24 weights, so exactly; up to 512 counts are joined, 2^-24 each, and the
+    # logarithm near 31 (21.5 in the end) is rounded by 2^-20 twice
+    assert float((lse[:, 0].double().cpu() - seen.log()).abs().max()) < 512 * 2.0 ** -24 + 4 * 2.0 ** -20
+
+
+def test_any_large_max_q():
+    cache, table, L, k, v = filled([100, 200], 2, 64, 16, 10)
+    q = torch.randn((9, 4, 64), device="cuda").to(torch.bfloat16)
+    want = la.kv4_attn(q, cache, R.starts([2, 7]), L, table, 9)
+    for most in (10, 1 << 31, 1 << 32, (1 << 63) - 1):
+        assert torch.equal(la.kv4_attn(q, cache, R.starts([2, 7]), L, table, most), want), most

@@ -105,3 +105,9 @@ def test_rope_arguments_refused():
 def test_binding_refuses_cpu_tensors():
     with pytest.raises(TypeError):
         la.rope(torch.zeros(4, 2, 64), torch.zeros(4, dtype=torch.int32), torch.zeros(32, dtype=torch.float64))
+
+
+@cpu_only
+def test_rope_sizes_past_the_limit_refused():
+    assert call(L=(1 << 26) - 3) == la.LA_ERR_SHAPE
+    assert call(L=(1 << 31) - 1) == la.LA_ERR_SHAPE

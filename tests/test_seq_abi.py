@@ -157,3 +157,18 @@ def test_kv4_page_bytes():
     with pytest.raises(TypeError):
         la.kv4_read(la.kv4_cache(1, 1, 64, 64, device="cpu"), torch.zeros(2, dtype=torch.int32),
                     torch.zeros(1, dtype=torch.int32), torch.zeros((1, 1), dtype=torch.int32), 1, 64)
+
+
+@cpu_only
+def test_sizes_past_the_limits_refused():
+    most = (1 << 31) - 4096
+    for big in (dict(Tq=most + 1), dict(Tk=most + 1), dict(S=most + 1), dict(Tq=(1 << 31) - 1)):
+        assert prompt(seqs(**big)) == la.LA_ERR_SHAPE, big
+        assert attn(seqs(**big), kv4()) == la.LA_ERR_SHAPE, big
+        assert la.lib().la_prompt_ws_bytes(ctypes.byref(seqs(**big))) == 0
+    for call in (append, read):
+        assert call(seqs(Tk=(1 << 28) - 31), kv4()) == la.LA_ERR_SHAPE, call
+    # the widest tables are of one size: a sequence ends before 2^31 tokens
+    need = [la.lib().la_kv4_ws_bytes(ctypes.byref(seqs()), ctypes.byref(kv4(page=1024, max_pages=n)), 1)
+            for n in (1 << 21, (1 << 31) - 1)]
+    assert 0 < need[0] == need[1]
