@@ -124,3 +124,35 @@ def test_a_chunk_over_context_in_4_bits_and_its_own_keys():
     # each part is rounded once more than the whole is
     assert float(((o - want).abs() / (2 * tol + 2 * R.U * (o1.double().abs() + o2.double().abs()))).max()) <= 1.0
     assert float((top.double() - lse).abs().max()) < 1e-5
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_far_strides(d):
+    # rows 32 MB apart (the largest stride), 4.4 GB in all: q, k, v and the outputs are columns of one buffer
+    T, Hq, Hkv, stride = 130, 4, 2, (1 << 24) - 8
+    buf = torch.empty((T, stride), dtype=torch.bfloat16, device="cuda")
+    at = lambda c, h: buf[:, c: c + h * d].unflatten(1, (h, d))       # noqa: E731
+    q, k, v, o, k2, v2 = (at(c, h) for c, h in ((0, Hq), (1 << 20, Hkv), (1 << 23, Hkv), ((1 << 24) - 2048, Hq),
+                                                (1 << 21, Hkv), (1 << 22, Hkv)))
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    for x in (q, k, v):
+        x.copy_(torch.randn(x.shape, generator=gen, device="cuda"))
+    cu, pos, f = R.starts([T]), torch.arange(T, dtype=torch.int32, device="cuda"), la.rope_frequencies(d)
+    near = [x.contiguous() for x in (q, k, v)]
+    assert torch.equal(la.prompt_attn(q, k, v, cu, out=o), la.prompt_attn(*near, cu))
+    assert torch.equal(o, la.prompt_attn(*near, cu))
+    assert torch.equal(la.rope(q, pos, f, out=o), la.rope(near[0], pos, f))
+    cache, lens = la.kv4_cache(9, Hkv, d, 16), torch.tensor([T], dtype=torch.int32, device="cuda")
+    table = torch.arange(9, dtype=torch.int32, device="cuda").view(1, 9)
+    la.kv4_append(cache, k, v, cu, lens, table)
+    want = la.kv4_read(cache, cu, lens, table, T, d)
+    got = la.kv4_read(cache, cu, lens, table, T, d, out=(k2, v2))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    again = torch.zeros_like(cache)
+    la.kv4_append(again, near[1], near[2], cu, lens, table)
+    read = la.kv4_read(again, cu, lens, table, T, d)
+    assert torch.equal(read[0], want[0]) and torch.equal(read[1], want[1])
+    for most in (1, T):
+        rows, c = (q[-1:], R.starts([1])) if most == 1 else (q, cu)
+        assert torch.equal(la.kv4_attn(rows, cache, c, lens, table, most, out=o[-1:] if most == 1 else o),
+                           la.kv4_attn(rows.contiguous(), cache, c, lens, table, most))
