@@ -11,8 +11,10 @@
 // a unit, less the extra, is rounded up to tiles of 64 keys, on both sides of a cut alike, so every
 // tile belongs to exactly one piece.  A cut costs a piece more, so a border no further than a 64th of a
 // share (or `extra`) from a unit's start or end is moved there, again on both sides alike; with few keys
-// to share, where a piece costs more to start than to work off, it is moved to the nearest one (256-row
-// units: 48 prompts of 1 to 300 tokens 24.4 -> 19.9 us, 4 of 500 tokens 38 -> 27).  The runs of a
+// to share, where a piece costs more to start than to work off, it is moved to the nearest one in units of
+// up to two shares (256-row units: 48 prompts of 1 to 300 tokens 24.4 -> 19.9 us, 4 of 500 tokens 38 -> 27;
+// in larger ones shares would differ by as much as themselves: 2164 queries over 3041 keys, 8 heads, 64 us
+// with it, 54 without).  The runs of a
 // causal sequence come from both ends in turn, the longest, the shortest, the second longest, ..:
 // pairs weigh the same, and where they fill the shares evenly no unit is cut at all (8192 tokens, 4
 // key heads: 512 units for 256 workgroups; in ascending order nearly every workgroup cut two, 34 MB of
@@ -38,7 +40,7 @@ struct SeqGeom {
   int causal;
   uint32_t extra;          // weight of a unit beside its keys, >= 1
   uint32_t cuts;           // 0: no unit is cut, the workgroup whose share holds its end does all of it
-  uint32_t whole;          // shares below this end where the nearest unit does
+  uint32_t whole;          // shares below this end where the nearest small unit does
   uint32_t min_share;      // more than two tiles, so that a share among a unit's keys is never empty
 };
 
@@ -117,7 +119,8 @@ __device__ __forceinline__ uint64_t line_before(const SeqGeom& g, const Seq& q, 
 struct Walk {
   uint64_t pos, end;       // the stretch still to do
   uint64_t unit0;          // where the present unit starts
-  uint32_t snap;           // borders this near a unit's start or end lie there
+  uint32_t snap;           // borders this near a unit's start or end lie there,
+  uint32_t small;          // and in units of at most this weight, those nearer than a quarter of it
   int s, kvh, part;        // sequence, key head, part of its group
   int j, b, nb;            // place of the run among the sequence's, run, runs
   Seq q;
@@ -137,6 +140,10 @@ __device__ __forceinline__ Seq load_seq_uniform(const SeqGeom& g, int s) {
 }
 
 // The part of the present unit that the stretch covers: tiles [ta, tb) of n, none if ta == tb.
+__device__ __forceinline__ uint32_t near_ends(const Walk& w, uint32_t weight) {
+  return weight <= w.small ? w.small / 4 : w.snap;
+}
+
 struct Piece {
   int keys;                // keys that the unit's last token sees
   int ta, tb, n;
@@ -151,9 +158,9 @@ __device__ __forceinline__ Piece walk_piece(const SeqGeom& g, const Walk& w, uin
   p.ta = xa <= g.extra ? 0 : (int)((xa - g.extra + 63u) >> 6);
   p.tb = p.n;
   if (w.end < *unit_end) {
-    const uint32_t xb = (uint32_t)(w.end - w.unit0);
-    if (xb <= w.snap) p.tb = 0;                         // the unit is the next workgroup's
-    else if (*unit_end - w.end > w.snap) p.tb = xb <= g.extra ? 0 : (int)((xb - g.extra + 63u) >> 6);
+    const uint32_t xb = (uint32_t)(w.end - w.unit0), near = near_ends(w, (uint32_t)p.keys + g.extra);
+    if (xb <= near) p.tb = 0;                           // the unit is the next workgroup's
+    else if (*unit_end - w.end > near) p.tb = xb <= g.extra ? 0 : (int)((xb - g.extra + 63u) >> 6);
   }
   p.ta = __builtin_amdgcn_readfirstlane(p.ta);
   p.tb = __builtin_amdgcn_readfirstlane(max(p.ta, p.tb));
@@ -208,7 +215,8 @@ __device__ __forceinline__ Walk start_walk(const SeqGeom& g, int l, int P) {
   Walk w;
   w.pos = first_lane_u64((uint64_t)(uint32_t)l * share);
   w.end = w.pos + share < total ? w.pos + share : total;
-  w.snap = !g.cuts ? ~0u : (uint32_t)(share < g.whole ? share / 2 : (share / 64 < g.extra ? share / 64 : g.extra));
+  w.snap = !g.cuts ? ~0u : (uint32_t)(share / 64 < g.extra ? share / 64 : g.extra);
+  w.small = g.cuts && share < g.whole ? 2 * (uint32_t)share : 0;
   w.s = w.kvh = w.part = w.j = w.b = w.nb = 0;
   w.unit0 = 0;
   w.q = Seq{0, 0, 0, 0};
@@ -254,9 +262,10 @@ __device__ __forceinline__ Walk start_walk(const SeqGeom& g, int l, int P) {
   w.nb = nb;
   w.q = q;
   w.unit0 = first_lane_u64(at + line_before(g, q, nb, ws, w.j));
-  const uint64_t unit_end = w.unit0 + (uint32_t)run_keys(g, q, w.b) + g.extra;
-  if (w.pos - w.unit0 <= w.snap) w.pos = w.unit0;
-  else if (unit_end - w.pos <= w.snap) walk_on<CACHE>(g, w, unit_end);
+  const uint32_t weight = (uint32_t)run_keys(g, q, w.b) + g.extra, near = near_ends(w, weight);
+  const uint64_t unit_end = w.unit0 + weight;
+  if (w.pos - w.unit0 <= near) w.pos = w.unit0;
+  else if (unit_end - w.pos <= near) walk_on<CACHE>(g, w, unit_end);
   return w;
 }
 
