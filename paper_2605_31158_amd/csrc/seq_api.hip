@@ -139,8 +139,12 @@ CacheGeom cache_geom(const la_seqs& s, const la_kv4& kv, const void* cache, cons
 // `rows` packed rows a unit, those of more by seq_attn_kernel.  The first reads the cache once for every
 // 32 rows, the second converts a tile once for 256 but takes longer to start a unit: over 6000 tokens, 4
 // key heads of 4 query heads, 8 sequences of 128 rows 37 against 55 us, 2 of 256 rows 33 against 46, 32 of
-// 128 rows 73 against 100, 32 of 256 rows 133 against 114.
+// 128 rows 73 against 100, 32 of 256 rows 133 against 114.  Where all rows over all that the table holds
+// are few products (kTokenWork query rows times keys) the first takes them whatever their length is: 539
+// rows over 986 keys 13.8 against 28.4 us, 1560 rows over 7396 keys 41 against 53, 9600 rows over
+// 6000 keys 57 against 61; 17300 rows over 3041 keys 57.5 against 54.3, 66000 rows over 1000 64 against 58.
 constexpr int kTokenRows = 192;
+constexpr double kTokenWork = 50e6;
 constexpr int kTokenPerCu = 2;
 struct CachePlan {
   int lq_token, rows;
@@ -155,8 +159,9 @@ CachePlan cache_plan(const la_seqs& s, const la_kv4& kv, int max_q) {
   const int G = s.Hq / s.Hkv;
   const int64_t cap64 = (int64_t)kv.max_pages * kv.page;
   const int cap = cap64 < kMaxTokens ? (int)cap64 : kMaxTokens;
-  c.lq_token = G >= kTokenRows ? 1 : kTokenRows / G;
   if (max_q > s.Tq) max_q = s.Tq;
+  c.lq_token = G >= kTokenRows ? 1 : kTokenRows / G;
+  if ((double)s.Tq * s.Hq * cap <= kTokenWork && max_q > c.lq_token) c.lq_token = max_q;
   c.many = max_q > c.lq_token;
   // a single sequence has all rows, so that it is one of many (or, where rows behind it are spare, may be
   // made like one); saves two launches, 9 us
