@@ -141,8 +141,8 @@ CacheGeom cache_geom(const la_seqs& s, const la_kv4& kv, const void* cache, cons
 // key heads of 4 query heads, 8 sequences of 128 rows 37 against 55 us, 2 of 256 rows 33 against 46, 32 of
 // 128 rows 73 against 100, 32 of 256 rows 133 against 114.  Where all rows over all that the table holds
 // are few products (kTokenWork query rows times keys) the first takes them whatever their length is: 539
-// rows over 986 keys 13.8 against 28.4 us, 1560 rows over 7396 keys 41 against 53, 9600 rows over
-// 6000 keys 57 against 61; 17300 rows over 3041 keys 57.5 against 54.3, 66000 rows over 1000 64 against 58.
+// rows over 986 keys 13.8 against 28.4 us, 5580 rows over 5825 keys 41 against 53, 9600 over 6000 56 against
+// 60; 17300 over 3041 57.5 against 54.3, 20200 over 3287 65 against 58.
 constexpr int kTokenRows = 192;
 constexpr double kTokenWork = 50e6;
 constexpr int kTokenPerCu = 2;
