@@ -5,8 +5,8 @@
 //
 // Bound by HBM: every value is read once and written once.  A workgroup has 4 tokens and all their
 // heads, queries and keys in one launch, so an angle is computed once for all heads: one of the
-// 4 x 64 at most per thread, in 64 bits as turns (p f / 2 pi less its whole turns, exact to 2^-30 of a
-// turn at positions of 10^9) and then sin and cos in fp32.  A lane moves 16 values of a row, the two
+// 4 x 64 at most per thread, in 64 bits as turns (p f / 2 pi less its whole turns: three roundings, 2^-24
+// of a turn at positions of 10^9) and then sin and cos in fp32.  A lane moves 16 values of a row, the two
 // halves of 8 pairs or 8 neighbouring ones, and holds their 8 cosines and sines in registers over the
 // heads; four rows are in flight per lane.  6240 tokens of 16 + 16 bf16 heads of 128 (102 MB) take 23.0 us,
 // 4.4 TB/s, 8191 tokens of 16 + 8 fp32 heads (201 MB) 47.3 us, 4.3 TB/s; a large copy reaches 5.1.  8 tokens
