@@ -357,7 +357,7 @@ la_status la_rope(const la_rope_shape* shape, const void* q, void* q_out, const 
 typedef struct la_seqs {
   int32_t S;                 /* sequences (>= 0) */
   int32_t Tq, Tk;            /* rows of q and o, and of k and v (>= 0); these and S at most 2^31 - 4096 */
-  int32_t Hq, Hkv;           /* heads: Hq a multiple of Hkv */
+  int32_t Hq, Hkv;           /* heads, at most 65535: Hq a multiple of Hkv */
   int32_t d;                 /* 64 or 128 */
   int32_t causal;            /* 0 or 1 */
   int64_t q_token, q_head;   /* strides in elements, multiples of 8: a token's >= d and < 2^24, */
@@ -406,7 +406,8 @@ typedef struct la_kv4 {
 size_t la_kv4_page_bytes(int32_t d, int32_t page);
 
 /* Enters rows of k and v into the cache.
- *   k, v  bf16 [Tk, Hkv, d] (la_seqs: S, Tk, Hkv, d and their strides are read; the rest is not).
+ *   k, v  bf16 [Tk, Hkv, d] (la_seqs: S, Tk, Hkv, d and their strides are used; Hq is 0 or a multiple of
+ *         Hkv; the rest is not looked at, here and for la_kv4_read).
  *   cu    int32 [S + 1]: rows [cu[s], cu[s + 1]) are the last tokens of sequence s, so that the last
  *         row is token lens[s] - 1.  Tokens before 0 or past the table are dropped.
  * Two rows must not go to one place (a page that two sequences share is entered by one of them).  Tk is
@@ -425,8 +426,8 @@ la_status la_kv4_read(const la_seqs* seqs, const la_kv4* kv, const void* cache, 
 size_t la_kv4_ws_bytes(const la_seqs* seqs, const la_kv4* kv, int32_t max_q);
 
 /* Attention of every sequence's queries over its cache: la_prompt_attn with the keys and values that
- * the cache stands for (k and v of la_seqs and Tk are not read).  With causal = 1 the last query sees
- * the last of lens[s] tokens.
+ * the cache stands for (the strides of k and v in la_seqs are not looked at; Tk is not used, and may be 0 or
+ * any valid number).  With causal = 1 the last query sees the last of lens[s] tokens.
  *   max_q  no sequence has more query rows; those of one that has are not written. */
 la_status la_kv4_attn(const la_seqs* seqs, const la_kv4* kv, int32_t max_q, const void* q, const void* cache,
                       const int32_t* cu_q, const int32_t* lens, const int32_t* table, float scale, void* o,

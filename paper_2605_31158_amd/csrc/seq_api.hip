@@ -23,13 +23,20 @@ constexpr int kMaxTokens = 0x7ffff000;
 // 2^32 - 1 threads along an axis.
 constexpr int kMaxCacheRows = (1 << 28) - 32;
 
-// Shared checks of a la_seqs; the strides of k and v only where the call has such rows.
-la_status check_seqs(const la_seqs* s) {
+// Fields that every call uses.  Hq is 0 where there are no queries; else it has to fit Hkv.
+la_status check_rows(const la_seqs* s) {
   if (!s) return LA_ERR_ARG;
-  if (s->S < 0 || s->Tq < 0 || s->Tk < 0 || s->Hq < 1 || s->Hkv < 1 || s->Hq % s->Hkv) return LA_ERR_SHAPE;
-  if (s->S > kMaxTokens || s->Tq > kMaxTokens || s->Tk > kMaxTokens) return LA_ERR_SHAPE;
-  if (s->Hq > 65535 || (s->d != 64 && s->d != 128)) return LA_ERR_SHAPE;
-  if (s->causal != 0 && s->causal != 1) return LA_ERR_SHAPE;
+  if (s->S < 0 || s->Tk < 0 || s->S > kMaxTokens || s->Tk > kMaxTokens) return LA_ERR_SHAPE;
+  if (s->Hkv < 1 || s->Hkv > 65535 || s->Hq < 0 || s->Hq > 65535 || s->Hq % s->Hkv) return LA_ERR_SHAPE;
+  if (s->d != 64 && s->d != 128) return LA_ERR_SHAPE;
+  return LA_OK;
+}
+
+// Those of the calls that have queries; the strides of q, k and v only where the call has such rows.
+la_status check_seqs(const la_seqs* s) {
+  const la_status st = check_rows(s);
+  if (st != LA_OK) return st;
+  if (s->Hq < 1 || s->Tq < 0 || s->Tq > kMaxTokens || (s->causal != 0 && s->causal != 1)) return LA_ERR_SHAPE;
   return LA_OK;
 }
 
@@ -184,7 +191,7 @@ CachePlan cache_plan(const la_seqs& s, const la_kv4& kv, int max_q) {
 
 la_status check_cache_rows(const la_seqs* s, const la_kv4* kv, const void* k, const void* v, const int32_t* cu,
                            const int32_t* lens, const int32_t* table, const void* cache, bool written) {
-  la_status st = check_seqs(s);
+  const la_status st = check_rows(s);
   if (st != LA_OK) return st;
   if (!kv) return LA_ERR_ARG;
   if (bad_kv4(kv) || s->Tk > kMaxCacheRows) return LA_ERR_SHAPE;
