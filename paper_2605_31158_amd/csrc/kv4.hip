@@ -31,10 +31,11 @@ struct KvRows {
 // Where the tokens of a workgroup lie: slot[i] = page << 16 | place for token t0 + i, or -1 where the
 // token belongs to no sequence, -2 where its place does not exist (a position below zero or past the
 // table, a page number out of range).  The search for a token's sequence goes through at most kCuLds
-// of the starts in LDS and then through those between two of them.
+// of the starts in LDS and then through those between two of them.  (S may come near 2^31: no sum of two
+// places among the starts is formed.)
 template <int TOKENS>
 __device__ void find_slots(const KvRows& r, const CacheGeom& cg, int t0, int64_t* slot, int32_t* cu) {
-  const int step = (r.S + 1 + kCuLds - 1) / kCuLds, n = (r.S + step) / step;     // starts 0, step, 2 step, ..
+  const int step = (r.S + 1 + kCuLds - 1) / kCuLds, n = r.S / step + 1;     // starts 0, step, 2 step, ..
   for (int i = threadIdx.x; i < n; i += kKvThreads) cu[i] = r.cu[i * step];
   __syncthreads();
   if (threadIdx.x < TOKENS) {
@@ -46,11 +47,15 @@ __device__ void find_slots(const KvRows& r, const CacheGeom& cg, int t0, int64_t
       if (cu[mid] <= t) lo = mid;
       else hi = mid;
     }
-    int s = lo * step, e = min(r.S + 1, s + step);
-    while (e - s > 1) {
-      const int mid = (s + e) >> 1;
-      if (r.cu[mid] <= t) s = mid;
-      else e = mid;
+    int s = lo * step, left = min(r.S + 1 - s, step);      // it is among starts s, .., s + left - 1
+    while (left > 1) {
+      const int half = left >> 1;
+      if (r.cu[s + half] <= t) {
+        s += half;
+        left -= half;
+      } else {
+        left = half;
+      }
     }
     int64_t x = -1;
     if (t < r.T && s < r.S && r.cu[s] <= t && t < r.cu[s + 1]) {
