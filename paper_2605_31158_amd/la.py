@@ -738,6 +738,13 @@ def _on_device(dev: int, fn: str, *args):
             _call(fn, *args)
 
 
+def _seqs(S, Tq, Tk, Hq, Hkv, *rest):
+    """A la_seqs by reference; ctypes would drop what passes 32 bits."""
+    if max(S, Tq, Tk, Hq, Hkv) > 0x7fffffff:
+        raise ValueError("2^31 or more sequences, tokens or heads")
+    return ctypes.byref(Seqs(S, Tq, Tk, Hq, Hkv, *rest))
+
+
 def _outputs(q, dev, T, Hq, d, want_lse, out, lse_out):
     """(o, its token and head stride, lse or None)."""
     if out is None:
@@ -786,7 +793,7 @@ def prompt_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.T
     _check_ints("cu_q", cu_q, dev, (S + 1,))
     _check_ints("cu_k", cu_k, dev, (S + 1,))
     o, ot, oh, lse = _outputs(q, dev, Tq, Hq, d, want_lse, out, lse_out)
-    seqs = ctypes.byref(Seqs(S, Tq, Tk, Hq, Hkv, d, 1 if causal else 0, qt, qh, ot, oh, kt, kh, vt, vh))
+    seqs = _seqs(S, Tq, Tk, Hq, Hkv, d, 1 if causal else 0, qt, qh, ot, oh, kt, kh, vt, vh)
     wp, nbytes, ws = _scratch(lib().la_prompt_ws_bytes(seqs), q, dev, ws)
     _on_device(dev, "la_prompt_attn", seqs, q.data_ptr(), k.data_ptr(), v.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(),
                scale if scale is not None else 0.0, o.data_ptr(), _ptr(lse), wp, nbytes, _stream(q))
@@ -816,6 +823,8 @@ def _check_cache(cache, lens, table, cu, d):
         raise ValueError("table must be an int32 [S, max_pages] tensor")
     dev = cache.get_device()
     S, most = table.shape
+    if most > 0x7fffffff:
+        raise ValueError("2^31 or more pages to a sequence")
     _check_ints("table", table, dev, (S, most))
     _check_ints("lens", lens, dev, (S,))
     _check_ints("cu", cu, dev, (S + 1,))
@@ -833,7 +842,7 @@ def kv4_append(cache: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: torch.
     Hkv, kv, S = _check_cache(cache, lens, table, cu, d)
     if cache.get_device() != dev or Hkv != H:
         raise ValueError(f"cache of {Hkv} heads on {cache.device}, k of {H} on {k.device}")
-    _on_device(dev, "la_kv4_append", ctypes.byref(Seqs(S, 0, T, H, H, d, 0, 0, 0, 0, 0, kt, kh, vt, vh)), kv, k.data_ptr(),
+    _on_device(dev, "la_kv4_append", _seqs(S, 0, T, H, H, d, 0, 0, 0, 0, 0, kt, kh, vt, vh), kv, k.data_ptr(),
                v.data_ptr(), cu.data_ptr(), lens.data_ptr(), table.data_ptr(), cache.data_ptr(), _stream(k))
 
 
@@ -851,7 +860,7 @@ def kv4_read(cache: torch.Tensor, cu: torch.Tensor, lens: torch.Tensor, table: t
         k, v = out
         _, _, _, kt, kh = _rows("k", k, dev, H, d, tokens)
         _, _, _, vt, vh = _rows("v", v, dev, H, d, tokens)
-    _on_device(dev, "la_kv4_read", ctypes.byref(Seqs(S, 0, tokens, H, H, d, 0, 0, 0, 0, 0, kt, kh, vt, vh)), kv,
+    _on_device(dev, "la_kv4_read", _seqs(S, 0, tokens, H, H, d, 0, 0, 0, 0, 0, kt, kh, vt, vh), kv,
                cache.data_ptr(), cu.data_ptr(), lens.data_ptr(), table.data_ptr(), k.data_ptr(), v.data_ptr(),
                _stream(cache))
     return k, v
@@ -872,8 +881,8 @@ def kv4_attn(q: torch.Tensor, cache: torch.Tensor, cu_q: torch.Tensor, lens: tor
     if cache.get_device() != dev:
         raise ValueError(f"cache is on {cache.device}, q on {q.device}")
     o, ot, oh, lse = _outputs(q, dev, Tq, Hq, d, want_lse, out, lse_out)
-    seqs = ctypes.byref(Seqs(S, Tq, 0, Hq, Hkv, d, 1 if causal else 0, qt, qh, ot, oh, 0, 0, 0, 0))
-    max_q = min(max_q, Tq)                     # a c_int32
+    seqs = _seqs(S, Tq, 0, Hq, Hkv, d, 1 if causal else 0, qt, qh, ot, oh, 0, 0, 0, 0)
+    max_q = min(max(max_q, -1), Tq)            # a c_int32; below 0 it is refused
     wp, nbytes, ws = _scratch(lib().la_kv4_ws_bytes(seqs, kv, max_q), q, dev, ws)
     _on_device(dev, "la_kv4_attn", seqs, kv, max_q, q.data_ptr(), cache.data_ptr(), cu_q.data_ptr(), lens.data_ptr(),
                table.data_ptr(), scale if scale is not None else 0.0, o.data_ptr(), _ptr(lse), wp, nbytes, _stream(q))
