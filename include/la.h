@@ -332,8 +332,8 @@ typedef struct la_rope_shape {
   int64_t k_batch, k_token, k_head, ko_batch, ko_token, ko_head;
 } la_rope_shape;
 
-/*   q, k       rows of d contiguous values with the strides above, 16-byte aligned
- *   q_out, k_out  the same; each may be its input (with its strides)
+/*   q, k       rows of d contiguous values with the strides above (0: a broadcast), 16-byte aligned
+ *   q_out, k_out  the same, rows that lie apart; each may be its input (with its strides)
  *   positions  int32 [axes, L] (device);  freqs  double [rot / 2] (device): radians per position.
  * One kernel launch.  LA_ERR_SHAPE for shapes and strides that do not fit, LA_ERR_ARG for pointers, a
  * bad dtype and an amplitude that is not finite. */

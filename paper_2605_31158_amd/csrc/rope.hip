@@ -161,8 +161,10 @@ void launch(const RopeArgs& a, bool neighbours, int B, hipStream_t st) {
   else hipLaunchKernelGGL((rope_kernel<D, BF16, false>), grid, dim3(kRopeThreads), 0, st, a);
 }
 
-bool bad_rows(int64_t batch, int64_t token, int64_t head, bool written) {
-  return batch < 0 || token < (written ? 1 : 0) || head < (written ? 1 : 0) || ((batch | token | head) & 7);
+// Rows that are written lie apart: no stride of 0 (of the batch, where there is one).
+bool bad_rows(int64_t batch, int64_t token, int64_t head, int B, bool written) {
+  return batch < (written && B > 1 ? 1 : 0) || token < (written ? 1 : 0) || head < (written ? 1 : 0) ||
+         ((batch | token | head) & 7);
 }
 
 }  // namespace
@@ -188,12 +190,14 @@ extern "C" la_status la_rope(const la_rope_shape* s, const void* q, void* q_out,
   if (isnan(amplitude) || isinf(amplitude)) return LA_ERR_ARG;
   if (s->B == 0 || s->L == 0 || (s->Hq == 0 && s->Hk == 0)) return LA_OK;
   if (s->Hq > 0) {
-    if (bad_rows(s->q_batch, s->q_token, s->q_head, false) || bad_rows(s->qo_batch, s->qo_token, s->qo_head, true))
+    if (bad_rows(s->q_batch, s->q_token, s->q_head, s->B, false) ||
+        bad_rows(s->qo_batch, s->qo_token, s->qo_head, s->B, true))
       return LA_ERR_SHAPE;
     if (!q || !q_out || ((uintptr_t)q & 15u) || ((uintptr_t)q_out & 15u)) return LA_ERR_ARG;
   }
   if (s->Hk > 0) {
-    if (bad_rows(s->k_batch, s->k_token, s->k_head, false) || bad_rows(s->ko_batch, s->ko_token, s->ko_head, true))
+    if (bad_rows(s->k_batch, s->k_token, s->k_head, s->B, false) ||
+        bad_rows(s->ko_batch, s->ko_token, s->ko_head, s->B, true))
       return LA_ERR_SHAPE;
     if (!k || !k_out || ((uintptr_t)k & 15u) || ((uintptr_t)k_out & 15u)) return LA_ERR_ARG;
   }
