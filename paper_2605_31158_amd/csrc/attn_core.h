@@ -54,7 +54,9 @@ __device__ inline uint32_t pack_bf16x2(float lo, float hi) {
 // Workgroup barrier for waves with asynchronous tile loads in flight that they do not wait for
 // here (an LDS release fence would wait for them: they write LDS).  The empty asm statements keep
 // the compiler from moving memory accesses across the barrier; every LDS read of the wave has been
-// consumed by then, and no wave writes LDS except by tile loads.
+// consumed by then.  The barrier waits for nothing else: a wave whose tile other waves read behind it
+// has waited for that tile itself, by vmcnt where it came by asynchronous loads and by lgkmcnt(0) where
+// it was stored (the tiles of a 4-bit cache).
 __device__ __forceinline__ void phase_barrier() {
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_barrier();

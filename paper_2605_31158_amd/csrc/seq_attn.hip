@@ -188,7 +188,11 @@ struct CacheTiles {
     write(dst);
     load();
   }
-  __device__ __forceinline__ void wait() { __builtin_amdgcn_s_waitcnt(0xC07F); }   // lgkmcnt(0): the LDS writes
+  // the tile stored last is in LDS
+  __device__ __forceinline__ void wait() {
+    asm volatile("" ::: "memory");                      // the compiler moves no store behind the wait
+    __builtin_amdgcn_s_waitcnt(0xC07F);                 // lgkmcnt(0)
+  }
 };
 
 // Starts a piece: O and l zero, the maximum at -inf, the wave's Q rows and how far each sees.

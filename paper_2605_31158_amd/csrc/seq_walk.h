@@ -139,11 +139,12 @@ __device__ __forceinline__ Seq load_seq_uniform(const SeqGeom& g, int s) {
   return q;
 }
 
-// The part of the present unit that the stretch covers: tiles [ta, tb) of n, none if ta == tb.
+// How near a border has to lie to an end of a unit of this weight to be moved there.
 __device__ __forceinline__ uint32_t near_ends(const Walk& w, uint32_t weight) {
   return weight <= w.small ? w.small / 4 : w.snap;
 }
 
+// The part of the present unit that the stretch covers: tiles [ta, tb) of n, none if ta == tb.
 struct Piece {
   int keys;                // keys that the unit's last token sees
   int ta, tb, n;
