@@ -315,8 +315,9 @@ la_status la_untile_o_3d(const la_grid3d* grid, const void* o_tiled, const float
  * Pair j of a head's first `rot` values is turned by positions[axis of j][token] * freqs[j] radians,
  *   (a, b) -> amplitude (a cos - b sin, b cos + a sin);
  * the pairs are (j, j + rot / 2), or with interleaved = 1 (2 j, 2 j + 1); the values from `rot` on are
- * copied.  Angles are computed in 64 bits, so far positions keep their precision; a negative position
- * turns back, and turning by -p undoes (and is the gradient of) turning by p at amplitude 1.
+ * copied.  Angles are computed and reduced in 64 bits, so far positions keep their precision; their sines
+ * and cosines and the products are fp32.  A negative position turns back, and turning by -p undoes (and
+ * is the gradient of) turning by p at amplitude 1.
  * -------------------------------------------------------------------------- */
 typedef struct la_rope_shape {
   int32_t B, L;              /* sequences of L tokens (<= 2^26 - 4) that share their positions (packed tokens:
@@ -375,17 +376,18 @@ size_t la_prompt_ws_bytes(const la_seqs* seqs);
  *   scale       <= 0 selects 1/sqrt(d).
  *   o           bf16, strides o_token and o_head;  lse  float [Tq, Hq] or NULL: natural-log sum of
  *               exp(logits).
- * Softmax in fp32, products in bf16 with fp32 accumulation.  Kernel launches only (one or two): a caller
- * may capture the call; calls that may overlap need a ws each. */
+ * Softmax in fp32, products in bf16 with fp32 accumulation (the weights are rounded to bf16 for the one
+ * with v).  Kernel launches only (one or two): a caller may capture the call; calls that may overlap need
+ * a ws each. */
 la_status la_prompt_attn(const la_seqs* seqs, const void* q, const void* k, const void* v,
                          const int32_t* cu_q, const int32_t* cu_k, float scale, void* o, float* lse,
                          void* ws, size_t ws_bytes, void* stream);
 
 /* A cache of keys and values in 4 bits, in pages that the sequences share.
  *   Values are e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6, and their negatives) times a power of two that the 32
- *   values of a block of a row share: 4.25 bits per value.  The power is the smallest under which the
- *   block's largest value is rounded by no more than half a step (held to 2^-125 .. 2^125); values are
- *   rounded to nearest, ties to the even code.  A block with a value that is not finite reads as NaN.
+ *   values of a block of a row share: 4.25 bits per value.  The power is the smallest 2^e with the block's
+ *   largest magnitude below 7 2^e, so that it is rounded by less than half a step (e is held to -125 .. 125);
+ *   values are rounded to nearest, ties to the even code.  A block with a value that is not finite reads as NaN.
  *   cache  uint8 [n_pages, Hkv, la_kv4_page_bytes(d, page)], 16-byte aligned: per page and key head
  *            K codes [page][d / 2]              two values to a byte, the lower 4 bits first;
  *            K scales [d / 32][page]            2^(byte - 127), 255 = NaN;
@@ -428,7 +430,9 @@ size_t la_kv4_ws_bytes(const la_seqs* seqs, const la_kv4* kv, int32_t max_q);
 /* Attention of every sequence's queries over its cache: la_prompt_attn with the keys and values that
  * the cache stands for (the strides of k and v in la_seqs are not looked at; Tk is not used, and may be 0 or
  * any valid number).  With causal = 1 the last query sees the last of lens[s] tokens.
- *   max_q  no sequence has more query rows; those of one that has are not written. */
+ *   max_q  no sequence has more query rows; those of one that has are not written.
+ * Whether work is split, and which kernel takes it, goes by what the table can hold, so a table no wider than
+ * the sequences need makes small calls faster. */
 la_status la_kv4_attn(const la_seqs* seqs, const la_kv4* kv, int32_t max_q, const void* q, const void* cache,
                       const int32_t* cu_q, const int32_t* lens, const int32_t* table, float scale, void* o,
                       float* lse, void* ws, size_t ws_bytes, void* stream);

@@ -2,8 +2,8 @@
 // (layout: kv4.h).
 //
 // Per 32 values of a row, x -> code(x / 2^e) with the smallest power of two under which the largest
-// value is rounded by no more than half a step: amax < 7 2^e, since 6 is the largest code and 7 lies
-// half a step above it.  In bf16 bits that is one addition: with 32 added to the magnitude's bits a
+// value is rounded by less than half a step: amax < 7 2^e, since 6 is the largest code and 7 lies half a
+// step above it.  In bf16 bits that is one addition: with 32 added to the magnitude's bits a
 // mantissa of 1.75 or more carries into the exponent.  e is held to [-125, 125], so that every value
 // read back is a normal, finite bf16.  A block with a value that is not finite gets the scale byte
 // 255 and reads as NaN.  Rounding is to nearest, ties to the even code, by the conversion

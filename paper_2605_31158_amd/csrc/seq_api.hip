@@ -45,10 +45,14 @@ constexpr int kRows = 256;              // packed rows of a workgroup (seq_attn.
 constexpr uint32_t kRowsExtra = 512, kTokenExtra = 384, kRowsShare = 512, kTokenShare = 256;
 constexpr int kMaxWorkgroups = 256;
 
-// Where no sequence can have more keys than this, units are not cut: nothing to join, so no workspace and
-// no second launch, which saves a caller 3 us.  On the GPU one token over 256 keys takes 6.4 us (cut 9.5),
-// over 512 8.1 (9.7), over 1000 11.0 (10.1), over 2000 16.2 (10.5); 32 sequences of 1000 keys 14.1 (13.9),
-// of 2000 21.4 (16.3); a prompt of 256 tokens 16.0 (17.4), of 512 21.0 (22.4).
+// Where no sequence can have more keys than this (a cache's: than its table holds, since the lengths are on
+// the GPU), units are not cut: nothing to join, so no workspace and no second launch.  kTokenWhole is set for
+// eager calls, whose host side takes 11 us without the join's launch and 14.3 with it: one token over 256, 512,
+// 1000 keys takes 11.0, 11.0, 11.1 us a call uncut and 14.4, 14.4, 14.3 cut, 32 sequences of 500 to 1000 keys 14.0
+// and 14.9.  On the GPU alone (a captured call) the two meet near 800 keys: 256 keys 6.4 us (cut 9.3), 512 8.0 (9.7),
+// 768 9.3 (9.8), 896 10.3 (9.9), 1000 11.0 (10.1), 2000 16.2 (10.5); 32 sequences of 256 to 512 keys 10.5 (12.5), of
+// 500 to 1000 15.0 (14.7), of 2000 21.4 (16.3): a captured call over 800 to 1024 keys pays up to 0.9 us.
+// kRowsWhole, on the GPU: a prompt of 256 tokens 16.0 us (cut 17.4), of 512 21.0 (22.4).
 constexpr int kTokenWhole = 1024, kRowsWhole = 512;
 
 SeqGeom seq_geom(const la_seqs& s, int rows, int kcap, uint32_t extra, uint32_t whole, uint32_t share, int uncut) {
@@ -149,7 +153,8 @@ CacheGeom cache_geom(const la_seqs& s, const la_kv4& kv, const void* cache, cons
 // 128 rows 73 against 100, 32 of 256 rows 133 against 114.  Where all rows over all that the table holds
 // are few products (kTokenWork query rows times keys) the first takes them whatever their length is: 539
 // rows over 986 keys 13.8 against 28.4 us, 5580 rows over 5825 keys 41 against 53, 9600 over 6000 56 against
-// 60; 17300 over 3041 57.5 against 54.3, 20200 over 3287 65 against 58.
+// 60; 17300 over 3041 57.5 against 54.3, 20200 over 3287 65 against 58.  The lengths are on the GPU, so a table
+// that is wider than the sequences are long leaves their rows with the second kernel.
 constexpr int kTokenRows = 192;
 constexpr double kTokenWork = 50e6;
 constexpr int kTokenPerCu = 2;

@@ -21,6 +21,12 @@
 // 32 sequences of 1000 to 16000 tokens (32 query heads over 8, d 128: 190 MB) take 49 us, 4 of them
 // before the first codes arrive and 4.5 for the join: 4.7 TB/s while it streams, a large copy's rate being
 // 5.1; with most of it in the last-level cache 41 us, 5.8 TB/s.  One sequence of 1000 tokens takes 11 us.
+// 8 sequences of 5 queries (32 query heads over 4: 40 packed rows, two units of up to 32) over 700 to 9000 tokens
+// take 24 us at d 128.  The 32-row instance has all 256 vector registers there and spills two, written before its
+// tile loop and read behind it.
+//
+// The weights 2^(s - m) are rounded to bf16 for the product with V, as in seq_attn.hip; m, l (of the weights
+// before they are rounded) and O are fp32.
 #include <math.h>
 
 #include <type_traits>

@@ -541,7 +541,8 @@ def grid3d_positions(g: Grid3D, frames=None, device="cuda"):
 
 
 class Rope(NamedTuple):
-    """How a path turns its queries and keys (see rope): frequencies, pairs of each axis, and positions."""
+    """How a path turns its queries and keys (see rope): frequencies, pairs of each axis, and positions.
+    Pairs are neighbours (2 j, 2 j + 1) unless interleaved is False, which is rope()'s own default."""
     freqs: torch.Tensor
     sections: Tuple[int, ...]
     q_positions: torch.Tensor
@@ -873,8 +874,10 @@ def kv4_attn(q: torch.Tensor, cache: torch.Tensor, cu_q: torch.Tensor, lens: tor
     """Attention of packed queries over a 4-bit cache -> o bf16 [Tq, Hq, d] (and lse fp32 [Tq, Hq]).
 
     q [Tq, Hq, d] in bf16 with free strides; sequence s has the rows [cu_q[s], cu_q[s + 1]), at most max_q
-    of them (1: the next token of every sequence), and lens[s] tokens in the cache (see kv4_append).
-    Causal: the last query of a sequence sees the last token, its queries being the last tokens."""
+    of them (1: the next token of every sequence), and lens[s] tokens in the cache (see kv4_append).  Rows of
+    a sequence that has more than max_q, and rows behind the last sequence, are not written (a new output
+    holds anything there).  Causal: the last query of a sequence sees the last token, its queries being the
+    last tokens."""
     Tq, Hq, d, qt, qh = _rows("q", q)
     dev = q.get_device()
     Hkv, kv, S = _check_cache(cache, lens, table, cu_q, d)
