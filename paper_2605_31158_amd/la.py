@@ -817,7 +817,7 @@ def _check_cache(cache, lens, table, cu, d):
     if cache.dtype is not torch.uint8 or cache.dim() != 3 or not cache.is_contiguous():
         raise TypeError("cache must be a contiguous uint8 [n_pages, Hkv, page bytes] tensor")
     n, Hkv, nbytes = cache.shape
-    page, rest = divmod(nbytes, d + d // 16)
+    page, rest = divmod(nbytes, d + d // 16) if d > 0 else (0, 0)
     if rest or page < 16 or page & (page - 1):
         raise ValueError(f"a cache of {nbytes} bytes a page is none for heads of {d}")
     if not isinstance(table, torch.Tensor) or table.dim() != 2:

@@ -1,4 +1,5 @@
-"""Numbers past 31 bits that a tensor's shape can hold, which the C structs cannot: refused, not wrapped."""
+"""Numbers past 31 bits that a tensor's shape can hold, which the C structs cannot: refused, not wrapped; and
+heads of no values."""
 import pytest
 import torch
 
@@ -51,3 +52,20 @@ def test_negative_max_q():
     for most in (-1, -FAR + 5, -FAR):
         with pytest.raises(la.LaError):
             la.kv4_attn(q, cache, cu, lens, table, most)
+
+
+def test_heads_of_no_values():
+    q = torch.zeros((3, 1, 0), dtype=torch.bfloat16, device="cuda")
+    cache = la.kv4_cache(1, 1, 64, 16)
+    cu, lens, table = (torch.zeros(s, dtype=torch.int32, device="cuda") for s in ((2,), (1,), (1, 1)))
+    with pytest.raises(ValueError):
+        la.kv4_attn(q, cache, cu, lens, table, 1)
+    with pytest.raises(ValueError):
+        la.kv4_append(cache, q, q, cu, lens, table)
+    for d in (0, -64, -1):
+        with pytest.raises(ValueError):
+            la.kv4_read(cache, cu, lens, table, 3, d)
+    with pytest.raises(la.LaError):
+        la.prompt_attn(q, q, q, cu)
+    with pytest.raises(la.LaError):
+        la.rope(q, cu.new_zeros(3), la.rope_frequencies(64))
