@@ -383,6 +383,57 @@ la_status la_prompt_attn(const la_seqs* seqs, const void* q, const void* k, cons
                          const int32_t* cu_q, const int32_t* cu_k, float scale, void* o, float* lse,
                          void* ws, size_t ws_bytes, void* stream);
 
+/* A learned bias by relative position, added to the logits (scale q.k) of la_prompt_attn: query i stands at place
+ * i + lk - lq among its sequence's keys, and key n at distance n - that place,
+ *   bias[h] = weight[bucket[clamp(distance, lo, hi) - lo]][h].
+ * What the buckets are is the caller's: one for every distance, or ever wider ones.  A bucket outside
+ * [0, buckets) has no bias (and takes no gradient).  A weight of -inf hides its distances; +inf and NaN are not
+ * supported. */
+typedef struct la_rel_bias {
+  int32_t lo, hi;            /* lo <= hi <= lo + 512, both within +-2^20 */
+  int32_t buckets;           /* rows of the weights: 1 to 2^20 */
+  int32_t dtype;             /* la_dtype of the weights and of their gradient */
+} la_rel_bias;
+
+/* la_prompt_attn with a bias.
+ *   bucket  int32 [hi - lo + 1], weight [buckets, Hq] (device).  `bias` NULL: la_prompt_attn.
+ * The scratch is la_prompt_bias_ws_bytes(seqs, bias). */
+size_t la_prompt_bias_ws_bytes(const la_seqs* seqs, const la_rel_bias* bias);
+la_status la_prompt_attn_bias(const la_seqs* seqs, const la_rel_bias* bias, const void* q, const void* k, const void* v,
+                              const int32_t* cu_q, const int32_t* cu_k, const int32_t* bucket, const void* weight,
+                              float scale, void* o, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* Gradients of la_prompt_attn and la_prompt_attn_bias: with x the logits, P = exp(x - lse),
+ * delta = do.o - dlse and dS = P (do.v - delta) over the pairs that see each other,
+ *   dq = scale dS k,   dk = scale dS^T q,   dv = P^T do   (dk and dv summed over the query heads of a key head),
+ *   dweight[b][h] = the sum of dS over the pairs of bucket b and head h, over all sequences.
+ * The probabilities are recomputed from q, k and lse; they and dS are rounded to bf16 for their products, sums
+ * are fp32 (dweight's 64 bits between workgroups) and in a fixed order: results repeat bit for bit on one device. */
+typedef struct la_prompt_grads {
+  int64_t do_token, do_head;   /* strides in elements, as in la_seqs: those of do may be a broadcast's (head 0) */
+  int64_t dq_token, dq_head;
+  int64_t dk_token, dk_head;
+  int64_t dv_token, dv_head;
+} la_prompt_grads;
+
+/* Bytes of scratch that la_prompt_attn_bwd needs; 0 for invalid arguments.  bias NULL: none. */
+size_t la_prompt_bwd_ws_bytes(const la_seqs* seqs, const la_rel_bias* bias);
+
+/*   dout    bf16 [Tq, Hq, d] (do_token, do_head): the gradient of o.
+ *   q, k, v, cu_q, cu_k, scale, and bucket and weight (with a bias): as in the forward call.
+ *   o, lse  what the forward call left (o with o_token and o_head; lse float [Tq, Hq]).
+ *   dlse    float [Tq, Hq] or NULL: the gradient of lse.
+ *   dq [Tq, Hq, d], dk, dv [Tk, Hkv, d]  bf16, not overlapping each other or an input.  Rows that no sequence
+ *           covers are not written; keys that no query sees get zeros.
+ *   dweight [buckets, Hq] in the weights' type, with a bias: written whole.
+ * A query that sees no key (lse = -inf) has no gradients and gives none.  Kernel launches only: a caller may
+ * capture the call; calls that may overlap need a ws each. */
+la_status la_prompt_attn_bwd(const la_seqs* seqs, const la_prompt_grads* grads, const la_rel_bias* bias,
+                             const void* dout, const void* q, const void* k, const void* v, const void* o,
+                             const float* lse, const float* dlse, const int32_t* cu_q, const int32_t* cu_k,
+                             const int32_t* bucket, const void* weight, float scale, void* dq, void* dk, void* dv,
+                             void* dweight, void* ws, size_t ws_bytes, void* stream);
+
 /* A cache of keys and values in 4 bits, in pages that the sequences share.
  *   Values are e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6, and their negatives) times a power of two that the 32
  *   values of a block of a row share: 4.25 bits per value.  The power is the smallest 2^e with the block's

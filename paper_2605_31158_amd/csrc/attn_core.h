@@ -286,16 +286,19 @@ __device__ __forceinline__ float row_max(float x) {
 // 0.15 % larger, 0.0023393 instead of 0.0023358 at 720P.  A lane tests its own values first, at half
 // the limit where it holds a quarter of the keys; the sums of the halves are taken where that fails
 // (in every tile they cost 2 % of the call).
-template <int D>
+// SHIFT: logits are S*scale + shift[qt] (a relative bias that is one number for the tile and row), which
+// moves the maximum that they are formed against and costs nothing a logit.
+template <int D, bool SHIFT = false>
 __device__ __forceinline__ void softmax_tile(typename Mma<D>::Acc (*sacc)[Mma<D>::QT], bf16x8 (*pb)[Mma<D>::QT],
                                              typename Mma<D>::Acc (*oacc)[Mma<D>::QT], float* m_run, float* l_run,
-                                             float scale_log2) {
+                                             float scale_log2, const float* shift = nullptr) {
   using X = Mma<D>;
+  auto against = [&](float m, int qt) { return SHIFT ? m - shift[qt] : m; };
   float rs[X::QT];
   bool over = false;
 #pragma unroll
   for (int qt = 0; qt < X::QT; ++qt) {
-    rs[qt] = softmax_exp<D>(sacc, pb, qt, m_run[qt], scale_log2);
+    rs[qt] = softmax_exp<D>(sacc, pb, qt, against(m_run[qt], qt), scale_log2);
     over = over || !(rs[qt] <= (X::NG == 4 ? 128.f : 256.f));
   }
   if (__builtin_expect(__any(over), 0)) {
@@ -316,7 +319,8 @@ __device__ __forceinline__ void softmax_tile(typename Mma<D>::Acc (*sacc)[Mma<D>
         for (int kt = 0; kt < KT / X::MR; ++kt)
 #pragma unroll
           for (int i = 0; i < X::AR; ++i) mx = fmaxf(mx, sacc[kt][qt][i]);
-        const float mt = row_max<D>(mx) * scale_log2;
+        float mt = row_max<D>(mx) * scale_log2;
+        if constexpr (SHIFT) mt += shift[qt];
         if (mt > m_run[qt]) {
           const float alpha = __builtin_amdgcn_exp2f(m_run[qt] - mt);   // 0 while m_run is -inf
           m_run[qt] = mt;
@@ -324,12 +328,44 @@ __device__ __forceinline__ void softmax_tile(typename Mma<D>::Acc (*sacc)[Mma<D>
 #pragma unroll
           for (int dt = 0; dt < D / X::MR; ++dt) oacc[dt][qt] *= alpha;
         }
-        rs[qt] = softmax_exp<D>(sacc, pb, qt, m_run[qt] == -INFINITY ? 0.f : m_run[qt], scale_log2);
+        rs[qt] = softmax_exp<D>(sacc, pb, qt, against(m_run[qt] == -INFINITY ? 0.f : m_run[qt], qt), scale_log2);
       }
     }
   }
 #pragma unroll
   for (int qt = 0; qt < X::QT; ++qt) l_run[qt] += rs[qt];
+}
+
+// The wave's row c of query column qt as bf16, 16 bytes (8 values) at a time: word i of lane group lg
+// belongs to column out_col(i, lg).  The accumulators give a lane 4 neighbouring values; it exchanges
+// every second quad with the next lane group's.  (Stored 8 bytes at a time, 16 rows of 32 bytes to an
+// instruction, a unit's 64 KB take 3 us more to issue, a third of what starting and ending it costs.)
+template <int D>
+__device__ __forceinline__ int out_col(int i, int lg) {
+  return Mma<D>::MR == 16 ? 32 * i + 16 * (lg & 1) + 8 * (lg >> 1) : 16 * i + 8 * lg;
+}
+template <int D>
+__device__ __forceinline__ void out_words(const typename Mma<D>::Acc (*oacc)[Mma<D>::QT], int qt, float inv, u32x4* y) {
+  using X = Mma<D>;
+  // quad n of the lane: values n MR .. (MR = 16), or 8 n .. (32), plus 4 lg
+  auto quad = [&](int n) {
+    const int e = 4 * n;
+    const typename X::Acc a = oacc[e / X::AR][qt] * inv;
+    return u32x2{pack_bf16x2(a[e % X::AR], a[e % X::AR + 1]), pack_bf16x2(a[e % X::AR + 2], a[e % X::AR + 3])};
+  };
+#pragma unroll
+  for (int i = 0; i < D / (8 * X::NG); ++i) {
+    const u32x2 a = quad(2 * i), b = quad(2 * i + 1);
+    u32x2 lo, hi;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const auto s = X::MR == 16 ? __builtin_amdgcn_permlane16_swap(a[w], b[w], false, false)
+                                 : __builtin_amdgcn_permlane32_swap(a[w], b[w], false, false);
+      lo[w] = (uint32_t)s[0];
+      hi[w] = (uint32_t)s[1];
+    }
+    y[i] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+  }
 }
 
 }  // namespace

@@ -87,7 +87,8 @@ hipError_t launch_latent_mse(const void* a, const void* b, int64_t n, int bf16, 
 struct SeqGeom;
 struct SeqIo;
 struct CacheGeom;
-hipError_t launch_prompt_attn(const SeqGeom& g, const SeqIo& io, int d, int P, hipStream_t st);
+struct SeqBias;
+hipError_t launch_prompt_attn(const SeqGeom& g, const SeqIo& io, const SeqBias* bias, int d, int P, hipStream_t st);
 // Attention over a 4-bit cache: sequences of many query rows, and of few.
 hipError_t launch_cache_tokens(const SeqGeom& g, const SeqIo& io, const CacheGeom& cg, int d, int rows, int P,
                                hipStream_t st);
@@ -97,6 +98,10 @@ hipError_t launch_kv4_append(const la_seqs& s, const CacheGeom& cg, const void* 
 hipError_t launch_kv4_read(const la_seqs& s, const CacheGeom& cg, const int32_t* cu, const int32_t* lens, void* k,
                            void* v, hipStream_t st);
 hipError_t launch_cache_rows(const SeqGeom& g, const SeqIo& io, const CacheGeom& cg, int d, int P, hipStream_t st);
+
+// Gradients of the attention over packed sequences (grad_walk.h).
+struct GradCall;
+hipError_t launch_prompt_bwd(const GradCall& c, int d, hipStream_t st);
 
 // CUs of the current device, 0 when HIP cannot say.  A constant of the device, asked for once per
 // device: four launches of a step need it.

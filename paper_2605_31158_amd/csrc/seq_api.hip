@@ -2,6 +2,7 @@
 // the kernels take, workspaces and launches.  Nothing here allocates device memory.
 #include <math.h>
 
+#include "grad_walk.h"
 #include "kv4.h"
 #include "la_internal.h"
 #include "seq_walk.h"
@@ -55,7 +56,8 @@ constexpr int kMaxWorkgroups = 256;
 // kRowsWhole, on the GPU: a prompt of 256 tokens 16.0 us (cut 17.4), of 512 21.0 (22.4).
 constexpr int kTokenWhole = 1024, kRowsWhole = 512;
 
-SeqGeom seq_geom(const la_seqs& s, int rows, int kcap, uint32_t extra, uint32_t whole, uint32_t share, int uncut) {
+SeqGeom seq_geom(const la_seqs& s, int rows, int kcap, uint32_t extra, uint32_t whole, uint32_t share, int uncut,
+                 int heads = kRows) {
   SeqGeom g{};
   g.S = s.S;
   g.Tq = s.Tq;
@@ -66,6 +68,7 @@ SeqGeom seq_geom(const la_seqs& s, int rows, int kcap, uint32_t extra, uint32_t 
   g.Hkv = s.Hkv;
   g.G = s.Hq / s.Hkv;
   g.GH = g.G < rows ? g.G : rows;
+  if (g.GH > heads) g.GH = heads;
   g.GS = ceil_div(g.G, g.GH);
   g.gh_magic = (65536 + g.GH - 1) / g.GH;
   g.TB = rows / g.GH;
@@ -134,6 +137,100 @@ SeqIo seq_io(const la_seqs& s, const void* q, void* o, float* lse, float scale) 
 int device_workgroups(int per_cu) {
   const int p = device_cu_count() / 8 * 8;
   return (p < 8 ? 8 : (p > kMaxWorkgroups ? kMaxWorkgroups : p)) * per_cu;
+}
+
+// The gradients' units, and where nothing is cut: inner axes of at most kGradWhole rows.
+constexpr uint32_t kGradExtra = 256, kGradShare = 512;
+constexpr int kGradWhole = 512, kGradPerCu = 2;
+
+GradGeom grad_geom(const la_seqs& s, bool keys, bool bias) {
+  GradGeom g{};
+  g.S = s.S;
+  g.Tq = s.Tq;
+  g.Tk = s.Tk;
+  g.Hq = s.Hq;
+  g.Hkv = s.Hkv;
+  g.G = s.Hq / s.Hkv;
+  // the pairs' distances are added up head by head, so that a unit of a call with a bias has one
+  g.GH = keys || bias ? 1 : (g.G < kGradRows ? g.G : kGradRows);
+  g.GS = keys ? 1 : ceil_div(g.G, g.GH);
+  g.gh_magic = (65536 + g.GH - 1) / g.GH;
+  g.TB = kGradRows / g.GH;
+  g.NH = s.Hkv * g.GS;
+  g.causal = s.causal;
+  g.extra = kGradExtra;
+  g.whole = 2 * kGradExtra;
+  g.min_share = kGradShare;
+  g.cuts = (keys ? (double)s.Tq * g.G : (double)s.Tk) > kGradWhole;
+  return g;
+}
+
+int grad_workgroups(const GradGeom& g, bool keys) {
+  const int rows = keys ? g.Tk : g.Tq;
+  const double units = (double)g.NH * ((double)rows / g.TB + (g.S < rows ? g.S : rows));
+  const double inner = keys ? (double)g.G * (g.Tq + 64.0 * (g.S < g.Tq ? g.S : g.Tq)) : (double)g.Tk;
+  const double shares = ceil(units * (inner + g.extra) / g.min_share);
+  const int most = kMaxWorkgroups * kGradPerCu, want = shares < most ? (int)shares : most;
+  return (want + 7) / 8 * 8;
+}
+
+// A workgroup of 256 threads takes the statistics of 16 tokens by 16 heads, and one more lays out each head's
+// bias; a grid has at most 2^32 - 1 threads along an axis.
+bool bad_grad_rows(const la_seqs& s) {
+  return (int64_t)ceil_div(s.Tq, 16) * ceil_div(s.Hq, 16) + s.Hq >= 1 << 24;
+}
+
+bool bad_bias(const la_rel_bias* b) {
+  return b->lo > b->hi || b->lo < -(1 << 20) || b->hi > (1 << 20) || b->hi - b->lo >= kBiasMost || b->buckets < 1 ||
+         b->buckets > (1 << 20);
+}
+int bias_pitch(const la_rel_bias* b) { return b->hi - b->lo + 1 + 2 * kBiasPad; }
+
+struct GradLayout {
+  float2* stat;
+  float *table, *dist;
+  uint64_t* line;
+  int4* cut;
+  float* part;
+  size_t bytes;
+};
+
+// The kernels run one after the other and share the scratch of their pieces.
+GradLayout grad_layout(const la_seqs& s, const la_rel_bias* bias, void* ws) {
+  GradLayout w{};
+  char* p = (char*)ws;
+  size_t at = 0;
+  auto take = [&](size_t n) {
+    char* r = p ? p + at : nullptr;
+    at += align256(n);
+    return r;
+  };
+  const GradGeom r = grad_geom(s, false, bias != nullptr), k = grad_geom(s, true, false);
+  const size_t rp = grad_workgroups(r, false), kp = grad_workgroups(k, true);
+  w.stat = (float2*)take(((size_t)s.Hq * s.Tq + 1) * sizeof(float2));     // read two at a time
+  if (bias) {
+    w.table = (float*)take((size_t)s.Hq * bias_pitch(bias) * sizeof(float));
+    w.dist = (float*)take((rp + r.NH) * bias_pitch(bias) * sizeof(float));
+    w.line = (uint64_t*)take(2 * sizeof(uint64_t));
+  }
+  const size_t rcut = r.cuts ? 2 * rp : 0, kcut = k.cuts ? 2 * kp : 0, most = rcut > 2 * kcut ? rcut : 2 * kcut;
+  w.cut = (int4*)take((rcut > kcut ? rcut : kcut) * sizeof(int4));
+  w.part = (float*)take(most * kGradRows * s.d * sizeof(float));
+  w.bytes = at;
+  return w;
+}
+
+la_status check_bias(const la_rel_bias* bias, const int32_t* bucket, const void* weight) {
+  if (bad_bias(bias)) return LA_ERR_SHAPE;
+  if (bias->dtype != LA_DTYPE_F32 && bias->dtype != LA_DTYPE_BF16) return LA_ERR_ARG;
+  const uintptr_t word = bias->dtype == LA_DTYPE_F32 ? 3u : 1u;
+  if (!bucket || !weight || ((uintptr_t)bucket & 3u) || ((uintptr_t)weight & word)) return LA_ERR_ARG;
+  return LA_OK;
+}
+
+// The units of a call over whole prompts; with a bias those of at most kBiasHeads heads, whose tables are in LDS.
+SeqGeom prompt_geom(const la_seqs& s, const la_rel_bias* bias) {
+  return seq_geom(s, kRows, s.Tk, kRowsExtra, 2 * kRowsExtra, kRowsShare, kRowsWhole, bias ? kBiasHeads : kRows);
 }
 
 bool bad_kv4(const la_kv4* kv) {
@@ -213,18 +310,30 @@ la_status check_cache_rows(const la_seqs* s, const la_kv4* kv, const void* k, co
 
 extern "C" {
 
-size_t la_prompt_ws_bytes(const la_seqs* seqs) {
-  if (check_seqs(seqs) != LA_OK || seqs->S == 0 || seqs->Tq == 0) return 0;
-  const SeqGeom g = seq_geom(*seqs, kRows, seqs->Tk, kRowsExtra, 2 * kRowsExtra, kRowsShare, kRowsWhole);
+size_t la_prompt_ws_bytes(const la_seqs* seqs) { return la_prompt_bias_ws_bytes(seqs, nullptr); }
+
+size_t la_prompt_bias_ws_bytes(const la_seqs* seqs, const la_rel_bias* bias) {
+  if (check_seqs(seqs) != LA_OK || (bias && bad_bias(bias)) || seqs->S == 0 || seqs->Tq == 0) return 0;
+  const SeqGeom g = prompt_geom(*seqs, bias);
   return part_layout(g, workgroups(g, seqs->Tk, kMaxWorkgroups), kRows, seqs->d, nullptr).bytes;
 }
 
 la_status la_prompt_attn(const la_seqs* seqs, const void* q, const void* k, const void* v, const int32_t* cu_q,
                          const int32_t* cu_k, float scale, void* o, float* lse, void* ws, size_t ws_bytes,
                          void* stream) {
+  return la_prompt_attn_bias(seqs, nullptr, q, k, v, cu_q, cu_k, nullptr, nullptr, scale, o, lse, ws, ws_bytes, stream);
+}
+
+la_status la_prompt_attn_bias(const la_seqs* seqs, const la_rel_bias* bias, const void* q, const void* k, const void* v,
+                              const int32_t* cu_q, const int32_t* cu_k, const int32_t* bucket, const void* weight,
+                              float scale, void* o, float* lse, void* ws, size_t ws_bytes, void* stream) {
   la_status st = check_seqs(seqs);
   if (st != LA_OK) return st;
   if (isnan(scale) || isinf(scale)) return LA_ERR_ARG;
+  if (bias) {
+    if (bad_bias(bias)) return LA_ERR_SHAPE;
+    if (bias->dtype != LA_DTYPE_F32 && bias->dtype != LA_DTYPE_BF16) return LA_ERR_ARG;
+  }
   if (seqs->S == 0 || seqs->Tq == 0) return LA_OK;
   if (bad_strides(seqs->q_token, seqs->q_head, seqs->d, false) || bad_strides(seqs->o_token, seqs->o_head, seqs->d, true))
     return LA_ERR_SHAPE;
@@ -234,7 +343,13 @@ la_status la_prompt_attn(const la_seqs* seqs, const void* q, const void* k, cons
   if (!q || !o || !cu_q || !cu_k || (seqs->Tk > 0 && (!k || !v))) return LA_ERR_ARG;
   if (misaligned(q) || misaligned(o) || misaligned(k) || misaligned(v)) return LA_ERR_ARG;
   if (((uintptr_t)cu_q | (uintptr_t)cu_k | (uintptr_t)lse) & 3u) return LA_ERR_ARG;
-  SeqGeom g = seq_geom(*seqs, kRows, seqs->Tk, kRowsExtra, 2 * kRowsExtra, kRowsShare, kRowsWhole);
+  SeqBias b{};
+  if (bias) {
+    st = check_bias(bias, bucket, weight);
+    if (st != LA_OK) return st;
+    b = SeqBias{bucket, weight, bias->dtype == LA_DTYPE_BF16, bias->buckets, bias->lo, bias->hi};
+  }
+  SeqGeom g = prompt_geom(*seqs, bias);
   g.cu_q = cu_q;
   g.ks = cu_k;
   const int most = workgroups(g, seqs->Tk, kMaxWorkgroups);
@@ -245,7 +360,8 @@ la_status la_prompt_attn(const la_seqs* seqs, const void* q, const void* k, cons
   io.v = (const uint16_t*)v;
   set_parts(&io, w);
   const int have = device_workgroups(1);
-  const hipError_t e = launch_prompt_attn(g, io, seqs->d, most < have ? most : have, (hipStream_t)stream);
+  const hipError_t e = launch_prompt_attn(g, io, bias ? &b : nullptr, seqs->d, most < have ? most : have,
+                                          (hipStream_t)stream);
   return e == hipSuccess ? LA_OK : LA_ERR_HIP;
 }
 
@@ -309,6 +425,101 @@ la_status la_kv4_attn(const la_seqs* seqs, const la_kv4* kv, int32_t max_q, cons
     const int have = device_workgroups(1);
     e = launch_cache_rows(c.many_rows, io, cg, seqs->d, c.p_many < have ? c.p_many : have, (hipStream_t)stream);
   }
+  return e == hipSuccess ? LA_OK : LA_ERR_HIP;
+}
+
+size_t la_prompt_bwd_ws_bytes(const la_seqs* seqs, const la_rel_bias* bias) {
+  if (check_seqs(seqs) != LA_OK || bad_grad_rows(*seqs) || (bias && bad_bias(bias)) || seqs->S == 0) return 0;
+  return grad_layout(*seqs, bias, nullptr).bytes;
+}
+
+la_status la_prompt_attn_bwd(const la_seqs* seqs, const la_prompt_grads* grads, const la_rel_bias* bias,
+                             const void* dout, const void* q, const void* k, const void* v, const void* o,
+                             const float* lse, const float* dlse, const int32_t* cu_q, const int32_t* cu_k,
+                             const int32_t* bucket, const void* weight, float scale, void* dq, void* dk, void* dv,
+                             void* dweight, void* ws, size_t ws_bytes, void* stream) {
+  la_status st = check_seqs(seqs);
+  if (st != LA_OK) return st;
+  if (!grads || isnan(scale) || isinf(scale)) return LA_ERR_ARG;
+  if (bad_grad_rows(*seqs)) return LA_ERR_SHAPE;
+  if (bias) {
+    st = check_bias(bias, bucket, weight);
+    if (st != LA_OK) return st;
+    if (!dweight || ((uintptr_t)dweight & (bias->dtype == LA_DTYPE_F32 ? 3u : 1u))) return LA_ERR_ARG;
+  }
+  const la_seqs& s = *seqs;
+  const bool rows = s.S > 0 && s.Tq > 0, keys = s.S > 0 && s.Tk > 0;
+  if (rows && (bad_strides(s.q_token, s.q_head, s.d, false) || bad_strides(s.o_token, s.o_head, s.d, false) ||
+               bad_strides(grads->do_token, grads->do_head, s.d, false) ||
+               bad_strides(grads->dq_token, grads->dq_head, s.d, true)))
+    return LA_ERR_SHAPE;
+  if (keys && (bad_strides(s.k_token, s.k_head, s.d, false) || bad_strides(s.v_token, s.v_head, s.d, false) ||
+               bad_strides(grads->dk_token, grads->dk_head, s.d, true) ||
+               bad_strides(grads->dv_token, grads->dv_head, s.d, true)))
+    return LA_ERR_SHAPE;
+  if (!rows && !keys && !bias) return LA_OK;
+  if (rows && (!dout || !q || !o || !lse || !dq)) return LA_ERR_ARG;
+  if (keys && (!k || !v || !dk || !dv)) return LA_ERR_ARG;
+  if ((rows || keys) && (!cu_q || !cu_k)) return LA_ERR_ARG;
+  if (misaligned(dout) || misaligned(q) || misaligned(k) || misaligned(v) || misaligned(o) || misaligned(dq) ||
+      misaligned(dk) || misaligned(dv))
+    return LA_ERR_ARG;
+  if (((uintptr_t)cu_q | (uintptr_t)cu_k | (uintptr_t)lse | (uintptr_t)dlse) & 3u) return LA_ERR_ARG;
+  GradLayout w{};
+  if (rows || keys) {
+    w = grad_layout(s, bias, ws);
+    if (w.bytes > 0 && (!ws || ws_bytes < w.bytes || ((uintptr_t)ws & 255u))) return LA_ERR_WORKSPACE;
+  }
+  GradCall c{};
+  c.rows = rows;
+  c.keys = keys;
+  c.has_bias = bias != nullptr;
+  c.rows_g = grad_geom(s, false, bias != nullptr);
+  c.keys_g = grad_geom(s, true, false);
+  c.rows_g.cu_q = c.keys_g.cu_q = cu_q;
+  c.rows_g.cu_k = c.keys_g.cu_k = cu_k;
+  const int have = device_workgroups(kGradPerCu);
+  c.rows_p = grad_workgroups(c.rows_g, false);
+  c.keys_p = grad_workgroups(c.keys_g, true);
+  if (c.rows_p > have) c.rows_p = have;
+  if (c.keys_p > have) c.keys_p = have;
+  GradIo io{};
+  io.q = (const uint16_t*)q;
+  io.k = (const uint16_t*)k;
+  io.v = (const uint16_t*)v;
+  io.dout = (const uint16_t*)dout;
+  io.q_tok = s.q_token; io.q_head = s.q_head;
+  io.k_tok = s.k_token; io.k_head = s.k_head;
+  io.v_tok = s.v_token; io.v_head = s.v_head;
+  io.do_tok = grads->do_token; io.do_head = grads->do_head;
+  io.stat = w.stat;
+  io.part = w.part;
+  io.cut = w.cut;
+  io.scale = scale > 0.0f ? scale : 1.0f / sqrtf((float)s.d);
+  io.scale_log2 = io.scale * 1.4426950408889634f;
+  if (bias) {
+    io.table = w.table;
+    io.bias_lo = bias->lo;
+    io.bias_hi = bias->hi;
+    io.bias_pitch = bias_pitch(bias);
+    io.dist = w.dist;
+    io.line = w.line;
+    c.bias = SeqBias{bucket, weight, bias->dtype == LA_DTYPE_BF16, bias->buckets, bias->lo, bias->hi};
+    c.dweight = dweight;
+  }
+  c.rows_io = c.keys_io = io;
+  c.rows_io.out0 = (uint16_t*)dq;
+  c.rows_io.out0_tok = grads->dq_token; c.rows_io.out0_head = grads->dq_head;
+  c.keys_io.out0 = (uint16_t*)dk;
+  c.keys_io.out0_tok = grads->dk_token; c.keys_io.out0_head = grads->dk_head;
+  c.keys_io.out1 = (uint16_t*)dv;
+  c.keys_io.out1_tok = grads->dv_token; c.keys_io.out1_head = grads->dv_head;
+  c.Tq = s.Tq;
+  c.o = (const uint16_t*)o;
+  c.o_tok = s.o_token; c.o_head = s.o_head;
+  c.lse = lse;
+  c.dlse = dlse;
+  const hipError_t e = launch_prompt_bwd(c, s.d, (hipStream_t)stream);
   return e == hipSuccess ? LA_OK : LA_ERR_HIP;
 }
 

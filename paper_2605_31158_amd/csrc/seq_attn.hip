@@ -233,38 +233,6 @@ __device__ __forceinline__ void start_rows(PieceState<D>& st, WaveCtx& w, const 
   st.seen = __builtin_amdgcn_readfirstlane(seen);
 }
 
-// The wave's row c of query column qt as bf16, 16 bytes (8 values) at a time: word i of lane group lg
-// belongs to column out_col(i, lg).  The accumulators give a lane 4 neighbouring values; it exchanges
-// every second quad with the next lane group's.  (Stored 8 bytes at a time, 16 rows of 32 bytes to an
-// instruction, a unit's 64 KB take 3 us more to issue, a third of what starting and ending it costs.)
-template <int D>
-__device__ __forceinline__ int out_col(int i, int lg) {
-  return Mma<D>::MR == 16 ? 32 * i + 16 * (lg & 1) + 8 * (lg >> 1) : 16 * i + 8 * lg;
-}
-template <int D>
-__device__ __forceinline__ void out_words(const typename Mma<D>::Acc (*oacc)[Mma<D>::QT], int qt, float inv, u32x4* y) {
-  using X = Mma<D>;
-  // quad n of the lane: values n MR .. (MR = 16), or 8 n .. (32), plus 4 lg
-  auto quad = [&](int n) {
-    const int e = 4 * n;
-    const typename X::Acc a = oacc[e / X::AR][qt] * inv;
-    return u32x2{pack_bf16x2(a[e % X::AR], a[e % X::AR + 1]), pack_bf16x2(a[e % X::AR + 2], a[e % X::AR + 3])};
-  };
-#pragma unroll
-  for (int i = 0; i < D / (8 * X::NG); ++i) {
-    const u32x2 a = quad(2 * i), b = quad(2 * i + 1);
-    u32x2 lo, hi;
-#pragma unroll
-    for (int w = 0; w < 2; ++w) {
-      const auto s = X::MR == 16 ? __builtin_amdgcn_permlane16_swap(a[w], b[w], false, false)
-                                 : __builtin_amdgcn_permlane32_swap(a[w], b[w], false, false);
-      lo[w] = (uint32_t)s[0];
-      hi[w] = (uint32_t)s[1];
-    }
-    y[i] = u32x4{lo[0], lo[1], hi[0], hi[1]};
-  }
-}
-
 // Ends a piece: bf16 rows (and lse) where the piece is the whole unit, else the partial.
 template <int D>
 __device__ __forceinline__ void end_rows(const PieceState<D>& st, const SeqGeom& g, const SeqIo& io, const Walk& wk,
@@ -312,7 +280,84 @@ struct SeqArgs {
   SeqGeom g;
   SeqIo io;
   CacheGeom cg;
+  SeqBias bias;
 };
+
+// A wave's relative bias: a table by distance in LDS for each head of the unit, from distance lo - kBiasPad on, so
+// that the tiles that need it (near) read it without a clamp; where all distances of a tile are beyond one end the
+// bias is one number a row, which the softmax takes as a shift.
+template <int D>
+struct WaveBias {
+  using X = Mma<D>;
+  int at[X::QT];                     // index of key 0's distance in the table, of this lane's first key
+  float lo[X::QT], hi[X::QT];        // beyond the ends
+  int first, last;                   // the first and last place of the wave's rows among the keys
+};
+
+template <int D>
+__device__ __forceinline__ void start_bias(WaveBias<D>& wb, float (*table)[kBiasPitch], const SeqArgs& a, const Walk& wk,
+                                           int r_off, int c, int lg) {
+  using X = Mma<D>;
+  const int off = wk.q.lk - wk.q.lq;
+  int first = 0x7fffffff, last = -0x7fffffff;
+#pragma unroll
+  for (int qt = 0; qt < X::QT; ++qt) {
+    const Row row = unit_row(a.g, wk, r_off + X::MR * qt + c);
+    if (row.ok) {
+      first = min(first, row.token + off);
+      last = max(last, row.token + off);
+    }
+  }
+#pragma unroll
+  for (int m = 1; m < X::MR; m <<= 1) {
+    first = min(first, __shfl_xor(first, m));
+    last = max(last, __shfl_xor(last, m));
+  }
+  wb.first = __builtin_amdgcn_readfirstlane(first);
+  wb.last = __builtin_amdgcn_readfirstlane(last);
+  const int n = a.bias.hi - a.bias.lo;
+#pragma unroll
+  for (int qt = 0; qt < X::QT; ++qt) {
+    const Row row = unit_row(a.g, wk, r_off + X::MR * qt + c);
+    const int head = row.ok ? row.head - unit_head0(a.g, wk) : 0;
+    // rows that do not exist read the places of one that does
+    const int place = row.ok ? row.token + off : wb.first;
+    wb.at[qt] = head * kBiasPitch + 4 * lg + kBiasPad - a.bias.lo - place;
+    wb.lo[qt] = table[head][kBiasPad];
+    wb.hi[qt] = table[head][kBiasPad + n];
+  }
+}
+
+// The unit's tables, by all threads.
+__device__ __forceinline__ void fill_bias(float (*table)[kBiasPitch], const SeqArgs& a, const Walk& wk) {
+  const int heads = unit_heads(a.g, wk), head0 = unit_head0(a.g, wk), n = a.bias.hi - a.bias.lo + 1 + 2 * kBiasPad;
+  for (int h = 0; h < heads; ++h)
+    for (int i = threadIdx.x; i < n; i += kThreads) table[h][i] = bias_log2(a.bias, i - kBiasPad, a.g.Hq, head0 + h);
+}
+
+// The bias of a tile: added to the scaled logits (whose scale is 1 then), or the shift of each row.
+template <int D>
+__device__ __forceinline__ float add_bias(const WaveBias<D>& wb, const float* table, typename Mma<D>::Acc (*sacc)[Mma<D>::QT],
+                                          float* shift, int key0, int lo, int hi, float scale_log2) {
+  using X = Mma<D>;
+  const bool left = key0 + 63 - wb.first <= lo, right = key0 - wb.last >= hi;
+  if (left || right) {
+#pragma unroll
+    for (int qt = 0; qt < X::QT; ++qt) shift[qt] = left ? wb.lo[qt] : wb.hi[qt];
+    return scale_log2;
+  }
+#pragma unroll
+  for (int qt = 0; qt < X::QT; ++qt) {
+    shift[qt] = 0.f;
+    const float* at = table + (wb.at[qt] + key0);
+#pragma unroll
+    for (int kt = 0; kt < KT / X::MR; ++kt)
+#pragma unroll
+      for (int i = 0; i < X::AR; ++i)
+        sacc[kt][qt][i] = __builtin_fmaf(sacc[kt][qt][i], scale_log2, at[X::MR * kt + X::acc_row(i)]);
+  }
+  return 1.0f;
+}
 
 // The arguments of seq_attn_kernel, read anew: 50 scalar registers that a piece needs at its ends must
 // not be held over its loop, which needs nearly all there are.
@@ -323,11 +368,12 @@ __device__ __forceinline__ SeqArgs fresh_args() {
   return *(const SeqArgs*)p;
 }
 
-template <int D, bool CACHE>
+template <int D, bool CACHE, bool BIAS>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void seq_attn_kernel(SeqArgs) {
   using T = Tile<D>;
   using X = Mma<D>;
   __shared__ __attribute__((aligned(1024))) unsigned char ring[6 * T::BYTES];
+  __shared__ float table[BIAS ? kBiasHeads : 1][BIAS ? kBiasPitch : 1];
 
   // workgroups of one XCD take consecutive stretches: they walk the same head's K and V
   const int P = gridDim.x;
@@ -357,6 +403,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   w.g4 = 4 * lg;
   w.scale_log2 = scale_log2;
   PieceState<D> st;
+  typename std::conditional<BIAS, WaveBias<D>, int>::type wb;
+  int bias_lo = 0, bias_hi = 0;
+  if constexpr (BIAS) {
+    const SeqArgs a = fresh_args();
+    bias_lo = a.bias.lo;
+    bias_hi = a.bias.hi;
+  }
 
   // Iteration i of a piece's tiles (phases as in attn.hip): tile i lies in stage i % 3.  Group 0
   // loads K(i + 2) and group 1 V(i + 1) at the end of their V phases, and both wait at the end of
@@ -386,6 +439,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
           const SeqArgs a = fresh_args();
           src.prime(a.io, wk, wk.kvh, pc.ta, pc.tb, IS_G1 ? s0 + VOFF : s0, IS_G1 ? nullptr : s1);
           start_rows<D>(st, w, a.g, a.io, wk, r_off, c, lg);
+          if constexpr (BIAS) {
+            // the waves read no table of the piece before any more: its last iteration ended with a barrier
+            fill_bias(table, a, wk);
+            __syncthreads();
+            start_bias<D>(wb, table, a, wk, r_off, c, lg);
+          }
           const int open = a.g.causal ? max(0, wk.q.lk - wk.q.lq + wk.b * a.g.TB + 1) : wk.q.lk;
           key_open = min(open, wk.q.lk) - 63;
         }
@@ -399,8 +458,15 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         auto v_phase = [&](int i) {
           const int key0 = 64 * (pc.ta + i);
           if (i >= 0 && i < N && key0 < st.seen) {
-            if (__builtin_expect(key0 >= key_open, 0)) mask_tile<D>(st.sacc, key0, 0, w);
-            softmax_tile<D>(st.sacc, st.pb, st.oacc, st.m_run, st.l_run, w.scale_log2);
+            if constexpr (BIAS) {
+              float shift[X::QT];
+              const float scale = add_bias<D>(wb, &table[0][0], st.sacc, shift, key0, bias_lo, bias_hi, w.scale_log2);
+              if (__builtin_expect(key0 >= key_open, 0)) mask_tile<D>(st.sacc, key0, 0, w);
+              softmax_tile<D, true>(st.sacc, st.pb, st.oacc, st.m_run, st.l_run, scale, shift);
+            } else {
+              if (__builtin_expect(key0 >= key_open, 0)) mask_tile<D>(st.sacc, key0, 0, w);
+              softmax_tile<D>(st.sacc, st.pb, st.oacc, st.m_run, st.l_run, w.scale_log2);
+            }
           }
         };
         auto iteration = [&](int i, unsigned char* sc, unsigned char* sp, unsigned char* sn) {
@@ -553,15 +619,19 @@ void launch_merge(const SeqGeom& g, const SeqIo& io, int P, hipStream_t st) {
 
 }  // namespace
 
-template <int D, bool CACHE>
-static hipError_t launch_rows(const SeqGeom& g, const SeqIo& io, const CacheGeom& cg, int P, hipStream_t st) {
-  hipLaunchKernelGGL((seq_attn_kernel<D, CACHE>), dim3(P), dim3(kThreads), 0, st, SeqArgs{g, io, cg});
+template <int D, bool CACHE, bool BIAS = false>
+static hipError_t launch_rows(const SeqGeom& g, const SeqIo& io, const CacheGeom& cg, int P, hipStream_t st,
+                              const SeqBias& bias = SeqBias{}) {
+  hipLaunchKernelGGL((seq_attn_kernel<D, CACHE, BIAS>), dim3(P), dim3(kThreads), 0, st, SeqArgs{g, io, cg, bias});
   if (g.cuts) launch_merge<D, QR>(g, io, P, st);
   return hipGetLastError();
 }
 
-hipError_t launch_prompt_attn(const SeqGeom& g, const SeqIo& io, int d, int P, hipStream_t st) {
+hipError_t launch_prompt_attn(const SeqGeom& g, const SeqIo& io, const SeqBias* bias, int d, int P, hipStream_t st) {
   const CacheGeom none{};
+  if (bias)
+    return d == 128 ? launch_rows<128, false, true>(g, io, none, P, st, *bias)
+                    : launch_rows<64, false, true>(g, io, none, P, st, *bias);
   return d == 128 ? launch_rows<128, false>(g, io, none, P, st) : launch_rows<64, false>(g, io, none, P, st);
 }
 

@@ -1,0 +1,900 @@
+// Gradients of the attention over packed sequences on gfx950, with recomputed probabilities.
+//
+// With x = scale q.k (+ bias), P = exp(x - lse), delta = do.o (- dlse), dP = do.v:
+//   dS = P (dP - delta);  dV = P^T dO;  dK = scale dS^T Q;  dQ = scale dS K
+// and the gradient of a bucket of the relative bias is the sum of dS over its pairs.
+//
+// Two kernels walk the pairs, so that no sum needs atomics and results repeat bit for bit: key_grad_kernel
+// holds 128 keys of a key head and goes over the queries that see them (four products, dK and dV in
+// registers), row_grad_kernel holds 128 packed query rows and goes over their keys (three, dQ in registers).
+#include <math.h>
+
+#include <type_traits>
+
+#include "attn_core.h"
+#include "grad_walk.h"
+
+namespace la {
+namespace {
+
+constexpr int kGradThreads = 256;        // four waves, each with 32 of a unit's 128 rows
+
+// A tile of ROWS rows of D bf16 in LDS that is read both ways: as operands along d (16 bytes of MR rows) and
+// transposed, as operands along the rows (chunks of 2 MR bytes of 4 rows a lane group).  The 16-byte slots of
+// row r are permuted by an exclusive or with swz(r), for which both spread over all 64 banks.
+template <int D, int ROWS>
+struct GradTile {
+  static constexpr int STRIDE = D * 2;
+  static constexpr int SLOTS = STRIDE / 16;
+  static constexpr int BYTES = ROWS * STRIDE;
+  static constexpr int PER = BYTES / 4096;             // 1 KiB loads of each of the four waves
+  __device__ static constexpr int swz(int r) {
+    return D == 128 ? ((r & 7) << 1) | ((r >> 3) & 1) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+  }
+};
+
+// Global byte offset of lane `lane` of the i-th load of wave lw, less the immediate 1024 i (see slot_offset).
+template <int D, int ROWS>
+__device__ __forceinline__ uint32_t grad_slot(int lw, int i, int lane, uint32_t stride) {
+  using T = GradTile<D, ROWS>;
+  const int slot = 64 * i + lane;
+  const int row = lw * (ROWS / 4) + slot / T::SLOTS;
+  return (uint32_t)row * stride + (uint32_t)(((slot % T::SLOTS) ^ T::swz(row)) * 16 - 1024 * i);
+}
+
+// Asynchronous load of a wave's quarter of a tile; rows past nrec bytes come as zeros.
+template <int D, int ROWS>
+__device__ __forceinline__ void grad_issue(unsigned char* dst, const uint16_t* base, uint64_t off, uint32_t nrec,
+                                           const uint32_t* lane_off) {
+  // attn_core.h's, of as many bytes: 128 or 64 values a row stand for four or two loads
+  issue_tile<GradTile<D, ROWS>::PER == 4 ? 128 : 64>(dst, base, off, nrec, lane_off);
+}
+
+// Asynchronous load of the statistics of up to 64 rows, by one wave: 16 bytes a lane, of which those behind nrec come
+// as zeros, as does the second KiB.
+constexpr int kStatBytes = 2048;
+__device__ __forceinline__ void stat_issue(unsigned char* dst, const float2* base, uint64_t off, uint32_t nrec, int lane) {
+  const uint32_t lane_off[2] = {16u * lane, 16u * lane};
+  issue_tile<64>(dst, (const uint16_t*)base, off, nrec, lane_off);
+}
+
+// acc[t][c] = A B: A the first NT MR rows of a tile, B columns of the other operand in registers.
+template <int D, int NT>
+__device__ __forceinline__ void rows_product(const unsigned char* __restrict__ tile, const bf16x8 (*b)[Mma<D>::QT],
+                                             typename Mma<D>::Acc (*acc)[Mma<D>::QT], int base) {
+  using X = Mma<D>;
+  constexpr int NO = NT * (D / X::KC);
+  constexpr int AHEAD = NO < 4 ? NO : 4;
+  bf16x8 a[NO];
+#pragma unroll
+  for (int i = 0; i < NO; ++i)
+    a[i] = *(const bf16x8*)(tile + (base ^ (16 * X::NG * (i / NT))) + (i % NT) * X::MR * (2 * D));
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int c = 0; c < X::QT; ++c)
+#pragma unroll
+      for (int i = 0; i < X::AR; ++i) acc[t][c][i] = 0.f;
+#pragma unroll
+  for (int i = 0; i < NO; ++i)
+#pragma unroll
+    for (int c = 0; c < X::QT; ++c) acc[i % NT][c] = X::mma(a[i], b[i / NT][c], acc[i % NT][c]);
+  __builtin_amdgcn_sched_group_barrier(kSgDsRead, AHEAD, 0);
+#pragma unroll
+  for (int i = 0; i < NO - AHEAD; ++i) {
+    __builtin_amdgcn_sched_group_barrier(kSgMfma, X::QT, 0);
+    __builtin_amdgcn_sched_group_barrier(kSgDsRead, 1, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(kSgMfma, X::QT * AHEAD, 0);
+}
+
+// The same with B in LDS too, rows of `other` at bbase (32 of them, column c MR of the product).
+template <int D, int NT>
+__device__ __forceinline__ void tiles_product(const unsigned char* __restrict__ tile,
+                                              const unsigned char* __restrict__ other,
+                                              typename Mma<D>::Acc (*acc)[Mma<D>::QT], int base, int bbase) {
+  using X = Mma<D>;
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int c = 0; c < X::QT; ++c)
+#pragma unroll
+      for (int i = 0; i < X::AR; ++i) acc[t][c][i] = 0.f;
+#pragma unroll
+  for (int ks = 0; ks < D / X::KC; ++ks) {
+    bf16x8 a[NT], b[X::QT];
+#pragma unroll
+    for (int c = 0; c < X::QT; ++c)
+      b[c] = *(const bf16x8*)(other + (bbase ^ (16 * X::NG * ks)) + c * X::MR * (2 * D));
+#pragma unroll
+    for (int t = 0; t < NT; ++t) a[t] = *(const bf16x8*)(tile + (base ^ (16 * X::NG * ks)) + t * X::MR * (2 * D));
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int c = 0; c < X::QT; ++c) acc[t][c] = X::mma(a[t], b[c], acc[t][c]);
+  }
+}
+
+// acc[dt][c] += A^T B over the rows of a tile: NS steps of KC rows, B columns [step][c] in registers, whose
+// slot e of lane group g is row 4 g + e (e < 4) or KC / 2 + 4 g + e - 4 of the step, as accumulators lie.
+template <int D, int NS>
+__device__ __forceinline__ void columns_product(const unsigned char* __restrict__ tile, const bf16x8 (*b)[Mma<D>::QT],
+                                                typename Mma<D>::Acc (*acc)[Mma<D>::QT], int base) {
+  using X = Mma<D>;
+  constexpr int DT = D / X::MR;
+  constexpr int NO = NS * DT;
+  constexpr int AHEAD = NO < 3 ? NO : (X::MR == 16 ? 3 : 2);
+  // KC / 2 rows on, the permutation of d 128 is the same, that of d 64 (8 rows) differs by 2
+  constexpr int HI = X::MR == 16 ? 0 : 32;
+  bf16x8 a[NO];
+#pragma unroll
+  for (int i = 0; i < NO; ++i) {
+    const int at = base ^ (2 * X::MR * (i % DT));
+    const unsigned char* p = tile + (X::KC * (i / DT)) * (2 * D);
+    const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS v4i16*)(p + at));
+    const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS v4i16*)(p + (at ^ HI) + X::KC / 2 * (2 * D)));
+    const v8i16 a8 = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    a[i] = __builtin_bit_cast(bf16x8, a8);
+  }
+#pragma unroll
+  for (int i = 0; i < NO; ++i)
+#pragma unroll
+    for (int c = 0; c < X::QT; ++c) acc[i % DT][c] = X::mma(a[i], b[i / DT][c], acc[i % DT][c]);
+  __builtin_amdgcn_sched_group_barrier(kSgDsRead, 2 * AHEAD, 0);
+#pragma unroll
+  for (int i = 0; i < NO - AHEAD; ++i) {
+    __builtin_amdgcn_sched_group_barrier(kSgMfma, X::QT, 0);
+    __builtin_amdgcn_sched_group_barrier(kSgDsRead, 2, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(kSgMfma, X::QT * AHEAD, 0);
+}
+
+// Bases of this lane for the two ways of reading a tile.
+template <int D>
+__device__ __forceinline__ int rows_base(int lane) {
+  using X = Mma<D>;
+  const int c = lane % X::MR, lg = lane / X::MR;
+  return c * (2 * D) + 16 * (lg ^ GradTile<D, 64>::swz(c));
+}
+template <int D>
+__device__ __forceinline__ int columns_base(int lane) {
+  using X = Mma<D>;
+  const int row = 4 * (lane / X::MR) + ((lane & 15) >> 2);
+  const int slot = (X::MR == 32 ? 2 * ((lane >> 4) & 1) : 0) + ((lane & 3) >> 1);
+  return row * (2 * D) + 16 * (slot ^ GradTile<D, 64>::swz(row)) + 8 * (lane & 1);
+}
+
+// Two products' accumulators of a step of KC rows as one bf16 operand: element e of the lane's 8.
+template <int D, int NT>
+__device__ __forceinline__ void as_operand(const typename Mma<D>::Acc (*acc)[Mma<D>::QT], bf16x8 (*b)[Mma<D>::QT]) {
+  using X = Mma<D>;
+#pragma unroll
+  for (int s = 0; s < NT * X::MR / X::KC; ++s)
+#pragma unroll
+    for (int c = 0; c < X::QT; ++c) {
+      u32x4 w;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int e = 8 * s + 2 * j;
+        w[j] = pack_bf16x2(acc[e / X::AR][c][e % X::AR], acc[e / X::AR][c][e % X::AR + 1]);
+      }
+      b[s][c] = __builtin_bit_cast(bf16x8, w);
+    }
+}
+
+// A wave's 32 rows of a result as bf16 (column c of `acc` is row MR c + lane % MR), or their fp32 partial sums.
+template <int D>
+__device__ __forceinline__ void store_rows(const typename Mma<D>::Acc (*acc)[Mma<D>::QT], int c, float factor, bool ok,
+                                           uint16_t* dst, int lg) {
+  using X = Mma<D>;
+  u32x4 y[D / (8 * X::NG)];
+  out_words<D>(acc, c, factor, y);
+  if (!ok) return;
+#pragma unroll
+  for (int i = 0; i < D / (8 * X::NG); ++i) *(u32x4*)(dst + out_col<D>(i, lg)) = y[i];
+}
+template <int D>
+__device__ __forceinline__ void store_part(const typename Mma<D>::Acc (*acc)[Mma<D>::QT], int c, float* dst, int lg) {
+  using X = Mma<D>;
+#pragma unroll
+  for (int dt = 0; dt < D / X::MR; ++dt)
+#pragma unroll
+    for (int i = 0; i < X::AR; i += 4)
+      *(f32x4*)(dst + X::MR * dt + X::acc_row(i) + 4 * lg) =
+          f32x4{acc[dt][c][i], acc[dt][c][i + 1], acc[dt][c][i + 2], acc[dt][c][i + 3]};
+}
+
+struct GradArgs {
+  GradGeom g;
+  GradIo io;
+};
+
+// How the bias enters a wave's tile of pairs: every pair by its distance, or one number for all.
+struct TileBias {
+  bool near;
+  float far;
+};
+struct FarBias {
+  float lo, hi;
+};
+__device__ __forceinline__ FarBias far_bias(const GradIo& io, const float* table) {
+  return FarBias{table[kBiasPad], table[kBiasPad + io.bias_hi - io.bias_lo]};
+}
+__device__ __forceinline__ TileBias tile_bias(const GradIo& io, const FarBias& far, int least, int most) {
+  if (most <= io.bias_lo) return TileBias{false, far.lo};
+  if (least >= io.bias_hi) return TileBias{false, far.hi};
+  return TileBias{true, 0.f};
+}
+
+// The compiler moves no access to LDS across (a wave's own come in order).
+__device__ __forceinline__ void lds_order() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// ------------------------------------------------------------------------------------------------
+// dK and dV
+
+template <int D, bool BIAS>
+__global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void key_grad_kernel(GradArgs a) {
+  using X = Mma<D>;
+  constexpr int QT = D == 128 ? 32 : 64;               // query rows of a tile
+  using T = GradTile<D, QT>;
+  using TV = GradTile<D, 64>;
+  constexpr int NT = QT / X::MR;
+  __shared__ __attribute__((aligned(1024))) unsigned char ring[4 * T::BYTES];       // Q, dO of two stages
+  __shared__ __attribute__((aligned(1024))) unsigned char vtile[2 * TV::BYTES];
+  __shared__ __attribute__((aligned(1024))) unsigned char stat[2 * kStatBytes];
+  const GradGeom& g = a.g;
+  const GradIo& io = a.io;
+  const int P = gridDim.x;
+  const int l = (blockIdx.x & 7) * (P >> 3) + (blockIdx.x >> 3);
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int lw = __builtin_amdgcn_readfirstlane(tid >> 6);
+  if (g.cuts && tid == 0) io.cut[2 * l] = io.cut[2 * l + 1] = int4{0, 0, 0, 0};
+  uint64_t share;
+  GradWalk wk = grad_start<QT>(g, l, P, &share);
+  if (!wk.more()) return;
+  const int c = lane % X::MR, lg = lane / X::MR;
+  const int rbase = rows_base<D>(lane), cbase = columns_base<D>(lane);
+  const uint32_t q_stride = (uint32_t)io.q_tok * 2u, do_stride = (uint32_t)io.do_tok * 2u,
+                 v_stride = (uint32_t)io.v_tok * 2u;
+  uint32_t q_off[T::PER], do_off[T::PER];
+#pragma unroll
+  for (int i = 0; i < T::PER; ++i) {
+    q_off[i] = grad_slot<D, QT>(lw, i, lane, q_stride);
+    do_off[i] = grad_slot<D, QT>(lw, i, lane, do_stride);
+  }
+  const int w0 = 32 * lw;                              // the wave's first key of the unit
+  typename X::Acc dk[D / X::MR][X::QT], dv[D / X::MR][X::QT];
+  bf16x8 kreg[D / X::KC][X::QT];
+
+  while (wk.more()) {
+    uint64_t unit_end;
+    const GradPiece pc = grad_piece<QT>(g, wk, &unit_end);
+    if (pc.tb > pc.ta) {
+      const Seq q = wk.q;
+      const int n0 = wk.b * kGradRows;                 // the unit's first key
+      const int off = q.lk - q.lq;
+      const int nq = (q.lq + QT - 1) / QT;
+      const int seen = (int)(grad_seen(wk.line, wk.b) / QT);
+      const int first = nq - seen;                     // first query tile that sees a key of the unit
+      // the inner tiles are the `seen` tiles of each head in turn
+      int64_t left = seen == 0 ? 0 : pc.tb - pc.ta;
+      int head = seen == 0 ? 0 : (int)(pc.ta / seen);
+      int tile = seen == 0 ? 0 : (int)(pc.ta - (int64_t)head * seen);
+      __syncthreads();                                 // the piece before is read
+      {
+        uint32_t v_off[TV::PER];
+#pragma unroll
+        for (int i = 0; i < TV::PER; ++i) v_off[i] = grad_slot<D, 64>(lw, i, lane, v_stride);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const int k0 = n0 + 64 * half;
+          const uint32_t nrec = __builtin_amdgcn_readfirstlane((uint32_t)min(max(q.lk - k0, 0), 64) * v_stride);
+          const uint64_t at =
+              first_lane_u64((uint64_t)(((int64_t)q.k0 + k0) * io.v_tok + (int64_t)wk.h * io.v_head) * 2u);
+          grad_issue<D, 64>(vtile + half * TV::BYTES + lw * (TV::BYTES / 4), io.v, at, nrec, v_off);
+        }
+      }
+      auto issue = [&](int h, int t, int st) {
+        const int row = t * QT, qh = wk.h * g.G + h;
+        const int rows = min(q.lq - row, QT);
+        const uint64_t tok = (uint64_t)q.q0 + row;
+        unsigned char* dst = ring + st * (2 * T::BYTES) + lw * (T::BYTES / 4);
+        grad_issue<D, QT>(dst, io.q, first_lane_u64((uint64_t)((int64_t)tok * io.q_tok + (int64_t)qh * io.q_head) * 2u),
+                          __builtin_amdgcn_readfirstlane((uint32_t)rows * q_stride), q_off);
+        grad_issue<D, QT>(dst + T::BYTES, io.dout,
+                          first_lane_u64((uint64_t)((int64_t)tok * io.do_tok + (int64_t)qh * io.do_head) * 2u),
+                          __builtin_amdgcn_readfirstlane((uint32_t)rows * do_stride), do_off);
+        // whole words of 16 bytes: the row behind an odd number of them is masked
+        if (lw == 0)
+          stat_issue(stat + st * kStatBytes, io.stat, first_lane_u64(((uint64_t)qh * (uint32_t)g.Tq + tok) * 8u),
+                     __builtin_amdgcn_readfirstlane((uint32_t)(rows + 1) / 2 * 16u), lane);
+      };
+      if (left > 0) issue(head, first + tile, 0);
+#pragma unroll
+      for (int kc = 0; kc < X::QT; ++kc) {
+        const int n = n0 + w0 + X::MR * kc + c;
+        const uint16_t* src = io.k + ((int64_t)q.k0 + n) * io.k_tok + (int64_t)wk.h * io.k_head + 8 * lg;
+#pragma unroll
+        for (int ks = 0; ks < D / X::KC; ++ks) {
+          u32x4 w = u32x4{0u, 0u, 0u, 0u};
+          if (n < q.lk) w = *(const u32x4*)(src + X::KC * ks);
+          kreg[ks][kc] = __builtin_bit_cast(bf16x8, w);
+        }
+#pragma unroll
+        for (int dt = 0; dt < D / X::MR; ++dt)
+#pragma unroll
+          for (int i = 0; i < X::AR; ++i) dk[dt][kc][i] = dv[dt][kc][i] = 0.f;
+      }
+      const bool here = n0 + w0 < q.lk;                // the wave has keys
+      const float* table = nullptr;                    // the bias of the present head
+      FarBias far{0.f, 0.f};
+      for (int st = 0; left > 0; --left, st ^= 1) {
+        __builtin_amdgcn_s_waitcnt(0);
+        phase_barrier();
+        const int row0 = (first + tile) * QT;
+        if constexpr (BIAS) {
+          if (table == nullptr || tile == 0) {
+            table = io.table + (int64_t)(wk.h * g.G + head) * io.bias_pitch;
+            far = far_bias(io, table);
+          }
+        }
+        if (++tile == seen) {
+          tile = 0;
+          ++head;
+        }
+        if (left > 1) issue(head, first + tile, st ^ 1);
+        // rows [row0, row0 + QT) and keys [key0, key0 + 32)
+        const int key0 = n0 + w0;
+        if (!here || (g.causal && row0 + QT - 1 + off < key0)) continue;
+        const unsigned char* qt = ring + st * (2 * T::BYTES);
+        const unsigned char* dt = qt + T::BYTES;
+        typename X::Acc s[NT][X::QT], dp[NT][X::QT];
+        rows_product<D, NT>(qt, kreg, s, rbase);
+        tiles_product<D, NT>(dt, vtile + (w0 >> 6) * TV::BYTES + (w0 & 63) * (2 * D), dp, rbase, rbase);
+        TileBias bias{false, 0.f};
+        if constexpr (BIAS) {
+          bias = tile_bias(io, far, key0 - (row0 + QT - 1 + off), key0 + 31 - (row0 + off));
+        }
+        const bool open = row0 + QT > q.lq || (g.causal && key0 + 31 > row0 + off);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int i = 0; i < X::AR; i += 4) {
+            const int r = X::MR * t + X::acc_row(i) + 4 * lg;        // the first of four rows
+            const f32x4 s01 = *(const f32x4*)(stat + st * kStatBytes + 8 * r);
+            const f32x4 s23 = *(const f32x4*)(stat + st * kStatBytes + 8 * r + 16);
+            const float lse[4] = {s01[0], s01[2], s23[0], s23[2]}, delta[4] = {s01[1], s01[3], s23[1], s23[3]};
+#pragma unroll
+            for (int kc = 0; kc < X::QT; ++kc) {
+              f32x4 b = f32x4{0.f, 0.f, 0.f, 0.f};
+              const int n = key0 + X::MR * kc + c;
+              if (BIAS && bias.near) {
+                const float* at = table + (n - (row0 + r + 3 + off) - io.bias_lo + kBiasPad);
+                b = f32x4{at[3], at[2], at[1], at[0]};
+              }
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                float m = lse[j];
+                if constexpr (BIAS) m -= bias.near ? b[j] : bias.far;
+                float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][kc][i + j], io.scale_log2, -m));
+                float ds = p * (dp[t][kc][i + j] - delta[j]);
+                if (open) {
+                  const int row = row0 + r + j;
+                  if (row >= q.lq || (g.causal && n > row + off)) p = ds = 0.f;
+                }
+                s[t][kc][i + j] = p;
+                dp[t][kc][i + j] = ds;
+              }
+            }
+          }
+        bf16x8 op[QT / X::KC][X::QT];
+        as_operand<D, NT>(s, op);
+        columns_product<D, QT / X::KC>(dt, op, dv, cbase);
+        as_operand<D, NT>(dp, op);
+        columns_product<D, QT / X::KC>(qt, op, dk, cbase);
+      }
+      __builtin_amdgcn_s_waitcnt(0);                   // V, where nothing saw the unit
+      const bool whole = pc.ta == 0 && pc.tb == pc.n;
+      const int slot = 2 * l + (pc.ta == 0 ? 1 : 0);
+      if (!whole && tid == 0) io.cut[slot] = int4{q.k0 + n0, min(kGradRows, q.lk - n0), wk.h, 1};
+#pragma unroll
+      for (int kc = 0; kc < X::QT; ++kc) {
+        const int r = w0 + X::MR * kc + c;
+        if (whole) {
+          const bool ok = n0 + r < q.lk;
+          const int64_t tok = (int64_t)q.k0 + n0 + r;
+          store_rows<D>(dk, kc, io.scale, ok, io.out0 + tok * io.out0_tok + (int64_t)wk.h * io.out0_head, lg);
+          store_rows<D>(dv, kc, 1.0f, ok, io.out1 + tok * io.out1_tok + (int64_t)wk.h * io.out1_head, lg);
+        } else {
+          float* dst = io.part + ((size_t)slot * 2 * kGradRows + r) * D;
+          store_part<D>(dk, kc, dst, lg);
+          store_part<D>(dv, kc, dst + (size_t)kGradRows * D, lg);
+        }
+      }
+    }
+    grad_on<QT>(g, wk, unit_end);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------
+// dQ, and the bias' gradient
+
+// Adds a wave's tile of dS to its sums by distance, `sums`, which start at distance lo - kBiasPad: X[t][c] is the
+// product's accumulator, key rows by query columns.
+//
+// The blocks of 16 keys by 16 queries whose keys are as far ahead of their queries are added first, then each
+// is laid into LDS row by row (a query's 16 keys) and its diagonals are summed: lane j of quarter h takes key
+// (j + r) mod 16 of the queries r = 4 h .. 4 h + 3, which lie at distance j where j + r < 16, else j - 16.
+template <int D>
+__device__ __forceinline__ void add_diagonals(const typename Mma<D>::Acc (*x)[Mma<D>::QT], float* block, float* sums,
+                                              int first, int lane) {
+  using X = Mma<D>;
+  // 16 x 16 blocks of the 64 keys and 32 queries: block e has 16 (kt - qt) = 16 e, e from -1 to 3
+#pragma unroll
+  for (int e = -1; e < 4; ++e) {
+    if constexpr (X::MR == 16) {
+      f32x4 y = e >= 0 ? x[e][0] : x[0][1];
+      if (e >= 0 && e < 3) y += x[e + 1][1];
+      *(f32x4*)(block + 16 * (lane & 15) + 4 * (lane >> 4)) = y;
+    } else {
+      // lanes 0..15 and 32..47 hold the columns of qt = 0, the others those of qt = 1; registers 8 (kt & 1) + 4 u + v
+      // of accumulator kt / 2 hold key 8 u + 4 (lane / 32) + v of key block kt.  A column's own block is e + qt.
+      const int qt = (lane >> 4) & 1;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
+        const int k0 = e, k1 = e + 1;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const float mine0 = k0 >= 0 ? x[k0 >> 1][0][8 * (k0 & 1) + 4 * u + v] : 0.f;
+          const float mine1 = k1 < 4 ? x[(k1 & 3) >> 1][0][8 * (k1 & 1) + 4 * u + v] : 0.f;
+          y[v] = qt ? mine1 : mine0;
+        }
+#pragma unroll
+        for (int v = 0; v < 4; ++v) y[v] += __shfl_xor(y[v], 16);
+        if (qt == 0) *(f32x4*)(block + 16 * (lane & 15) + 8 * u + 4 * (lane >> 5)) = y;
+      }
+    }
+    lds_order();
+    const int j = lane & 15, quarter = lane >> 4;
+    float ahead = 0.f, behind = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = 4 * quarter + i;
+      const float v = block[16 * r + ((j + r) & 15)];
+      if (j + r < 16) ahead += v;
+      else behind += v;
+    }
+    lds_order();
+    ahead += __shfl_xor(ahead, 16);
+    ahead += __shfl_xor(ahead, 32);
+    behind += __shfl_xor(behind, 16);
+    behind += __shfl_xor(behind, 32);
+    if (lane < 32) sums[first + 16 * e + (lane < 16 ? j : j - 16)] += lane < 16 ? ahead : behind;
+    lds_order();
+  }
+}
+
+template <int D, bool BIAS>
+__global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void row_grad_kernel(GradArgs a) {
+  using X = Mma<D>;
+  constexpr int NT = KT / X::MR;
+  using T = GradTile<D, KT>;
+  __shared__ __attribute__((aligned(1024))) unsigned char ring[4 * T::BYTES];       // K, V of two stages
+  __shared__ __attribute__((aligned(16))) float block[BIAS ? 4 : 1][BIAS ? 256 : 4];
+  __shared__ float sums[BIAS ? 4 : 1][BIAS ? kBiasPitch : 1];
+  const GradGeom& g = a.g;
+  const GradIo& io = a.io;
+  const int P = gridDim.x;
+  const int l = (blockIdx.x & 7) * (P >> 3) + (blockIdx.x >> 3);
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int lw = __builtin_amdgcn_readfirstlane(tid >> 6);
+  if (g.cuts && tid == 0) io.cut[2 * l] = io.cut[2 * l + 1] = int4{0, 0, 0, 0};
+  uint64_t share;
+  GradWalk wk = grad_start<0>(g, l, P, &share);
+  if (BIAS && blockIdx.x == 0 && tid == 0) {
+    io.line[0] = wk.head;
+    io.line[1] = share;
+  }
+  // a stretch that its borders' moving left empty still writes its heads' sums
+  if (!wk.more() && !(BIAS && (uint64_t)(uint32_t)l * share < wk.head * (uint32_t)g.NH)) return;
+  // the heads whose sums this workgroup writes
+  int sum_head = 0, last_head = 0;
+  float far_lo = 0.f, far_hi = 0.f;
+  if constexpr (BIAS) {
+    sum_head = (int)((uint64_t)(uint32_t)l * share / wk.head);
+    last_head = (int)((wk.end - 1) / wk.head);
+    for (int i = tid; i < 4 * kBiasPitch; i += kGradThreads) (&sums[0][0])[i] = 0.f;
+    __syncthreads();
+  }
+  // writes the sums of the heads before `until`
+  auto flush = [&](int until) {
+    if constexpr (BIAS) {
+      for (; sum_head < until; ++sum_head) {
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) {
+          far_lo += __shfl_xor(far_lo, m);
+          far_hi += __shfl_xor(far_hi, m);
+        }
+        if (lane == 0) {
+          sums[lw][0] += far_lo;
+          sums[lw][io.bias_pitch - 1] += far_hi;
+        }
+        far_lo = far_hi = 0.f;
+        __syncthreads();
+        float* dst = io.dist + (size_t)(l + sum_head) * io.bias_pitch;
+        for (int i = tid; i < io.bias_pitch; i += kGradThreads) {
+          dst[i] = (sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]);
+          sums[0][i] = sums[1][i] = sums[2][i] = sums[3][i] = 0.f;
+        }
+        __syncthreads();
+      }
+    }
+  };
+  const int c = lane % X::MR, lg = lane / X::MR;
+  const int rbase = rows_base<D>(lane), cbase = columns_base<D>(lane);
+  const uint32_t k_stride = (uint32_t)io.k_tok * 2u, v_stride = (uint32_t)io.v_tok * 2u;
+  uint32_t k_off[T::PER], v_off[T::PER];
+#pragma unroll
+  for (int i = 0; i < T::PER; ++i) {
+    k_off[i] = grad_slot<D, KT>(lw, i, lane, k_stride);
+    v_off[i] = grad_slot<D, KT>(lw, i, lane, v_stride);
+  }
+  const int w0 = 32 * lw;
+  typename X::Acc dq[D / X::MR][X::QT];
+  bf16x8 qreg[D / X::KC][X::QT], doreg[D / X::KC][X::QT];
+
+  while (wk.more()) {
+    uint64_t unit_end;
+    const GradPiece pc = grad_piece<KT>(g, wk, &unit_end);
+    if (pc.tb > pc.ta) {
+      const Seq q = wk.q;
+      const int off = q.lk - q.lq;
+      const int kvh = wk.h / g.GS, head0 = wk.h % g.GS * g.GH;         // the unit's heads within the group
+      const int heads = min(g.GH, g.G - head0);
+      const int t0 = wk.b * g.TB, tokens = min(g.TB, q.lq - t0);
+      if constexpr (BIAS) flush(wk.h);
+      __syncthreads();                                 // the piece before is read
+      const int keys = (int)grad_seen(wk.line, wk.b);  // keys that the unit's last token sees
+      const int first = (int)pc.ta, N = keys == 0 ? 0 : (int)(pc.tb - pc.ta);
+      auto issue = [&](int t, int st) {
+        const int k0 = 64 * t;
+        const int rows = min(q.lk - k0, 64);
+        unsigned char* dst = ring + st * (2 * T::BYTES) + lw * (T::BYTES / 4);
+        const int64_t tok = (int64_t)q.k0 + k0;
+        grad_issue<D, KT>(dst, io.k, first_lane_u64((uint64_t)(tok * io.k_tok + (int64_t)kvh * io.k_head) * 2u),
+                          __builtin_amdgcn_readfirstlane((uint32_t)rows * k_stride), k_off);
+        grad_issue<D, KT>(dst + T::BYTES, io.v,
+                          first_lane_u64((uint64_t)(tok * io.v_tok + (int64_t)kvh * io.v_head) * 2u),
+                          __builtin_amdgcn_readfirstlane((uint32_t)rows * v_stride), v_off);
+      };
+      if (N > 0) issue(first, 0);
+      float lse[X::QT], delta[X::QT];
+      int limit[X::QT], wave_keys = 0, wave_open = 0x7fffffff;
+      int row_at[X::QT];                               // the token, or -1
+#pragma unroll
+      for (int qc = 0; qc < X::QT; ++qc) {
+        const int r = w0 + X::MR * qc + c;
+        const int t = (int)(((uint32_t)r * (uint32_t)g.gh_magic) >> 16), j = r - t * g.GH;
+        const bool ok = t < tokens && j < heads;
+        const int token = t0 + t, head = kvh * g.G + head0 + j;
+        row_at[qc] = ok ? token : -1;
+        const int64_t tok = (int64_t)q.q0 + token;
+        const uint16_t* qs = io.q + tok * io.q_tok + (int64_t)head * io.q_head + 8 * lg;
+        const uint16_t* ds = io.dout + tok * io.do_tok + (int64_t)head * io.do_head + 8 * lg;
+#pragma unroll
+        for (int ks = 0; ks < D / X::KC; ++ks) {
+          u32x4 w = u32x4{0u, 0u, 0u, 0u}, x = w;
+          if (ok) {
+            w = *(const u32x4*)(qs + X::KC * ks);
+            x = *(const u32x4*)(ds + X::KC * ks);
+          }
+          qreg[ks][qc] = __builtin_bit_cast(bf16x8, w);
+          doreg[ks][qc] = __builtin_bit_cast(bf16x8, x);
+        }
+        float2 z = float2{INFINITY, 0.f};
+        if (ok) z = io.stat[(uint64_t)head * (uint32_t)g.Tq + (uint64_t)tok];
+        lse[qc] = z.x;
+        delta[qc] = z.y;
+        limit[qc] = ok ? (g.causal ? max(0, min(q.lk, off + token + 1)) : q.lk) : 0x7fffffff;
+        wave_keys = max(wave_keys, ok ? limit[qc] : 0);
+        wave_open = min(wave_open, limit[qc]);
+#pragma unroll
+        for (int dt = 0; dt < D / X::MR; ++dt)
+#pragma unroll
+          for (int i = 0; i < X::AR; ++i) dq[dt][qc][i] = 0.f;
+      }
+#pragma unroll
+      for (int m = 1; m < X::MR; m <<= 1) {
+        wave_keys = max(wave_keys, __shfl_xor(wave_keys, m));
+        wave_open = min(wave_open, __shfl_xor(wave_open, m));
+      }
+      wave_keys = __builtin_amdgcn_readfirstlane(wave_keys);       // keys that some row of the wave sees
+      wave_open = __builtin_amdgcn_readfirstlane(wave_open);       // and that all of them see
+      const float* table = nullptr;
+      FarBias far{0.f, 0.f};
+      int least_pos = 0;                               // place of the wave's first query among the keys
+      if constexpr (BIAS) {
+        table = io.table + (int64_t)(kvh * g.G + head0) * io.bias_pitch;
+        far = far_bias(io, table);
+        least_pos = off + t0 + w0;
+      }
+      for (int i = 0, st = 0; i < N; ++i, st ^= 1) {
+        __builtin_amdgcn_s_waitcnt(0);
+        phase_barrier();
+        if (i + 1 < N) issue(first + i + 1, st ^ 1);
+        const int key0 = 64 * (first + i);
+        if (key0 >= wave_keys) continue;
+        const unsigned char* kt = ring + st * (2 * T::BYTES);
+        typename X::Acc s[NT][X::QT], dp[NT][X::QT];
+        rows_product<D, NT>(kt, qreg, s, rbase);
+        rows_product<D, NT>(kt + T::BYTES, doreg, dp, rbase);
+        TileBias bias{false, 0.f};
+        if constexpr (BIAS) bias = tile_bias(io, far, key0 - (least_pos + 31), key0 + 63 - least_pos);
+        const bool open = key0 + 64 > wave_open;
+#pragma unroll
+        for (int qc = 0; qc < X::QT; ++qc) {
+          const float m = BIAS && !bias.near ? lse[qc] - bias.far : lse[qc];
+          const int lim = limit[qc] - key0;
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < X::AR; e += 4) {
+              const int r = X::MR * t + X::acc_row(e) + 4 * lg;
+              f32x4 b = f32x4{0.f, 0.f, 0.f, 0.f};
+              if (BIAS && bias.near) {
+                const float* at = table + (key0 + r - (least_pos + X::MR * qc + c) - io.bias_lo + kBiasPad);
+                b = f32x4{at[0], at[1], at[2], at[3]};
+              }
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                float mm = m;
+                if (BIAS && bias.near) mm -= b[j];
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][qc][e + j], io.scale_log2, -mm));
+                const float ds = p * (dp[t][qc][e + j] - delta[qc]);
+                dp[t][qc][e + j] = open && r + j >= lim ? 0.f : ds;
+              }
+            }
+        }
+        if constexpr (BIAS) {
+          if (bias.near) {
+            add_diagonals<D>(dp, block[lw], sums[lw], key0 - least_pos - io.bias_lo + kBiasPad, lane);
+          } else {
+            float x = 0.f;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+              for (int qc = 0; qc < X::QT; ++qc)
+#pragma unroll
+                for (int e = 0; e < X::AR; ++e) x += dp[t][qc][e];
+            if (key0 + 63 - least_pos <= io.bias_lo) far_lo += x;
+            else far_hi += x;
+          }
+        }
+        bf16x8 op[KT / X::KC][X::QT];
+        as_operand<D, NT>(dp, op);
+        columns_product<D, KT / X::KC>(kt, op, dq, cbase);
+      }
+      const bool whole = pc.ta == 0 && pc.tb == pc.n;
+      const int slot = 2 * l + (pc.ta == 0 ? 1 : 0);
+      if (!whole && tid == 0) io.cut[slot] = int4{q.q0 + t0, tokens, kvh * g.G + head0, heads};
+#pragma unroll
+      for (int qc = 0; qc < X::QT; ++qc) {
+        const int r = w0 + X::MR * qc + c;
+        const int t = (int)(((uint32_t)r * (uint32_t)g.gh_magic) >> 16), j = r - t * g.GH;
+        if (whole)
+          store_rows<D>(dq, qc, io.scale, row_at[qc] >= 0,
+                        io.out0 + ((int64_t)q.q0 + t0 + t) * io.out0_tok + (int64_t)(kvh * g.G + head0 + j) * io.out0_head,
+                        lg);
+        else
+          store_part<D>(dq, qc, io.part + ((size_t)slot * kGradRows + r) * D, lg);
+      }
+    }
+    grad_on<0>(g, wk, unit_end);
+  }
+  if constexpr (BIAS) flush(last_head + 1);
+}
+
+// ------------------------------------------------------------------------------------------------
+// Joins the pieces of a unit that several stretches share, in the order of the stretches (as seq_merge_kernel,
+// but sums alone).  Workgroup (l, y, z) joins rows [16 y, 16 y + 16) of array z.
+template <int D>
+__global__ __launch_bounds__(256) void grad_merge_kernel(GradIo io, int GH, int P) {
+  constexpr int TPR = 16, W = D / TPR;
+  const int l0 = blockIdx.x, A = gridDim.z;
+  const int lane = threadIdx.x & 63;
+  const int4 u = io.cut[2 * l0 + 1];
+  if (u.w == 0) return;
+  int n = 0;
+  for (;;) {
+    const int l = l0 + 1 + n + lane;
+    const int4 x = io.cut[2 * min(l, P - 1)];
+    const uint64_t other = ~__ballot(l < P && x.w != 0 && x.x == u.x && x.z == u.z);
+    if (other) {
+      n += __builtin_ctzll(other);
+      break;
+    }
+    n += 64;
+  }
+  const int r = blockIdx.y * 16 + threadIdx.x / TPR, part = threadIdx.x % TPR;
+  const int token = r / GH, head = r - token * GH;
+  if (token >= u.y || head >= u.w) return;
+  float acc[W];
+#pragma unroll
+  for (int e = 0; e < W; ++e) acc[e] = 0.f;
+  constexpr int BATCH = 4;
+  for (int i0 = 0; i0 <= n; i0 += BATCH) {
+    f32x4 x[BATCH][W / 4];
+#pragma unroll
+    for (int j = 0; j < BATCH; ++j) {
+      const int i = min(i0 + j, n);
+      const size_t slot = i == 0 ? 2 * l0 + 1 : 2 * (l0 + i);
+#pragma unroll
+      for (int e = 0; e < W / 4; ++e)
+        x[j][e] = *(const f32x4*)(io.part + ((slot * A + blockIdx.z) * kGradRows + r) * D + part * W + 4 * e);
+    }
+#pragma unroll
+    for (int j = 0; j < BATCH; ++j) {
+      if (i0 + j > n) break;
+#pragma unroll
+      for (int e = 0; e < W; ++e) acc[e] += x[j][e / 4][e % 4];
+    }
+  }
+  const bool second = blockIdx.z == 1;
+  const float f = second ? 1.0f : io.scale;
+  uint16_t* dst = (second ? io.out1 : io.out0) + (int64_t)(u.x + token) * (second ? io.out1_tok : io.out0_tok) +
+                  (int64_t)(u.z + head) * (second ? io.out1_head : io.out0_head) + part * W;
+#pragma unroll
+  for (int e = 0; e < W; e += 4)
+    *(u32x2*)(dst + e) = u32x2{pack_bf16x2(acc[e] * f, acc[e + 1] * f), pack_bf16x2(acc[e + 2] * f, acc[e + 3] * f)};
+}
+
+// ------------------------------------------------------------------------------------------------
+// What both kernels need of a row: lse in base 2, and delta.  Workgroups behind the rows' lay out the bias.
+struct PrepArgs {
+  const uint16_t *o, *dout;
+  const float *lse, *dlse;
+  int64_t o_tok, o_head, do_tok, do_head;
+  float2* stat;
+  int Tq, Hq;
+  int row_groups;                        // workgroups of rows: 16 tokens by 16 heads each
+  SeqBias bias;
+  int pitch;
+  float* table;
+};
+
+template <int D>
+__global__ __launch_bounds__(256) void grad_prep_kernel(PrepArgs a) {
+  const int tid = threadIdx.x;
+  if ((int)blockIdx.x >= a.row_groups) {
+    const int h = blockIdx.x - a.row_groups;
+    for (int i = tid; i < a.pitch; i += 256) {
+      a.table[(size_t)h * a.pitch + i] = bias_log2(a.bias, i - kBiasPad, a.Hq, h);
+    }
+    return;
+  }
+  constexpr int LPR = D / 8;             // lanes of a row
+  constexpr int RPP = 256 / LPR;         // rows of a pass
+  __shared__ float dots[256];
+  const int HB = (a.Hq + 15) / 16;
+  const int64_t t0 = (int64_t)(blockIdx.x / HB) * 16;
+  const int h0 = blockIdx.x % HB * 16;
+#pragma unroll 4
+  for (int p = 0; p < 256 / RPP; ++p) {
+    const int r = p * RPP + tid / LPR;   // token r / 16, head r % 16
+    const int64_t t = t0 + r / 16;
+    const int h = h0 + r % 16;
+    float x = 0.f;
+    if (t < a.Tq && h < a.Hq) {
+      const u32x4 u = *(const u32x4*)(a.o + t * a.o_tok + (int64_t)h * a.o_head + 8 * (tid % LPR));
+      const u32x4 v = *(const u32x4*)(a.dout + t * a.do_tok + (int64_t)h * a.do_head + 8 * (tid % LPR));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x = __builtin_fmaf(__uint_as_float(u[i] << 16), __uint_as_float(v[i] << 16), x);
+        x = __builtin_fmaf(__uint_as_float(u[i] & 0xffff0000u), __uint_as_float(v[i] & 0xffff0000u), x);
+      }
+    }
+#pragma unroll
+    for (int m = 1; m < LPR; m <<= 1) x += __shfl_xor(x, m);
+    if (tid % LPR == 0) dots[r] = x;
+  }
+  __syncthreads();
+  const int64_t t = t0 + tid % 16;
+  const int h = h0 + tid / 16;
+  if (t >= a.Tq || h >= a.Hq) return;
+  const float lse = a.lse[t * a.Hq + h];
+  float delta = dots[tid % 16 * 16 + tid / 16];
+  if (a.dlse) delta -= a.dlse[t * a.Hq + h];
+  // a row that sees nothing has no probabilities: exp2(x - inf) = 0
+  const bool none = lse == -INFINITY;
+  a.stat[(size_t)h * a.Tq + t] = float2{none ? INFINITY : lse * 1.4426950408889634f, none ? 0.f : delta};
+}
+
+// The gradient of the bias' weights: workgroup h adds the sums by distance of head h, over the workgroups
+// that met it and then over a bucket's distances, in 64 bits and a fixed order.
+struct DistArgs {
+  const float* dist;
+  const uint64_t* line;
+  const int32_t* bucket;
+  void* dweight;
+  int bf16, buckets, lo, hi, pitch, Hq, P, empty;
+};
+__global__ __launch_bounds__(1024) void dist_merge_kernel(DistArgs a) {
+  __shared__ double sums[kBiasPitch];
+  __shared__ int to[kBiasMost];
+  const int h = blockIdx.x, tid = threadIdx.x;
+  const int n = a.hi - a.lo + 1;
+  const uint64_t head = a.empty ? 0 : a.line[0], share = a.empty ? 1 : a.line[1];
+  for (int i = tid; i < a.pitch; i += 1024) {
+    double x = 0.0;
+    if (head > 0) {
+      const int l0 = (int)(head * (uint32_t)h / share);
+      const int l1 = min((int)((head * ((uint32_t)h + 1ull) - 1) / share), a.P - 1);
+#pragma unroll 8
+      for (int l = l0; l <= l1; ++l) x += a.dist[(size_t)(l + h) * a.pitch + i];
+    }
+    sums[i] = x;
+  }
+  for (int i = tid; i < n; i += 1024) to[i] = a.bucket[i];
+  __syncthreads();
+  if (tid < 2) {                          // what lies beyond the ends belongs to them
+    double x = 0.0;
+    for (int i = 0; i < kBiasPad; ++i) x += sums[tid == 0 ? i : kBiasPad + n + i];
+    sums[tid == 0 ? 0 : kBiasPad + n] = x;
+  }
+  __syncthreads();
+  for (int b = tid; b < a.buckets; b += 1024) {
+    double x = 0.0;
+    for (int i = 0; i < n; ++i) {
+      if (to[i] != b) continue;
+      x += sums[kBiasPad + i];
+      if (i == 0) x += sums[0];
+      if (i == n - 1) x += sums[kBiasPad + n];
+    }
+    const size_t at = (size_t)b * a.Hq + h;
+    if (a.bf16) ((uint16_t*)a.dweight)[at] = (uint16_t)(pack_bf16x2((float)x, 0.f) & 0xffffu);
+    else ((float*)a.dweight)[at] = (float)x;
+  }
+}
+
+}  // namespace
+
+template <int D>
+static hipError_t launch_grad(const GradCall& c, hipStream_t st) {
+  if (c.rows) {
+    const int groups = ceil_div(c.Tq, 16) * ceil_div(c.rows_g.Hq, 16);
+    const PrepArgs p{c.o, c.rows_io.dout, c.lse, c.dlse, c.o_tok, c.o_head, c.rows_io.do_tok, c.rows_io.do_head,
+                     const_cast<float2*>(c.rows_io.stat), c.Tq, c.rows_g.Hq, groups, c.bias, c.rows_io.bias_pitch,
+                     const_cast<float*>(c.rows_io.table)};
+    hipLaunchKernelGGL((grad_prep_kernel<D>), dim3(groups + (c.has_bias ? c.rows_g.Hq : 0)), dim3(256), 0, st, p);
+    const GradArgs a{c.rows_g, c.rows_io};
+    if (c.has_bias) hipLaunchKernelGGL((row_grad_kernel<D, true>), dim3(c.rows_p), dim3(kGradThreads), 0, st, a);
+    else hipLaunchKernelGGL((row_grad_kernel<D, false>), dim3(c.rows_p), dim3(kGradThreads), 0, st, a);
+    if (c.rows_g.cuts)
+      hipLaunchKernelGGL((grad_merge_kernel<D>), dim3(c.rows_p, kGradRows / 16, 1), dim3(256), 0, st, c.rows_io,
+                         c.rows_g.GH, c.rows_p);
+  }
+  if (c.keys) {
+    const GradArgs a{c.keys_g, c.keys_io};
+    if (c.has_bias) hipLaunchKernelGGL((key_grad_kernel<D, true>), dim3(c.keys_p), dim3(kGradThreads), 0, st, a);
+    else hipLaunchKernelGGL((key_grad_kernel<D, false>), dim3(c.keys_p), dim3(kGradThreads), 0, st, a);
+    if (c.keys_g.cuts)
+      hipLaunchKernelGGL((grad_merge_kernel<D>), dim3(c.keys_p, kGradRows / 16, 2), dim3(256), 0, st, c.keys_io, 1,
+                         c.keys_p);
+  }
+  if (c.has_bias) {
+    const DistArgs d{c.rows_io.dist, c.rows_io.line, c.bias.bucket, c.dweight, c.bias.bf16, c.bias.buckets, c.bias.lo,
+                     c.bias.hi, c.rows_io.bias_pitch, c.rows_g.Hq, c.rows_p, !c.rows};
+    hipLaunchKernelGGL(dist_merge_kernel, dim3(c.rows_g.Hq), dim3(1024), 0, st, d);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_prompt_bwd(const GradCall& c, int d, hipStream_t st) {
+  return d == 128 ? launch_grad<128>(c, st) : launch_grad<64>(c, st);
+}
+
+}  // namespace la

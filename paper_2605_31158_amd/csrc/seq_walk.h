@@ -60,7 +60,29 @@ struct SeqIo {
   float scale_log2;
 };
 
+// Distances that a tile of 64 x 32 pairs can have beyond the bias' first or last one while it still needs the table.
+constexpr int kBiasPad = 96;
+constexpr int kBiasMost = 513;                              // distances
+constexpr int kBiasPitch = kBiasMost + 2 * kBiasPad;
+constexpr int kBiasHeads = 8;                               // of a unit of la_prompt_attn_bias
+
+// A learned bias by relative position (la_rel_bias).
+struct SeqBias {
+  const int32_t* bucket;
+  const void* weight;      // [buckets][Hq], fp32 or bf16
+  int bf16, buckets, lo, hi;
+};
+
 namespace {
+
+// The bias of bucket bucket[i] and head h in base 2.
+__device__ __forceinline__ float bias_log2(const SeqBias& b, int i, int Hq, int h) {
+  const int n = b.bucket[min(max(i, 0), b.hi - b.lo)];
+  if (n < 0 || n >= b.buckets) return 0.f;
+  const size_t at = (size_t)n * Hq + h;
+  const float w = b.bf16 ? __uint_as_float((uint32_t)((const uint16_t*)b.weight)[at] << 16) : ((const float*)b.weight)[at];
+  return w * 1.4426950408889634f;
+}
 
 template <bool CACHE>
 __device__ __forceinline__ Seq load_seq(const SeqGeom& g, int s) {

@@ -57,6 +57,16 @@ class Seqs(ctypes.Structure):
                                               "v_head")]
 
 
+class RelBias(ctypes.Structure):
+    """la_rel_bias: the distances of a relative bias, and the buckets of its weights."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("lo", "hi", "buckets", "dtype")]
+
+
+class PromptGrads(ctypes.Structure):
+    """la_prompt_grads: the strides of a backward call's gradients."""
+    _fields_ = [(f"{t}_{n}", ctypes.c_int64) for t in ("do", "dq", "dk", "dv") for n in ("token", "head")]
+
+
 class Kv4(ctypes.Structure):
     """la_kv4: the pages of a 4-bit cache."""
     _fields_ = [(n, ctypes.c_int32) for n in ("n_pages", "page", "max_pages")]
@@ -72,6 +82,8 @@ _GP = ctypes.POINTER(Grid3D)
 _QP = ctypes.POINTER(Seqs)
 _KP = ctypes.POINTER(Kv4)
 _RP = ctypes.POINTER(RopeShape)
+_BP = ctypes.POINTER(RelBias)
+_DP = ctypes.POINTER(PromptGrads)
 
 _SIGNATURES = {
     "la_workspace_bytes": (ctypes.c_size_t, [_SP]),
@@ -98,6 +110,12 @@ _SIGNATURES = {
     "la_rope": (ctypes.c_int, [_RP, _P, _P, _P, _P, _P, _P, ctypes.c_float, _P]),
     "la_prompt_ws_bytes": (ctypes.c_size_t, [_QP]),
     "la_prompt_attn": (ctypes.c_int, [_QP, _P, _P, _P, _P, _P, ctypes.c_float, _P, _P, _P, ctypes.c_size_t, _P]),
+    "la_prompt_bias_ws_bytes": (ctypes.c_size_t, [_QP, _BP]),
+    "la_prompt_attn_bias": (ctypes.c_int, [_QP, _BP, _P, _P, _P, _P, _P, _P, _P, ctypes.c_float, _P, _P, _P,
+                                           ctypes.c_size_t, _P]),
+    "la_prompt_bwd_ws_bytes": (ctypes.c_size_t, [_QP, _BP]),
+    "la_prompt_attn_bwd": (ctypes.c_int, [_QP, _DP, _BP, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, ctypes.c_float,
+                                          _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
     "la_kv4_page_bytes": (ctypes.c_size_t, [ctypes.c_int32, ctypes.c_int32]),
     "la_kv4_append": (ctypes.c_int, [_QP, _KP, _P, _P, _P, _P, _P, _P, _P]),
     "la_kv4_read": (ctypes.c_int, [_QP, _KP, _P, _P, _P, _P, _P, _P, _P]),
@@ -774,16 +792,66 @@ def _scratch(need, q, dev, ws):
     return ws.data_ptr(), ws.numel() * ws.element_size(), ws
 
 
+class RelativeBias(NamedTuple):
+    """A learned bias by relative position: the logit of a query at place p among its sequence's keys (query i of
+    lq stands at i + lk - lq) and key n gets weight[bucket[clamp(n - p, lo, hi) - lo], head].
+
+    weight  [buckets, Hq], fp32 or bf16, contiguous, on the GPU.  bucket  int32 [hi - lo + 1] on the GPU, at most
+    513 distances (relative_buckets makes the usual ones); a bucket outside the weights' rows has no bias."""
+    weight: torch.Tensor
+    bucket: torch.Tensor
+    lo: int
+
+
+def relative_buckets(buckets: int = 32, reach: int = 128, both: bool = True, device="cuda"):
+    """(bucket int32 [distances], lo) of a RelativeBias with logarithmic buckets.
+
+    Of the buckets of a side the first half hold one distance each, 0, 1, .., and the others ever more, on a
+    logarithm that reaches the last bucket's end at `reach`; all distances from there on are in the last one.  both:
+    the keys behind a query (positive distances) have the upper half of the buckets, else they share that of
+    distance 0."""
+    n = buckets // 2 if both else buckets
+    one = n // 2
+    if n < 2 or not one < reach <= (256 if both else 512):
+        raise ValueError(f"no {buckets} buckets over {reach} distances" + (" to either side" if both else ""))
+
+    def side(m):
+        if m < one:
+            return m
+        # the largest j with log(m / one) / log(reach / one) (n - one) >= j, in whole numbers
+        j = 0
+        while one + j + 1 < n and m ** (n - one) * one ** (j + 1) >= reach ** (j + 1) * one ** (n - one):
+            j += 1
+        return one + j
+
+    to = [side(m) for m in range(reach + 1)]
+    rows = to[::-1] + ([n + b for b in to[1:]] if both else [])
+    return torch.tensor(rows, dtype=torch.int32, device=device), -reach
+
+
+def _rel_bias(bias, dev, Hq):
+    """The la_rel_bias of a RelativeBias by reference; raises for what does not fit."""
+    w, b = bias.weight, bias.bucket
+    if not isinstance(w, torch.Tensor) or w.get_device() != dev or w.dtype not in _DTYPES or w.dim() != 2 \
+            or w.shape[1] != Hq or not w.is_contiguous():
+        raise ValueError(f"bias.weight must be a contiguous float32 or bfloat16 [buckets, {Hq}] tensor on GPU {dev}")
+    n = b.numel() if isinstance(b, torch.Tensor) else 0
+    _check_ints("bias.bucket", b, dev, (n,))
+    if not 1 <= n <= 513 or not -(1 << 20) <= bias.lo <= (1 << 20) or not 1 <= w.shape[0] <= (1 << 20):
+        raise ValueError("a bias has 1 to 513 distances within 2^20 of 0, and 1 to 2^20 buckets")
+    return ctypes.byref(RelBias(bias.lo, bias.lo + n - 1, w.shape[0], _DTYPES[w.dtype]))
+
+
 def prompt_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor,
                 cu_k: Optional[torch.Tensor] = None, causal: bool = True, scale: Optional[float] = None,
                 want_lse: bool = False, ws: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
-                lse_out: Optional[torch.Tensor] = None):
+                lse_out: Optional[torch.Tensor] = None, bias: Optional[RelativeBias] = None):
     """Attention of packed sequences over their own keys -> o bf16 [Tq, Hq, d] (and lse fp32 [Tq, Hq]).
 
     q [Tq, Hq, d]; k, v [Tk, Hkv, d] in bf16, Hq a multiple of Hkv; token and head strides are free
     (multiples of 8).  cu_q, cu_k int32 [S + 1] on the GPU: the first row of every sequence (cu_k None:
-    cu_q).  Causal: the last query of a sequence sees its last key.  Rows behind the last sequence are
-    not written (a new output holds anything there)."""
+    cu_q).  Causal: the last query of a sequence sees its last key.  bias: added to the scaled logits.  Rows
+    behind the last sequence are not written (a new output holds anything there)."""
     Tq, Hq, d, qt, qh = _rows("q", q)
     dev = q.get_device()
     Tk, Hkv, _, kt, kh = _rows("k", k, dev, d=d)
@@ -795,10 +863,81 @@ def prompt_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.T
     _check_ints("cu_k", cu_k, dev, (S + 1,))
     o, ot, oh, lse = _outputs(q, dev, Tq, Hq, d, want_lse, out, lse_out)
     seqs = _seqs(S, Tq, Tk, Hq, Hkv, d, 1 if causal else 0, qt, qh, ot, oh, kt, kh, vt, vh)
-    wp, nbytes, ws = _scratch(lib().la_prompt_ws_bytes(seqs), q, dev, ws)
-    _on_device(dev, "la_prompt_attn", seqs, q.data_ptr(), k.data_ptr(), v.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(),
-               scale if scale is not None else 0.0, o.data_ptr(), _ptr(lse), wp, nbytes, _stream(q))
+    scale = scale if scale is not None else 0.0
+    if bias is None:
+        wp, nbytes, ws = _scratch(lib().la_prompt_ws_bytes(seqs), q, dev, ws)
+        _on_device(dev, "la_prompt_attn", seqs, q.data_ptr(), k.data_ptr(), v.data_ptr(), cu_q.data_ptr(),
+                   cu_k.data_ptr(), scale, o.data_ptr(), _ptr(lse), wp, nbytes, _stream(q))
+    else:
+        rel = _rel_bias(bias, dev, Hq)
+        wp, nbytes, ws = _scratch(lib().la_prompt_bias_ws_bytes(seqs, rel), q, dev, ws)
+        _on_device(dev, "la_prompt_attn_bias", seqs, rel, q.data_ptr(), k.data_ptr(), v.data_ptr(), cu_q.data_ptr(),
+                   cu_k.data_ptr(), bias.bucket.data_ptr(), bias.weight.data_ptr(), scale, o.data_ptr(), _ptr(lse), wp,
+                   nbytes, _stream(q))
     return o if lse is None else (o, lse)
+
+
+def _stat(name, t, dev, shape):
+    """Checks a contiguous fp32 [Tq, Hq] tensor."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or t.shape != shape or not t.is_contiguous() \
+            or t.get_device() != dev:
+        raise ValueError(f"{name} must be a contiguous float32 {list(shape)} tensor on GPU {dev}")
+
+
+def prompt_attn_bwd(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor,
+                    lse: torch.Tensor, cu_q: torch.Tensor, cu_k: Optional[torch.Tensor] = None, causal: bool = True,
+                    scale: Optional[float] = None, bias: Optional[RelativeBias] = None,
+                    dlse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                    out: Optional[Tuple[torch.Tensor, ...]] = None):
+    """Gradients of prompt_attn -> (dq [Tq, Hq, d], dk, dv [Tk, Hkv, d]) in bf16, and with a bias that of its
+    weights, in their type.
+
+    do [Tq, Hq, d] bf16: the gradient of o, any strides that prompt_attn's q may have.  o, lse: what prompt_attn
+    returned with want_lse for these q, k, v, cu_q, cu_k, causal, scale and bias.  dlse fp32 [Tq, Hq]: the
+    gradient of lse, where lse was used too.  out: tensors to write, (dq, dk, dv) or with a bias (dq, dk, dv,
+    dweight); they must not overlap each other or an input.  Rows that no sequence covers are not written (new
+    outputs hold anything there); keys that no query sees get zeros."""
+    Tq, Hq, d, qt, qh = _rows("q", q)
+    dev = q.get_device()
+    Tk, Hkv, _, kt, kh = _rows("k", k, dev, d=d)
+    _, _, _, vt, vh = _rows("v", v, dev, Hkv, d, Tk)
+    _, _, _, dt, dh = _rows("do", do, dev, Hq, d, Tq)
+    _, _, _, ot, oh = _rows("o", o, dev, Hq, d, Tq)
+    _stat("lse", lse, dev, (Tq, Hq))
+    if dlse is not None:
+        _stat("dlse", dlse, dev, (Tq, Hq))
+    if cu_k is None:
+        cu_k = cu_q
+    S = cu_q.numel() - 1 if isinstance(cu_q, torch.Tensor) else 0
+    _check_ints("cu_q", cu_q, dev, (S + 1,))
+    _check_ints("cu_k", cu_k, dev, (S + 1,))
+    rel, dw = None, None
+    if bias is not None:
+        rel = _rel_bias(bias, dev, Hq)
+    if out is None:
+        dq = torch.empty_like(q, memory_format=torch.contiguous_format)
+        dk, dv = (torch.empty_like(x, memory_format=torch.contiguous_format) for x in (k, v))
+        if bias is not None:
+            dw = torch.empty_like(bias.weight)
+    elif len(out) != (3 if bias is None else 4):
+        raise ValueError("out must be (dq, dk, dv), and dweight with a bias")
+    else:
+        dq, dk, dv = out[:3]
+        if bias is not None:
+            dw = out[3]
+            if not isinstance(dw, torch.Tensor) or dw.dtype is not bias.weight.dtype or dw.shape != bias.weight.shape \
+                    or not dw.is_contiguous() or dw.get_device() != dev:
+                raise ValueError("dweight must be a contiguous tensor like bias.weight")
+    grads = PromptGrads(dt, dh, *_rows("dq", dq, dev, Hq, d, Tq)[3:], *_rows("dk", dk, dev, Hkv, d, Tk)[3:],
+                        *_rows("dv", dv, dev, Hkv, d, Tk)[3:])
+    seqs = _seqs(S, Tq, Tk, Hq, Hkv, d, 1 if causal else 0, qt, qh, ot, oh, kt, kh, vt, vh)
+    wp, nbytes, ws = _scratch(lib().la_prompt_bwd_ws_bytes(seqs, rel), q, dev, ws)
+    _on_device(dev, "la_prompt_attn_bwd", seqs, ctypes.byref(grads), rel, do.data_ptr(), q.data_ptr(), k.data_ptr(),
+               v.data_ptr(), o.data_ptr(), lse.data_ptr(), _ptr(dlse), cu_q.data_ptr(), cu_k.data_ptr(),
+               _ptr(bias.bucket if bias else None), _ptr(bias.weight if bias else None),
+               scale if scale is not None else 0.0, dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _ptr(dw), wp, nbytes,
+               _stream(q))
+    return (dq, dk, dv) if bias is None else (dq, dk, dv, dw)
 
 
 def kv4_cache(n_pages: int, Hkv: int, d: int, page: int = 64, device="cuda") -> torch.Tensor:

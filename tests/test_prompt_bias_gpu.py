@@ -1,0 +1,149 @@
+"""Attention over packed prompts with a learned bias by relative position (la_prompt_attn_bias) against 64 bits:
+lengths, grouped heads, both directions, short and long reaches, weights that hide distances, strides, rows outside
+the sequences, graph capture."""
+import pytest
+import torch
+
+from paper_2605_31158_amd import la
+import grad_reference as G
+import seq_reference as R
+
+pytestmark = pytest.mark.gpu
+
+
+def make(lq, lk, Hq, Hkv, d, seed, qscale=1.5, spare=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    f = lambda n, h, s: (torch.randn((n, h, d), generator=g, device="cuda") * s).to(torch.bfloat16)   # noqa: E731
+    return f(sum(lq) + spare, Hq, qscale), f(sum(lk) + spare, Hkv, 1.0), f(sum(lk) + spare, Hkv, 1.0)
+
+
+def rel(Hq, seed, buckets=32, reach=128, both=True, dtype=torch.float32):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    bucket, lo = la.relative_buckets(buckets, reach, both)
+    return la.RelativeBias(torch.randn((buckets, Hq), generator=g, device="cuda").to(dtype), bucket, lo)
+
+
+CASES = [
+    # (query lengths, key lengths or None for the same, Hq, Hkv, d, causal, buckets, reach, both)
+    ([1], None, 1, 1, 64, True, 8, 16, False),
+    ([1], [700], 4, 2, 128, True, 32, 128, False),
+    ([1] * 9, [1, 2, 63, 64, 65, 129, 400, 1000, 5], 16, 16, 64, True, 32, 128, False),
+    ([63, 65, 1, 2], None, 2, 1, 64, False, 32, 128, True),
+    ([255, 256, 257], None, 2, 2, 128, False, 32, 40, True),
+    ([255, 256, 257], None, 2, 2, 64, True, 16, 256, True),
+    ([1000], None, 3, 1, 128, True, 32, 128, False),
+    ([700, 1, 300], None, 5, 1, 64, False, 20, 34, True),
+    ([333, 90], None, 14, 2, 128, True, 32, 512, False),      # more heads to a key head than a unit takes
+    ([40, 3], None, 40, 2, 64, False, 32, 128, True),
+    ([0, 5, 0, 0, 70, 0], None, 4, 2, 128, True, 8, 16, True),
+    ([5, 7, 9], [0, 3, 200], 4, 2, 64, True, 32, 128, True),
+    ([500], [20], 2, 2, 128, False, 32, 128, True),           # queries stand before the first key
+    ([130], [2100], 6, 2, 64, False, 64, 256, True),
+    ([2500], None, 2, 1, 128, True, 32, 128, False),
+    ([2100], None, 2, 2, 64, False, 32, 128, True),           # units are cut
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=[str(i) for i in range(len(CASES))])
+def test_against_64_bits(case):
+    lq, lk, Hq, Hkv, d, causal, buckets, reach, both = case
+    lk = lq if lk is None else lk
+    print(f"[bias] {str(lq)[:60]} over {str(lk)[:60]} {case[2:]}", flush=True)
+    q, k, v = make(lq, lk, Hq, Hkv, d, 15)
+    bias = rel(Hq, 16, buckets, reach, both)
+    cu_q, cu_k = R.starts(lq), R.starts(lk)
+    o, lse = la.prompt_attn(q, k, v, cu_q, cu_k, causal=causal, want_lse=True, bias=bias)
+    torch.cuda.synchronize()
+    R.check(o, lse, G.forward(q, k, v, lq, lk, causal, bias=bias), str(case)[:80])
+    again, lse2 = la.prompt_attn(q, k, v, cu_q, cu_k, causal=causal, want_lse=True, bias=bias)
+    assert torch.equal(o, again) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_one_distance_and_shifted_ranges(d):
+    # a bias of one distance is a constant (o stays, lse moves); ranges that lie to one side of 0
+    lq = [300, 65]
+    q, k, v = make(lq, lq, 4, 2, d, 17)
+    cu = R.starts(lq)
+    o, lse = la.prompt_attn(q, k, v, cu, want_lse=True)
+    one = la.RelativeBias(torch.full((1, 4), 0.75, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda"), 5)
+    o1, lse1 = la.prompt_attn(q, k, v, cu, want_lse=True, bias=one)
+    R.check(o1, lse1, G.forward(q, k, v, lq, lq, True, bias=one), "one distance")
+    assert float((lse1 - lse - 0.75).abs().max()) < 1e-5
+    g = torch.Generator(device="cuda").manual_seed(3)
+    for lo, n in ((-200, 100), (20, 90), (-512, 513), (-1, 3), (400, 7), (1000, 2), (-1 << 20, 9), ((1 << 20) - 8, 9)):
+        b = la.RelativeBias(torch.randn((n, 4), generator=g, device="cuda"),
+                            torch.arange(n, dtype=torch.int32, device="cuda"), lo)
+        for causal in (True, False):
+            got, l2 = la.prompt_attn(q, k, v, cu, causal=causal, want_lse=True, bias=b)
+            R.check(got, l2, G.forward(q, k, v, lq, lq, causal, bias=b), f"distances from {lo}, {n}")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_weights_that_hide_and_buckets_that_are_none(d):
+    lq, lk = [200, 300, 3], [260, 100, 3]
+    q, k, v = make(lq, lk, 4, 4, d, 18)
+    cu_q, cu_k = R.starts(lq), R.starts(lk)
+    b = rel(4, 19)
+    # the far buckets of head 0 hidden, of head 1 all but the past, of head 2 everything: rows that see nothing
+    b.weight[15, 0] = b.weight[31, 0] = -torch.inf
+    b.weight[16:, 1] = -torch.inf
+    b.weight[0, 1] = -torch.inf
+    b.weight[:, 2] = -torch.inf
+    for causal in (True, False):
+        o, lse = la.prompt_attn(q, k, v, cu_q, cu_k, causal=causal, want_lse=True, bias=b)
+        assert bool((o[:, 2] == 0).all()) and bool((lse[:, 2] == -torch.inf).all())
+        R.check(o, lse, G.forward(q, k, v, lq, lk, causal, bias=b), f"hidden, causal {causal}")
+    to = b.bucket.clone()
+    to[::3] = 32
+    to[1::5] = -7
+    b = la.RelativeBias(rel(4, 20).weight, to, b.lo)
+    o, lse = la.prompt_attn(q, k, v, cu_q, cu_k, causal=False, want_lse=True, bias=b)
+    R.check(o, lse, G.forward(q, k, v, lq, lk, False, bias=b), "buckets outside the weights")
+
+
+def test_large_biases_scales_and_bf16_weights():
+    lq = [150, 400]
+    q, k, v = make(lq, lq, 4, 2, 128, 21, qscale=1.0)
+    cu = R.starts(lq)
+    b = rel(4, 22, dtype=torch.bfloat16)
+    for factor, scale in ((40.0, None), (1.0, 0.5), (3.0, 1e-6), (200.0, 0.02)):
+        c = b._replace(weight=b.weight * factor)
+        o, lse = la.prompt_attn(q, k, v, cu, causal=False, scale=scale, want_lse=True, bias=c)
+        R.check(o, lse, G.forward(q, k, v, lq, lq, False, scale, bias=c), f"times {factor}, scale {scale}")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_strides_and_rows_outside(d):
+    lq, spare = [70, 300, 1], 19
+    q, k, v = make(lq, lq, 6, 2, d, 23, spare=spare)
+    T, b, cu = sum(lq), rel(6, 24), R.starts(lq)
+    want = G.forward(q[:T], k[:T], v[:T], lq, lq, True, bias=b)
+    q[T:], k[T:], v[T:] = float("nan"), float("nan"), float("inf")
+    buf = torch.cat([q, k, v], 1)
+    out = torch.full((6, T + spare, d), 7.0, dtype=torch.bfloat16, device="cuda").transpose(0, 1)
+    lse = torch.full((T + spare, 6), 7.0, device="cuda")
+    la.prompt_attn(buf[:, :6], buf[:, 6:8], buf[:, 8:], cu, out=out, lse_out=lse, bias=b)
+    R.check(out[:T], lse[:T], want, "one buffer")
+    assert bool((out[T:] == 7).all()) and bool((lse[T:] == 7).all())
+
+
+def test_captured_and_replayed():
+    lq = [600, 37]
+    q, k, v = make(lq, lq, 4, 2, 64, 25)
+    cu, b = R.starts(lq), rel(4, 26)
+    ws = torch.empty(1 << 26, dtype=torch.uint8, device="cuda")
+    out = torch.empty_like(q)
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):
+        la.prompt_attn(q, k, v, cu, bias=b, ws=ws, out=out)
+    st.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        la.prompt_attn(q, k, v, cu, bias=b, ws=ws, out=out)
+    for i in range(4):
+        q.copy_(torch.randn(q.shape, device="cuda").to(torch.bfloat16))
+        b.weight.normal_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, la.prompt_attn(q, k, v, cu, bias=b)), i
