@@ -209,20 +209,30 @@ struct GradArgs {
   GradIo io;
 };
 
+// The arguments, read anew: the scalar registers that a unit needs at its ends must not be held over its loop.
+__device__ __forceinline__ GradArgs grad_args() {
+  typedef const __attribute__((address_space(4))) GradArgs CArgs;
+  CArgs* p = (CArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const GradArgs*)p;
+}
+
 // How the bias enters a wave's tile of pairs: every pair by its distance, or one number for all.
+struct FarBias {
+  int lo, hi;              // the first and last distance of the table
+  float at_lo, at_hi;      // the bias there and beyond
+};
 struct TileBias {
   bool near;
   float far;
 };
-struct FarBias {
-  float lo, hi;
-};
-__device__ __forceinline__ FarBias far_bias(const GradIo& io, const float* table) {
-  return FarBias{table[kBiasPad], table[kBiasPad + io.bias_hi - io.bias_lo]};
+__device__ __forceinline__ void far_bias(FarBias& b, const float* table) {
+  b.at_lo = table[kBiasPad];
+  b.at_hi = table[kBiasPad + b.hi - b.lo];
 }
-__device__ __forceinline__ TileBias tile_bias(const GradIo& io, const FarBias& far, int least, int most) {
-  if (most <= io.bias_lo) return TileBias{false, far.lo};
-  if (least >= io.bias_hi) return TileBias{false, far.hi};
+__device__ __forceinline__ TileBias tile_bias(const FarBias& b, int least, int most) {
+  if (most <= b.lo) return TileBias{false, b.at_lo};
+  if (least >= b.hi) return TileBias{false, b.at_hi};
   return TileBias{true, 0.f};
 }
 
@@ -236,7 +246,7 @@ __device__ __forceinline__ void lds_order() {
 // dK and dV
 
 template <int D, bool BIAS>
-__global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void key_grad_kernel(GradArgs a) {
+__global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void key_grad_kernel(GradArgs) {
   using X = Mma<D>;
   constexpr int QT = D == 128 ? 32 : 64;               // query rows of a tile
   using T = GradTile<D, QT>;
@@ -245,25 +255,35 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
   __shared__ __attribute__((aligned(1024))) unsigned char ring[4 * T::BYTES];       // Q, dO of two stages
   __shared__ __attribute__((aligned(1024))) unsigned char vtile[2 * TV::BYTES];
   __shared__ __attribute__((aligned(1024))) unsigned char stat[2 * kStatBytes];
-  const GradGeom& g = a.g;
-  const GradIo& io = a.io;
   const int P = gridDim.x;
   const int l = (blockIdx.x & 7) * (P >> 3) + (blockIdx.x >> 3);
   const int tid = threadIdx.x, lane = tid & 63;
   const int lw = __builtin_amdgcn_readfirstlane(tid >> 6);
-  if (g.cuts && tid == 0) io.cut[2 * l] = io.cut[2 * l + 1] = int4{0, 0, 0, 0};
-  uint64_t share;
-  GradWalk wk = grad_start<QT>(g, l, P, &share);
-  if (!wk.more()) return;
   const int c = lane % X::MR, lg = lane / X::MR;
   const int rbase = rows_base<D>(lane), cbase = columns_base<D>(lane);
-  const uint32_t q_stride = (uint32_t)io.q_tok * 2u, do_stride = (uint32_t)io.do_tok * 2u,
-                 v_stride = (uint32_t)io.v_tok * 2u;
+  GradWalk wk;
+  float scale_log2;
+  uint32_t q_stride, do_stride;
   uint32_t q_off[T::PER], do_off[T::PER];
+  FarBias far{0, 0, 0.f, 0.f};
+  {
+    const GradArgs a = grad_args();
+    if (a.g.cuts && tid == 0) a.io.cut[2 * l] = a.io.cut[2 * l + 1] = int4{0, 0, 0, 0};
+    uint64_t share;
+    wk = grad_start<QT>(a.g, l, P, &share);
+    if (!wk.more()) return;
+    scale_log2 = a.io.scale_log2;
+    q_stride = (uint32_t)a.io.q_tok * 2u;
+    do_stride = (uint32_t)a.io.do_tok * 2u;
+    if constexpr (BIAS) {
+      far.lo = a.io.bias_lo;
+      far.hi = a.io.bias_hi;
+    }
 #pragma unroll
-  for (int i = 0; i < T::PER; ++i) {
-    q_off[i] = grad_slot<D, QT>(lw, i, lane, q_stride);
-    do_off[i] = grad_slot<D, QT>(lw, i, lane, do_stride);
+    for (int i = 0; i < T::PER; ++i) {
+      q_off[i] = grad_slot<D, QT>(lw, i, lane, q_stride);
+      do_off[i] = grad_slot<D, QT>(lw, i, lane, do_stride);
+    }
   }
   const int w0 = 32 * lw;                              // the wave's first key of the unit
   typename X::Acc dk[D / X::MR][X::QT], dv[D / X::MR][X::QT];
@@ -271,20 +291,56 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
 
   while (wk.more()) {
     uint64_t unit_end;
-    const GradPiece pc = grad_piece<QT>(g, wk, &unit_end);
+    GradPiece pc;
+    {
+      const GradArgs a = grad_args();
+      pc = grad_piece<QT>(a.g, wk, &unit_end);
+    }
     if (pc.tb > pc.ta) {
-      const Seq q = wk.q;
-      const int n0 = wk.b * kGradRows;                 // the unit's first key
-      const int off = q.lk - q.lq;
-      const int nq = (q.lq + QT - 1) / QT;
-      const int seen = (int)(grad_seen(wk.line, wk.b) / QT);
-      const int first = nq - seen;                     // first query tile that sees a key of the unit
+      const int lq = wk.q.lq, off = wk.q.lk - wk.q.lq;
+      const int key0 = wk.b * kGradRows + w0;          // the wave's first key
+      const int seen = __builtin_amdgcn_readfirstlane((int)(grad_seen(wk.line, wk.b) / QT));
+      const int first = (lq + QT - 1) / QT - seen;     // first query tile that sees a key of the unit
       // the inner tiles are the `seen` tiles of each head in turn
       int64_t left = seen == 0 ? 0 : pc.tb - pc.ta;
-      int head = seen == 0 ? 0 : (int)(pc.ta / seen);
-      int tile = seen == 0 ? 0 : (int)(pc.ta - (int64_t)head * seen);
+      int head = __builtin_amdgcn_readfirstlane(seen == 0 ? 0 : (int)(pc.ta / seen));       // of the present tile
+      int tile = __builtin_amdgcn_readfirstlane(seen == 0 ? 0 : (int)(pc.ta - (int64_t)head * seen));
+      // the tile to load next, and where its rows are
+      int next_head = head, next_tile = tile;
+      uint64_t next_q, next_do, next_stat;
+      auto seek = [&]() {
+        const GradArgs a = grad_args();
+        const int64_t tok = (int64_t)wk.q.q0 + (first + next_tile) * QT;
+        const int qh = wk.h * a.g.G + next_head;
+        next_q = first_lane_u64((uint64_t)(uintptr_t)a.io.q + (uint64_t)(tok * a.io.q_tok + qh * a.io.q_head) * 2u);
+        next_do = first_lane_u64((uint64_t)(uintptr_t)a.io.dout + (uint64_t)(tok * a.io.do_tok + qh * a.io.do_head) * 2u);
+        next_stat = first_lane_u64((uint64_t)(uintptr_t)a.io.stat + ((uint64_t)qh * (uint32_t)a.g.Tq + (uint64_t)tok) * 8u);
+      };
+      auto issue = [&](int st) {
+        const uint32_t rows = (uint32_t)min(lq - (first + next_tile) * QT, QT);
+        unsigned char* dst = ring + st * (2 * T::BYTES) + lw * (T::BYTES / 4);
+        grad_issue<D, QT>(dst, nullptr, first_lane_u64(next_q), __builtin_amdgcn_readfirstlane(rows * q_stride), q_off);
+        grad_issue<D, QT>(dst + T::BYTES, nullptr, first_lane_u64(next_do), __builtin_amdgcn_readfirstlane(rows * do_stride), do_off);
+        // whole words of 16 bytes: the row behind an odd number of them is masked
+        if (lw == 0)
+          stat_issue(stat + st * kStatBytes, nullptr, first_lane_u64(next_stat), __builtin_amdgcn_readfirstlane((rows + 1) / 2 * 16u), lane);
+        if (++next_tile < seen) {
+          next_q += (uint64_t)QT * q_stride;
+          next_do += (uint64_t)QT * do_stride;
+          next_stat += QT * 8;
+        } else {
+          next_tile = 0;
+          ++next_head;
+          seek();
+        }
+      };
       __syncthreads();                                 // the piece before is read
+      const float* table = nullptr;                    // the bias of the present head
       {
+        const GradArgs a = grad_args();
+        const Seq& q = wk.q;
+        const int n0 = wk.b * kGradRows;
+        const uint32_t v_stride = (uint32_t)a.io.v_tok * 2u;
         uint32_t v_off[TV::PER];
 #pragma unroll
         for (int i = 0; i < TV::PER; ++i) v_off[i] = grad_slot<D, 64>(lw, i, lane, v_stride);
@@ -293,72 +349,79 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
           const int k0 = n0 + 64 * half;
           const uint32_t nrec = __builtin_amdgcn_readfirstlane((uint32_t)min(max(q.lk - k0, 0), 64) * v_stride);
           const uint64_t at =
-              first_lane_u64((uint64_t)(((int64_t)q.k0 + k0) * io.v_tok + (int64_t)wk.h * io.v_head) * 2u);
-          grad_issue<D, 64>(vtile + half * TV::BYTES + lw * (TV::BYTES / 4), io.v, at, nrec, v_off);
+              first_lane_u64((uint64_t)(((int64_t)q.k0 + k0) * a.io.v_tok + (int64_t)wk.h * a.io.v_head) * 2u);
+          grad_issue<D, 64>(vtile + half * TV::BYTES + lw * (TV::BYTES / 4), a.io.v, at, nrec, v_off);
         }
-      }
-      auto issue = [&](int h, int t, int st) {
-        const int row = t * QT, qh = wk.h * g.G + h;
-        const int rows = min(q.lq - row, QT);
-        const uint64_t tok = (uint64_t)q.q0 + row;
-        unsigned char* dst = ring + st * (2 * T::BYTES) + lw * (T::BYTES / 4);
-        grad_issue<D, QT>(dst, io.q, first_lane_u64((uint64_t)((int64_t)tok * io.q_tok + (int64_t)qh * io.q_head) * 2u),
-                          __builtin_amdgcn_readfirstlane((uint32_t)rows * q_stride), q_off);
-        grad_issue<D, QT>(dst + T::BYTES, io.dout,
-                          first_lane_u64((uint64_t)((int64_t)tok * io.do_tok + (int64_t)qh * io.do_head) * 2u),
-                          __builtin_amdgcn_readfirstlane((uint32_t)rows * do_stride), do_off);
-        // whole words of 16 bytes: the row behind an odd number of them is masked
-        if (lw == 0)
-          stat_issue(stat + st * kStatBytes, io.stat, first_lane_u64(((uint64_t)qh * (uint32_t)g.Tq + tok) * 8u),
-                     __builtin_amdgcn_readfirstlane((uint32_t)(rows + 1) / 2 * 16u), lane);
-      };
-      if (left > 0) issue(head, first + tile, 0);
-#pragma unroll
-      for (int kc = 0; kc < X::QT; ++kc) {
-        const int n = n0 + w0 + X::MR * kc + c;
-        const uint16_t* src = io.k + ((int64_t)q.k0 + n) * io.k_tok + (int64_t)wk.h * io.k_head + 8 * lg;
-#pragma unroll
-        for (int ks = 0; ks < D / X::KC; ++ks) {
-          u32x4 w = u32x4{0u, 0u, 0u, 0u};
-          if (n < q.lk) w = *(const u32x4*)(src + X::KC * ks);
-          kreg[ks][kc] = __builtin_bit_cast(bf16x8, w);
+        if (left > 0) {
+          seek();
+          issue(0);
+        }
+        if constexpr (BIAS) {
+          table = a.io.table + (int64_t)(wk.h * a.g.G + head) * a.io.bias_pitch;
+          far_bias(far, table);
         }
 #pragma unroll
-        for (int dt = 0; dt < D / X::MR; ++dt)
+        for (int kc = 0; kc < X::QT; ++kc) {
+          const int n = key0 + X::MR * kc + c;
+          const uint16_t* src = a.io.k + ((int64_t)q.k0 + n) * a.io.k_tok + (int64_t)wk.h * a.io.k_head + 8 * lg;
 #pragma unroll
-          for (int i = 0; i < X::AR; ++i) dk[dt][kc][i] = dv[dt][kc][i] = 0.f;
+          for (int ks = 0; ks < D / X::KC; ++ks) {
+            u32x4 w = u32x4{0u, 0u, 0u, 0u};
+            if (n < q.lk) w = *(const u32x4*)(src + X::KC * ks);
+            kreg[ks][kc] = __builtin_bit_cast(bf16x8, w);
+          }
+#pragma unroll
+          for (int dt = 0; dt < D / X::MR; ++dt)
+#pragma unroll
+            for (int i = 0; i < X::AR; ++i) dk[dt][kc][i] = dv[dt][kc][i] = 0.f;
+        }
       }
-      const bool here = n0 + w0 < q.lk;                // the wave has keys
-      const float* table = nullptr;                    // the bias of the present head
-      FarBias far{0.f, 0.f};
+      // rows before this one see none of the wave's keys, those from it on all of them
+      const bool causal = grad_args().g.causal;
+      const int from = key0 < wk.q.lk ? (causal ? key0 - off : 0) : 0x7fffffff;
+      const int whole_from = causal ? key0 + 31 - off : 0;
       for (int st = 0; left > 0; --left, st ^= 1) {
         __builtin_amdgcn_s_waitcnt(0);
         phase_barrier();
         const int row0 = (first + tile) * QT;
         if constexpr (BIAS) {
-          if (table == nullptr || tile == 0) {
-            table = io.table + (int64_t)(wk.h * g.G + head) * io.bias_pitch;
-            far = far_bias(io, table);
+          if (tile == 0) {
+            const GradArgs a = grad_args();
+            table = a.io.table + (int64_t)(wk.h * a.g.G + head) * a.io.bias_pitch;
+            far_bias(far, table);
           }
         }
         if (++tile == seen) {
           tile = 0;
           ++head;
         }
-        if (left > 1) issue(head, first + tile, st ^ 1);
-        // rows [row0, row0 + QT) and keys [key0, key0 + 32)
-        const int key0 = n0 + w0;
-        if (!here || (g.causal && row0 + QT - 1 + off < key0)) continue;
+        if (left > 1) issue(st ^ 1);
+        if (row0 + (QT - 1) < from) continue;
         const unsigned char* qt = ring + st * (2 * T::BYTES);
         const unsigned char* dt = qt + T::BYTES;
         typename X::Acc s[NT][X::QT], dp[NT][X::QT];
         rows_product<D, NT>(qt, kreg, s, rbase);
-        tiles_product<D, NT>(dt, vtile + (w0 >> 6) * TV::BYTES + (w0 & 63) * (2 * D), dp, rbase, rbase);
-        TileBias bias{false, 0.f};
+        float to_log2 = scale_log2, shift = 0.f;
         if constexpr (BIAS) {
-          bias = tile_bias(io, far, key0 - (row0 + QT - 1 + off), key0 + 31 - (row0 + off));
+          const TileBias bias = tile_bias(far, key0 - (row0 + QT - 1 + off), key0 + 31 - (row0 + off));
+          shift = bias.far;
+          if (bias.near) {
+            to_log2 = 1.0f;
+            const float* at0 = table + (key0 + c - (row0 + 4 * lg + 3 + off) - far.lo + kBiasPad);
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+              for (int kc = 0; kc < X::QT; ++kc)
+#pragma unroll
+                for (int i = 0; i < X::AR; i += 4) {
+                  const float* at = at0 + (X::MR * kc - X::MR * t - X::acc_row(i));
+#pragma unroll
+                  for (int j = 0; j < 4; ++j)
+                    s[t][kc][i + j] = __builtin_fmaf(s[t][kc][i + j], scale_log2, at[3 - j]);
+                }
+          }
         }
-        const bool open = row0 + QT > q.lq || (g.causal && key0 + 31 > row0 + off);
+        tiles_product<D, NT>(dt, vtile + (w0 >> 6) * TV::BYTES + (w0 & 63) * (2 * D), dp, rbase, rbase);
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -368,28 +431,33 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
             const f32x4 s23 = *(const f32x4*)(stat + st * kStatBytes + 8 * r + 16);
             const float lse[4] = {s01[0], s01[2], s23[0], s23[2]}, delta[4] = {s01[1], s01[3], s23[1], s23[3]};
 #pragma unroll
-            for (int kc = 0; kc < X::QT; ++kc) {
-              f32x4 b = f32x4{0.f, 0.f, 0.f, 0.f};
-              const int n = key0 + X::MR * kc + c;
-              if (BIAS && bias.near) {
-                const float* at = table + (n - (row0 + r + 3 + off) - io.bias_lo + kBiasPad);
-                b = f32x4{at[3], at[2], at[1], at[0]};
-              }
+            for (int j = 0; j < 4; ++j) {
+              const float m = BIAS ? lse[j] - shift : lse[j];
 #pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                float m = lse[j];
-                if constexpr (BIAS) m -= bias.near ? b[j] : bias.far;
-                float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][kc][i + j], io.scale_log2, -m));
-                float ds = p * (dp[t][kc][i + j] - delta[j]);
-                if (open) {
-                  const int row = row0 + r + j;
-                  if (row >= q.lq || (g.causal && n > row + off)) p = ds = 0.f;
-                }
+              for (int kc = 0; kc < X::QT; ++kc) {
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][kc][i + j], to_log2, -m));
                 s[t][kc][i + j] = p;
-                dp[t][kc][i + j] = ds;
+                dp[t][kc][i + j] = p * (dp[t][kc][i + j] - delta[j]);
               }
             }
           }
+        if (__builtin_expect(row0 + QT > lq || row0 < whole_from, 0)) {
+          // rows that do not exist, whatever their statistics are, and pairs that do not see each other
+          const int end = lq - row0 - 4 * lg;
+#pragma unroll
+          for (int kc = 0; kc < X::QT; ++kc) {
+            const int begin = causal ? key0 + X::MR * kc + c - off - row0 - 4 * lg : 0;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+              for (int i = 0; i < X::AR; ++i) {
+                const int r = X::MR * t + X::acc_row(i);
+                const bool none = (r >= end) | (causal & (r < begin));
+                s[t][kc][i] = none ? 0.f : s[t][kc][i];
+                dp[t][kc][i] = none ? 0.f : dp[t][kc][i];
+              }
+          }
+        }
         bf16x8 op[QT / X::KC][X::QT];
         as_operand<D, NT>(s, op);
         columns_product<D, QT / X::KC>(dt, op, dv, cbase);
@@ -397,25 +465,28 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
         columns_product<D, QT / X::KC>(qt, op, dk, cbase);
       }
       __builtin_amdgcn_s_waitcnt(0);                   // V, where nothing saw the unit
+      const GradArgs a = grad_args();
       const bool whole = pc.ta == 0 && pc.tb == pc.n;
       const int slot = 2 * l + (pc.ta == 0 ? 1 : 0);
-      if (!whole && tid == 0) io.cut[slot] = int4{q.k0 + n0, min(kGradRows, q.lk - n0), wk.h, 1};
+      const int n0 = wk.b * kGradRows;
+      if (!whole && tid == 0) a.io.cut[slot] = int4{wk.q.k0 + n0, min(kGradRows, wk.q.lk - n0), wk.h, 1};
 #pragma unroll
       for (int kc = 0; kc < X::QT; ++kc) {
         const int r = w0 + X::MR * kc + c;
         if (whole) {
-          const bool ok = n0 + r < q.lk;
-          const int64_t tok = (int64_t)q.k0 + n0 + r;
-          store_rows<D>(dk, kc, io.scale, ok, io.out0 + tok * io.out0_tok + (int64_t)wk.h * io.out0_head, lg);
-          store_rows<D>(dv, kc, 1.0f, ok, io.out1 + tok * io.out1_tok + (int64_t)wk.h * io.out1_head, lg);
+          const bool ok = n0 + r < wk.q.lk;
+          const int64_t tok = (int64_t)wk.q.k0 + n0 + r;
+          store_rows<D>(dk, kc, a.io.scale, ok, a.io.out0 + tok * a.io.out0_tok + (int64_t)wk.h * a.io.out0_head, lg);
+          store_rows<D>(dv, kc, 1.0f, ok, a.io.out1 + tok * a.io.out1_tok + (int64_t)wk.h * a.io.out1_head, lg);
         } else {
-          float* dst = io.part + ((size_t)slot * 2 * kGradRows + r) * D;
+          float* dst = a.io.part + ((size_t)slot * 2 * kGradRows + r) * D;
           store_part<D>(dk, kc, dst, lg);
           store_part<D>(dv, kc, dst + (size_t)kGradRows * D, lg);
         }
       }
     }
-    grad_on<QT>(g, wk, unit_end);
+    const GradArgs a = grad_args();
+    grad_on<QT>(a.g, wk, unit_end);
   }
 }
 
@@ -479,40 +550,54 @@ __device__ __forceinline__ void add_diagonals(const typename Mma<D>::Acc (*x)[Mm
 }
 
 template <int D, bool BIAS>
-__global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void row_grad_kernel(GradArgs a) {
+__global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void row_grad_kernel(GradArgs) {
   using X = Mma<D>;
   constexpr int NT = KT / X::MR;
   using T = GradTile<D, KT>;
   __shared__ __attribute__((aligned(1024))) unsigned char ring[4 * T::BYTES];       // K, V of two stages
   __shared__ __attribute__((aligned(16))) float block[BIAS ? 4 : 1][BIAS ? 256 : 4];
   __shared__ float sums[BIAS ? 4 : 1][BIAS ? kBiasPitch : 1];
-  const GradGeom& g = a.g;
-  const GradIo& io = a.io;
   const int P = gridDim.x;
   const int l = (blockIdx.x & 7) * (P >> 3) + (blockIdx.x >> 3);
   const int tid = threadIdx.x, lane = tid & 63;
   const int lw = __builtin_amdgcn_readfirstlane(tid >> 6);
-  if (g.cuts && tid == 0) io.cut[2 * l] = io.cut[2 * l + 1] = int4{0, 0, 0, 0};
-  uint64_t share;
-  GradWalk wk = grad_start<0>(g, l, P, &share);
-  if (BIAS && blockIdx.x == 0 && tid == 0) {
-    io.line[0] = wk.head;
-    io.line[1] = share;
-  }
-  // a stretch that its borders' moving left empty still writes its heads' sums
-  if (!wk.more() && !(BIAS && (uint64_t)(uint32_t)l * share < wk.head * (uint32_t)g.NH)) return;
-  // the heads whose sums this workgroup writes
-  int sum_head = 0, last_head = 0;
-  float far_lo = 0.f, far_hi = 0.f;
-  if constexpr (BIAS) {
-    sum_head = (int)((uint64_t)(uint32_t)l * share / wk.head);
-    last_head = (int)((wk.end - 1) / wk.head);
-    for (int i = tid; i < 4 * kBiasPitch; i += kGradThreads) (&sums[0][0])[i] = 0.f;
-    __syncthreads();
+  GradWalk wk;
+  float scale_log2;
+  FarBias far{0, 0, 0.f, 0.f};
+  int sum_head = 0, last_head = 0;       // the heads whose sums this workgroup writes
+  float far_lo = 0.f, far_hi = 0.f;      // the lane's sums of dS beyond the table's ends
+  uint32_t k_stride, v_stride;
+  {
+    const GradArgs a = grad_args();
+    if (a.g.cuts && tid == 0) a.io.cut[2 * l] = a.io.cut[2 * l + 1] = int4{0, 0, 0, 0};
+    uint64_t share;
+    wk = grad_start<0>(a.g, l, P, &share);
+    scale_log2 = a.io.scale_log2;
+    k_stride = (uint32_t)a.io.k_tok * 2u;
+    v_stride = (uint32_t)a.io.v_tok * 2u;
+    if constexpr (BIAS) {
+      if (blockIdx.x == 0 && tid == 0) {
+        a.io.line[0] = wk.head;
+        a.io.line[1] = share;
+      }
+      // a stretch that its borders' moving left empty still writes its heads' sums
+      if ((uint64_t)(uint32_t)l * share >= wk.head * (uint32_t)a.g.NH) return;
+      far.lo = a.io.bias_lo;
+      far.hi = a.io.bias_hi;
+      sum_head = (int)((uint64_t)(uint32_t)l * share / wk.head);
+      last_head = (int)((wk.end - 1) / wk.head);
+      for (int i = tid; i < 4 * kBiasPitch; i += kGradThreads) (&sums[0][0])[i] = 0.f;
+      __syncthreads();
+    } else if (!wk.more()) {
+      return;
+    }
   }
   // writes the sums of the heads before `until`
   auto flush = [&](int until) {
     if constexpr (BIAS) {
+      if (sum_head >= until) return;
+      const GradArgs a = grad_args();
+      const int pitch = a.io.bias_pitch;
       for (; sum_head < until; ++sum_head) {
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) {
@@ -521,12 +606,12 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
         }
         if (lane == 0) {
           sums[lw][0] += far_lo;
-          sums[lw][io.bias_pitch - 1] += far_hi;
+          sums[lw][pitch - 1] += far_hi;
         }
         far_lo = far_hi = 0.f;
         __syncthreads();
-        float* dst = io.dist + (size_t)(l + sum_head) * io.bias_pitch;
-        for (int i = tid; i < io.bias_pitch; i += kGradThreads) {
+        float* dst = a.io.dist + (size_t)(l + sum_head) * pitch;
+        for (int i = tid; i < pitch; i += kGradThreads) {
           dst[i] = (sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]);
           sums[0][i] = sums[1][i] = sums[2][i] = sums[3][i] = 0.f;
         }
@@ -536,7 +621,6 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
   };
   const int c = lane % X::MR, lg = lane / X::MR;
   const int rbase = rows_base<D>(lane), cbase = columns_base<D>(lane);
-  const uint32_t k_stride = (uint32_t)io.k_tok * 2u, v_stride = (uint32_t)io.v_tok * 2u;
   uint32_t k_off[T::PER], v_off[T::PER];
 #pragma unroll
   for (int i = 0; i < T::PER; ++i) {
@@ -549,63 +633,81 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
 
   while (wk.more()) {
     uint64_t unit_end;
-    const GradPiece pc = grad_piece<KT>(g, wk, &unit_end);
+    GradPiece pc;
+    {
+      const GradArgs a = grad_args();
+      pc = grad_piece<KT>(a.g, wk, &unit_end);
+    }
     if (pc.tb > pc.ta) {
-      const Seq q = wk.q;
-      const int off = q.lk - q.lq;
-      const int kvh = wk.h / g.GS, head0 = wk.h % g.GS * g.GH;         // the unit's heads within the group
-      const int heads = min(g.GH, g.G - head0);
-      const int t0 = wk.b * g.TB, tokens = min(g.TB, q.lq - t0);
-      if constexpr (BIAS) flush(wk.h);
-      __syncthreads();                                 // the piece before is read
+      const int lk = wk.q.lk, off = wk.q.lk - wk.q.lq;
       const int keys = (int)grad_seen(wk.line, wk.b);  // keys that the unit's last token sees
       const int first = (int)pc.ta, N = keys == 0 ? 0 : (int)(pc.tb - pc.ta);
-      auto issue = [&](int t, int st) {
-        const int k0 = 64 * t;
-        const int rows = min(q.lk - k0, 64);
+      if constexpr (BIAS) flush(wk.h);
+      __syncthreads();                                 // the piece before is read
+      uint64_t next_k = 0, next_v = 0;                 // where the tile to load next starts
+      int next_left = 0;                               // keys from it on
+      auto issue = [&](int st) {
+        const uint32_t rows = (uint32_t)min(next_left, KT);
         unsigned char* dst = ring + st * (2 * T::BYTES) + lw * (T::BYTES / 4);
-        const int64_t tok = (int64_t)q.k0 + k0;
-        grad_issue<D, KT>(dst, io.k, first_lane_u64((uint64_t)(tok * io.k_tok + (int64_t)kvh * io.k_head) * 2u),
-                          __builtin_amdgcn_readfirstlane((uint32_t)rows * k_stride), k_off);
-        grad_issue<D, KT>(dst + T::BYTES, io.v,
-                          first_lane_u64((uint64_t)(tok * io.v_tok + (int64_t)kvh * io.v_head) * 2u),
-                          __builtin_amdgcn_readfirstlane((uint32_t)rows * v_stride), v_off);
+        grad_issue<D, KT>(dst, nullptr, first_lane_u64(next_k), __builtin_amdgcn_readfirstlane(rows * k_stride), k_off);
+        grad_issue<D, KT>(dst + T::BYTES, nullptr, first_lane_u64(next_v), __builtin_amdgcn_readfirstlane(rows * v_stride), v_off);
+        next_k += (uint64_t)KT * k_stride;
+        next_v += (uint64_t)KT * v_stride;
+        next_left -= KT;
       };
-      if (N > 0) issue(first, 0);
       float lse[X::QT], delta[X::QT];
       int limit[X::QT], wave_keys = 0, wave_open = 0x7fffffff;
-      int row_at[X::QT];                               // the token, or -1
-#pragma unroll
-      for (int qc = 0; qc < X::QT; ++qc) {
-        const int r = w0 + X::MR * qc + c;
-        const int t = (int)(((uint32_t)r * (uint32_t)g.gh_magic) >> 16), j = r - t * g.GH;
-        const bool ok = t < tokens && j < heads;
-        const int token = t0 + t, head = kvh * g.G + head0 + j;
-        row_at[qc] = ok ? token : -1;
-        const int64_t tok = (int64_t)q.q0 + token;
-        const uint16_t* qs = io.q + tok * io.q_tok + (int64_t)head * io.q_head + 8 * lg;
-        const uint16_t* ds = io.dout + tok * io.do_tok + (int64_t)head * io.do_head + 8 * lg;
-#pragma unroll
-        for (int ks = 0; ks < D / X::KC; ++ks) {
-          u32x4 w = u32x4{0u, 0u, 0u, 0u}, x = w;
-          if (ok) {
-            w = *(const u32x4*)(qs + X::KC * ks);
-            x = *(const u32x4*)(ds + X::KC * ks);
-          }
-          qreg[ks][qc] = __builtin_bit_cast(bf16x8, w);
-          doreg[ks][qc] = __builtin_bit_cast(bf16x8, x);
+      const float* table = nullptr;
+      int least_pos = 0;                               // place of the wave's first query among the keys
+      {
+        const GradArgs a = grad_args();
+        const Seq& q = wk.q;
+        const int kvh = wk.h / a.g.GS, head0 = wk.h % a.g.GS * a.g.GH;       // the unit's heads within the group
+        const int heads = min(a.g.GH, a.g.G - head0);
+        const int t0 = wk.b * a.g.TB, tokens = min(a.g.TB, q.lq - t0);
+        if (N > 0) {
+          const int64_t tok = (int64_t)q.k0 + 64 * (int64_t)first;
+          next_k = first_lane_u64((uint64_t)(uintptr_t)a.io.k + (uint64_t)(tok * a.io.k_tok + kvh * a.io.k_head) * 2u);
+          next_v = first_lane_u64((uint64_t)(uintptr_t)a.io.v + (uint64_t)(tok * a.io.v_tok + kvh * a.io.v_head) * 2u);
+          next_left = lk - 64 * first;
+          issue(0);
         }
-        float2 z = float2{INFINITY, 0.f};
-        if (ok) z = io.stat[(uint64_t)head * (uint32_t)g.Tq + (uint64_t)tok];
-        lse[qc] = z.x;
-        delta[qc] = z.y;
-        limit[qc] = ok ? (g.causal ? max(0, min(q.lk, off + token + 1)) : q.lk) : 0x7fffffff;
-        wave_keys = max(wave_keys, ok ? limit[qc] : 0);
-        wave_open = min(wave_open, limit[qc]);
+        if constexpr (BIAS) {
+          table = a.io.table + (int64_t)(kvh * a.g.G + head0) * a.io.bias_pitch;
+          far_bias(far, table);
+          least_pos = off + t0 + w0;
+        }
 #pragma unroll
-        for (int dt = 0; dt < D / X::MR; ++dt)
+        for (int qc = 0; qc < X::QT; ++qc) {
+          const int r = w0 + X::MR * qc + c;
+          const int t = (int)(((uint32_t)r * (uint32_t)a.g.gh_magic) >> 16), j = r - t * a.g.GH;
+          const bool ok = t < tokens && j < heads;
+          const int token = t0 + t, head = kvh * a.g.G + head0 + j;
+          const int64_t tok = (int64_t)q.q0 + token;
+          const uint16_t* qs = a.io.q + tok * a.io.q_tok + (int64_t)head * a.io.q_head + 8 * lg;
+          const uint16_t* ds = a.io.dout + tok * a.io.do_tok + (int64_t)head * a.io.do_head + 8 * lg;
 #pragma unroll
-          for (int i = 0; i < X::AR; ++i) dq[dt][qc][i] = 0.f;
+          for (int ks = 0; ks < D / X::KC; ++ks) {
+            u32x4 w = u32x4{0u, 0u, 0u, 0u}, x = w;
+            if (ok) {
+              w = *(const u32x4*)(qs + X::KC * ks);
+              x = *(const u32x4*)(ds + X::KC * ks);
+            }
+            qreg[ks][qc] = __builtin_bit_cast(bf16x8, w);
+            doreg[ks][qc] = __builtin_bit_cast(bf16x8, x);
+          }
+          float2 z = float2{INFINITY, 0.f};
+          if (ok) z = a.io.stat[(uint64_t)head * (uint32_t)a.g.Tq + (uint64_t)tok];
+          lse[qc] = z.x;
+          delta[qc] = z.y;
+          limit[qc] = ok ? (a.g.causal ? max(0, min(lk, off + token + 1)) : lk) : 0x7fffffff;
+          wave_keys = max(wave_keys, ok ? limit[qc] : 0);
+          wave_open = min(wave_open, limit[qc]);
+#pragma unroll
+          for (int dt = 0; dt < D / X::MR; ++dt)
+#pragma unroll
+            for (int i = 0; i < X::AR; ++i) dq[dt][qc][i] = 0.f;
+        }
       }
 #pragma unroll
       for (int m = 1; m < X::MR; m <<= 1) {
@@ -614,54 +716,59 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
       }
       wave_keys = __builtin_amdgcn_readfirstlane(wave_keys);       // keys that some row of the wave sees
       wave_open = __builtin_amdgcn_readfirstlane(wave_open);       // and that all of them see
-      const float* table = nullptr;
-      FarBias far{0.f, 0.f};
-      int least_pos = 0;                               // place of the wave's first query among the keys
-      if constexpr (BIAS) {
-        table = io.table + (int64_t)(kvh * g.G + head0) * io.bias_pitch;
-        far = far_bias(io, table);
-        least_pos = off + t0 + w0;
-      }
-      for (int i = 0, st = 0; i < N; ++i, st ^= 1) {
+      int key0 = 64 * first;
+      for (int left = N, st = 0; left > 0; --left, st ^= 1, key0 += KT) {
         __builtin_amdgcn_s_waitcnt(0);
         phase_barrier();
-        if (i + 1 < N) issue(first + i + 1, st ^ 1);
-        const int key0 = 64 * (first + i);
+        if (left > 1) issue(st ^ 1);
         if (key0 >= wave_keys) continue;
         const unsigned char* kt = ring + st * (2 * T::BYTES);
         typename X::Acc s[NT][X::QT], dp[NT][X::QT];
         rows_product<D, NT>(kt, qreg, s, rbase);
+        float to_log2 = scale_log2, shift = 0.f;
+        bool near = false;
+        if constexpr (BIAS) {
+          const TileBias bias = tile_bias(far, key0 - (least_pos + 31), key0 + 63 - least_pos);
+          shift = bias.far;
+          near = bias.near;
+          if (near) {
+            to_log2 = 1.0f;
+            const float* at = table + (key0 + 4 * lg - (least_pos + c) - far.lo + kBiasPad);
+#pragma unroll
+            for (int qc = 0; qc < X::QT; ++qc)
+#pragma unroll
+              for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < X::AR; ++i)
+                  s[t][qc][i] = __builtin_fmaf(s[t][qc][i], scale_log2, at[X::MR * t + X::acc_row(i) - X::MR * qc]);
+          }
+        }
         rows_product<D, NT>(kt + T::BYTES, doreg, dp, rbase);
-        TileBias bias{false, 0.f};
-        if constexpr (BIAS) bias = tile_bias(io, far, key0 - (least_pos + 31), key0 + 63 - least_pos);
-        const bool open = key0 + 64 > wave_open;
 #pragma unroll
         for (int qc = 0; qc < X::QT; ++qc) {
-          const float m = BIAS && !bias.near ? lse[qc] - bias.far : lse[qc];
-          const int lim = limit[qc] - key0;
+          const float m = BIAS ? lse[qc] - shift : lse[qc];
 #pragma unroll
           for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int e = 0; e < X::AR; e += 4) {
-              const int r = X::MR * t + X::acc_row(e) + 4 * lg;
-              f32x4 b = f32x4{0.f, 0.f, 0.f, 0.f};
-              if (BIAS && bias.near) {
-                const float* at = table + (key0 + r - (least_pos + X::MR * qc + c) - io.bias_lo + kBiasPad);
-                b = f32x4{at[0], at[1], at[2], at[3]};
-              }
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                float mm = m;
-                if (BIAS && bias.near) mm -= b[j];
-                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][qc][e + j], io.scale_log2, -mm));
-                const float ds = p * (dp[t][qc][e + j] - delta[qc]);
-                dp[t][qc][e + j] = open && r + j >= lim ? 0.f : ds;
-              }
+            for (int i = 0; i < X::AR; ++i) {
+              const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][qc][i], to_log2, -m));
+              dp[t][qc][i] = p * (dp[t][qc][i] - delta[qc]);
             }
         }
+        if (__builtin_expect(key0 + KT > wave_open, 0)) {
+#pragma unroll
+          for (int qc = 0; qc < X::QT; ++qc) {
+            const int lim = limit[qc] - key0 - 4 * lg;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+              for (int i = 0; i < X::AR; ++i)
+                if (X::MR * t + X::acc_row(i) >= lim) dp[t][qc][i] = 0.f;
+          }
+        }
         if constexpr (BIAS) {
-          if (bias.near) {
-            add_diagonals<D>(dp, block[lw], sums[lw], key0 - least_pos - io.bias_lo + kBiasPad, lane);
+          if (near) {
+            add_diagonals<D>(dp, block[lw], sums[lw], key0 - least_pos - far.lo + kBiasPad, lane);
           } else {
             float x = 0.f;
 #pragma unroll
@@ -669,8 +776,8 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
 #pragma unroll
               for (int qc = 0; qc < X::QT; ++qc)
 #pragma unroll
-                for (int e = 0; e < X::AR; ++e) x += dp[t][qc][e];
-            if (key0 + 63 - least_pos <= io.bias_lo) far_lo += x;
+                for (int i = 0; i < X::AR; ++i) x += dp[t][qc][i];
+            if (key0 + 63 - least_pos <= far.lo) far_lo += x;
             else far_hi += x;
           }
         }
@@ -678,22 +785,28 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
         as_operand<D, NT>(dp, op);
         columns_product<D, KT / X::KC>(kt, op, dq, cbase);
       }
+      const GradArgs a = grad_args();
       const bool whole = pc.ta == 0 && pc.tb == pc.n;
       const int slot = 2 * l + (pc.ta == 0 ? 1 : 0);
-      if (!whole && tid == 0) io.cut[slot] = int4{q.q0 + t0, tokens, kvh * g.G + head0, heads};
+      const int kvh = wk.h / a.g.GS, head0 = wk.h % a.g.GS * a.g.GH;
+      const int heads = min(a.g.GH, a.g.G - head0);
+      const int t0 = wk.b * a.g.TB, tokens = min(a.g.TB, wk.q.lq - t0);
+      if (!whole && tid == 0) a.io.cut[slot] = int4{wk.q.q0 + t0, tokens, kvh * a.g.G + head0, heads};
 #pragma unroll
       for (int qc = 0; qc < X::QT; ++qc) {
         const int r = w0 + X::MR * qc + c;
-        const int t = (int)(((uint32_t)r * (uint32_t)g.gh_magic) >> 16), j = r - t * g.GH;
+        const int t = (int)(((uint32_t)r * (uint32_t)a.g.gh_magic) >> 16), j = r - t * a.g.GH;
         if (whole)
-          store_rows<D>(dq, qc, io.scale, row_at[qc] >= 0,
-                        io.out0 + ((int64_t)q.q0 + t0 + t) * io.out0_tok + (int64_t)(kvh * g.G + head0 + j) * io.out0_head,
+          store_rows<D>(dq, qc, a.io.scale, t < tokens && j < heads,
+                        a.io.out0 + ((int64_t)wk.q.q0 + t0 + t) * a.io.out0_tok +
+                            (int64_t)(kvh * a.g.G + head0 + j) * a.io.out0_head,
                         lg);
         else
-          store_part<D>(dq, qc, io.part + ((size_t)slot * kGradRows + r) * D, lg);
+          store_part<D>(dq, qc, a.io.part + ((size_t)slot * kGradRows + r) * D, lg);
       }
     }
-    grad_on<0>(g, wk, unit_end);
+    const GradArgs a = grad_args();
+    grad_on<0>(a.g, wk, unit_end);
   }
   if constexpr (BIAS) flush(last_head + 1);
 }
