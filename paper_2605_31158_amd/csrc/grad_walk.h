@@ -127,6 +127,20 @@ __device__ __forceinline__ uint64_t grad_before(const GradGeom& g, const GradLin
   return (uint64_t)sum * w.mult + (uint64_t)b * g.extra;
 }
 
+// The j-th run of a sequence on the line, and the weight of those before it: the runs of a causal sequence come from
+// both ends in turn (see seq_walk.h).
+__device__ __forceinline__ int grad_run(const GradGeom& g, int nb, int j) {
+  return g.causal ? ((j & 1) ? j >> 1 : nb - 1 - (j >> 1)) : j;
+}
+__device__ __forceinline__ uint64_t grad_line_before(const GradGeom& g, const GradLine& w, uint64_t all, int j) {
+  if (!g.causal) return grad_before(g, w, j);
+  const int m = j >> 1;                                     // m runs of either end
+  uint64_t x = grad_before(g, w, m);
+  if (m > 0) x += all - grad_before(g, w, w.nb - m);
+  if (j & 1) x += (uint64_t)grad_seen(w, w.nb - 1 - m) * w.mult + g.extra;
+  return x;
+}
+
 __device__ __forceinline__ Seq grad_seq(const GradGeom& g, int s) {
   Seq q;
   q.q0 = min(max(g.cu_q[s], 0), g.Tq);
@@ -146,7 +160,7 @@ struct GradWalk {
   uint64_t unit0;          // where the present unit starts
   uint64_t head;           // weight of a head
   uint32_t snap, small;    // as in Walk
-  int h, s, b;             // head group, sequence, run
+  int h, s, j, b;          // head group, sequence, place of the run among the sequence's, run
   Seq q;
   GradLine line;
   __device__ __forceinline__ bool more() const { return pos < end; }
@@ -187,8 +201,11 @@ template <int QT>
 __device__ __forceinline__ void grad_on(const GradGeom& g, GradWalk& w, uint64_t unit_end) {
   w.pos = w.unit0 = unit_end;
   if (w.pos >= w.end) return;
-  if (++w.b < w.line.nb) return;
-  w.b = 0;
+  if (++w.j < w.line.nb) {
+    w.b = grad_run(g, w.line.nb, w.j);
+    return;
+  }
+  w.j = 0;
   do {
     if (++w.s >= g.S) {
       w.s = 0;
@@ -200,6 +217,7 @@ __device__ __forceinline__ void grad_on(const GradGeom& g, GradWalk& w, uint64_t
     w.q = grad_seq(g, w.s);
     w.line = grad_line<QT>(g, w.q);
   } while (w.line.nb == 0);
+  w.b = grad_run(g, w.line.nb, 0);
 }
 
 // Start of the stretch of workgroup l of P; *share is what a workgroup takes.
@@ -231,7 +249,7 @@ __device__ __forceinline__ GradWalk grad_start(const GradGeom& g, int l, int P, 
   w.end = w.pos + share < total ? w.pos + share : total;
   w.snap = !g.cuts ? ~0u : (uint32_t)(share / 64 < g.extra ? share / 64 : g.extra);
   w.small = g.cuts && share < g.whole ? 2 * (uint32_t)share : 0;
-  w.h = w.s = w.b = 0;
+  w.h = w.s = w.j = w.b = 0;
   w.unit0 = 0;
   w.q = Seq{0, 0, 0, 0};
   w.line = GradLine{0, 0, 0, 0, 0, 0, 0};
@@ -255,16 +273,17 @@ __device__ __forceinline__ GradWalk grad_start(const GradGeom& g, int l, int P, 
   w.s = s;
   const uint64_t rem = in_head - at;
   int lo = 0, n = w.line.nb;
-  while (n > 1) {                                           // the run is in [lo, lo + n)
+  while (n > 1) {                                           // the run's place is in [lo, lo + n)
     const int step = (n + 63) / 64;
     const int64_t j = (int64_t)lo + (int64_t)lane * step;
-    const bool below = j < lo + n && grad_before(g, w.line, (int)j) <= rem;
+    const bool below = j < lo + n && grad_line_before(g, w.line, ws, (int)j) <= rem;
     const int i = __popcll(__ballot(below)) - 1;            // lane 0 is always below
     lo += i * step;
     n = min(step, n - i * step);
   }
-  w.b = __builtin_amdgcn_readfirstlane(lo);
-  w.unit0 = first_lane_u64(w.head * (uint32_t)w.h + at + grad_before(g, w.line, w.b));
+  w.j = __builtin_amdgcn_readfirstlane(lo);
+  w.b = grad_run(g, w.line.nb, w.j);
+  w.unit0 = first_lane_u64(w.head * (uint32_t)w.h + at + grad_line_before(g, w.line, ws, w.j));
   const uint64_t weight = (uint64_t)grad_seen(w.line, w.b) * w.line.mult + g.extra;
   const uint32_t near = grad_near(w, weight);
   const uint64_t unit_end = w.unit0 + weight;

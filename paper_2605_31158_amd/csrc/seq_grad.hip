@@ -935,38 +935,50 @@ struct DistArgs {
   void* dweight;
   int bf16, buckets, lo, hi, pitch, Hq, P, empty;
 };
+__device__ __forceinline__ double wave_sum_f64(double x) {
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
+  return x;
+}
 __global__ __launch_bounds__(1024) void dist_merge_kernel(DistArgs a) {
+  constexpr int PARTS = 4;                // of the workgroups, by turns
+  __shared__ double parts[PARTS][kBiasPitch];
   __shared__ double sums[kBiasPitch];
   __shared__ int to[kBiasMost];
-  const int h = blockIdx.x, tid = threadIdx.x;
+  const int h = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int n = a.hi - a.lo + 1;
   const uint64_t head = a.empty ? 0 : a.line[0], share = a.empty ? 1 : a.line[1];
-  for (int i = tid; i < a.pitch; i += 1024) {
+  const int l0 = (int)(head * (uint32_t)h / share);
+  const int l1 = head == 0 ? l0 - 1 : min((int)((head * ((uint32_t)h + 1ull) - 1) / share), a.P - 1);
+  for (int j = tid; j < PARTS * a.pitch; j += 1024) {
+    const int part = j / a.pitch, i = j - part * a.pitch;
     double x = 0.0;
-    if (head > 0) {
-      const int l0 = (int)(head * (uint32_t)h / share);
-      const int l1 = min((int)((head * ((uint32_t)h + 1ull) - 1) / share), a.P - 1);
 #pragma unroll 8
-      for (int l = l0; l <= l1; ++l) x += a.dist[(size_t)(l + h) * a.pitch + i];
-    }
-    sums[i] = x;
+    for (int l = l0 + part; l <= l1; l += PARTS) x += a.dist[(size_t)(l + h) * a.pitch + i];
+    parts[part][i] = x;
   }
   for (int i = tid; i < n; i += 1024) to[i] = a.bucket[i];
   __syncthreads();
-  if (tid < 2) {                          // what lies beyond the ends belongs to them
-    double x = 0.0;
-    for (int i = 0; i < kBiasPad; ++i) x += sums[tid == 0 ? i : kBiasPad + n + i];
-    sums[tid == 0 ? 0 : kBiasPad + n] = x;
+  for (int i = tid; i < a.pitch; i += 1024) sums[i] = (parts[0][i] + parts[1][i]) + (parts[2][i] + parts[3][i]);
+  __syncthreads();
+  if (wave < 2) {                         // what lies beyond the ends belongs to them
+    const int end = wave == 0 ? 0 : kBiasPad + n;
+    double x = sums[end + lane];
+    if (lane < kBiasPad - 64) x += sums[end + 64 + lane];
+    x = wave_sum_f64(x);
+    if (lane == 0) sums[end] = x;
   }
   __syncthreads();
-  for (int b = tid; b < a.buckets; b += 1024) {
+  for (int b = wave; b < a.buckets; b += 16) {
     double x = 0.0;
-    for (int i = 0; i < n; ++i) {
+    for (int i = lane; i < n; i += 64) {
       if (to[i] != b) continue;
       x += sums[kBiasPad + i];
       if (i == 0) x += sums[0];
       if (i == n - 1) x += sums[kBiasPad + n];
     }
+    x = wave_sum_f64(x);
+    if (lane != 0) continue;
     const size_t at = (size_t)b * a.Hq + h;
     if (a.bf16) ((uint16_t*)a.dweight)[at] = (uint16_t)(pack_bf16x2((float)x, 0.f) & 0xffffu);
     else ((float*)a.dweight)[at] = (float)x;
