@@ -190,12 +190,11 @@ struct GradLayout {
   float2* stat;
   float *table, *dist;
   uint64_t* line;
-  int4* cut;
-  float* part;
+  int4 *keys_cut, *rows_cut;
+  float *keys_part, *rows_part;
   size_t bytes;
 };
 
-// The kernels run one after the other and share the scratch of their pieces.
 GradLayout grad_layout(const la_seqs& s, const la_rel_bias* bias, void* ws) {
   GradLayout w{};
   char* p = (char*)ws;
@@ -213,9 +212,11 @@ GradLayout grad_layout(const la_seqs& s, const la_rel_bias* bias, void* ws) {
     w.dist = (float*)take((rp + r.NH) * bias_pitch(bias) * sizeof(float));
     w.line = (uint64_t*)take(2 * sizeof(uint64_t));
   }
-  const size_t rcut = r.cuts ? 2 * rp : 0, kcut = k.cuts ? 2 * kp : 0, most = rcut > 2 * kcut ? rcut : 2 * kcut;
-  w.cut = (int4*)take((rcut > kcut ? rcut : kcut) * sizeof(int4));
-  w.part = (float*)take(most * kGradRows * s.d * sizeof(float));
+  const size_t rcut = r.cuts ? 2 * rp : 0, kcut = k.cuts ? 2 * kp : 0;
+  w.keys_cut = (int4*)take(kcut * sizeof(int4));
+  w.rows_cut = (int4*)take(rcut * sizeof(int4));
+  w.keys_part = (float*)take(2 * kcut * kGradRows * s.d * sizeof(float));
+  w.rows_part = (float*)take(rcut * kGradRows * s.d * sizeof(float));
   w.bytes = at;
   return w;
 }
@@ -493,8 +494,6 @@ la_status la_prompt_attn_bwd(const la_seqs* seqs, const la_prompt_grads* grads, 
   io.v_tok = s.v_token; io.v_head = s.v_head;
   io.do_tok = grads->do_token; io.do_head = grads->do_head;
   io.stat = w.stat;
-  io.part = w.part;
-  io.cut = w.cut;
   io.scale = scale > 0.0f ? scale : 1.0f / sqrtf((float)s.d);
   io.scale_log2 = io.scale * 1.4426950408889634f;
   if (bias) {
@@ -508,6 +507,10 @@ la_status la_prompt_attn_bwd(const la_seqs* seqs, const la_prompt_grads* grads, 
     c.dweight = dweight;
   }
   c.rows_io = c.keys_io = io;
+  c.rows_io.part = w.rows_part;
+  c.rows_io.cut = w.rows_cut;
+  c.keys_io.part = w.keys_part;
+  c.keys_io.cut = w.keys_cut;
   c.rows_io.out0 = (uint16_t*)dq;
   c.rows_io.out0_tok = grads->dq_token; c.rows_io.out0_head = grads->dq_head;
   c.keys_io.out0 = (uint16_t*)dk;

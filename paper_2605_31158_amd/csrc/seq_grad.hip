@@ -4,9 +4,9 @@
 //   dS = P (dP - delta);  dV = P^T dO;  dK = scale dS^T Q;  dQ = scale dS K
 // and the gradient of a bucket of the relative bias is the sum of dS over its pairs.
 //
-// Two kernels walk the pairs, so that no sum needs atomics and results repeat bit for bit: key_grad_kernel
-// holds 128 keys of a key head and goes over the queries that see them (four products, dK and dV in
-// registers), row_grad_kernel holds 128 packed query rows and goes over their keys (three, dQ in registers).
+// Two walks over the pairs, so that no sum needs atomics and results repeat bit for bit: key_grad holds 128 keys of a
+// key head and goes over the queries that see them (four products, dK and dV in registers), row_grad holds 128 packed
+// query rows and goes over their keys (three, dQ in registers).
 #include <math.h>
 
 #include <type_traits>
@@ -207,14 +207,19 @@ __device__ __forceinline__ void store_part(const typename Mma<D>::Acc (*acc)[Mma
 struct GradArgs {
   GradGeom g;
   GradIo io;
+  int P;                   // workgroups
+};
+struct GradBoth {
+  GradArgs keys, rows;
 };
 
 // The arguments, read anew: the scalar registers that a unit needs at its ends must not be held over its loop.
+template <bool KEYS>
 __device__ __forceinline__ GradArgs grad_args() {
-  typedef const __attribute__((address_space(4))) GradArgs CArgs;
+  typedef const __attribute__((address_space(4))) GradBoth CArgs;
   CArgs* p = (CArgs*)__builtin_amdgcn_kernarg_segment_ptr();
   asm volatile("" : "+s"(p));
-  return *(const GradArgs*)p;
+  return KEYS ? ((const GradBoth*)p)->keys : ((const GradBoth*)p)->rows;
 }
 
 // How the bias enters a wave's tile of pairs: every pair by its distance, or one number for all.
@@ -245,18 +250,23 @@ __device__ __forceinline__ void lds_order() {
 // ------------------------------------------------------------------------------------------------
 // dK and dV
 
+template <int D>
+constexpr int key_lds() {
+  return 4 * 64 * 128 + 2 * GradTile<D, 64>::BYTES + 2 * kStatBytes;
+}
+
 template <int D, bool BIAS>
-__global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void key_grad_kernel(GradArgs) {
+__device__ __forceinline__ void key_grad(unsigned char* lds, int block, int P) {
   using X = Mma<D>;
   constexpr int QT = D == 128 ? 32 : 64;               // query rows of a tile
   using T = GradTile<D, QT>;
   using TV = GradTile<D, 64>;
   constexpr int NT = QT / X::MR;
-  __shared__ __attribute__((aligned(1024))) unsigned char ring[4 * T::BYTES];       // Q, dO of two stages
-  __shared__ __attribute__((aligned(1024))) unsigned char vtile[2 * TV::BYTES];
-  __shared__ __attribute__((aligned(1024))) unsigned char stat[2 * kStatBytes];
-  const int P = gridDim.x;
-  const int l = (blockIdx.x & 7) * (P >> 3) + (blockIdx.x >> 3);
+  static_assert(T::BYTES == 64 * 128);
+  unsigned char* const ring = lds;                     // Q, dO of two stages
+  unsigned char* const vtile = lds + 4 * T::BYTES;
+  unsigned char* const stat = vtile + 2 * TV::BYTES;
+  const int l = (block & 7) * (P >> 3) + (block >> 3);
   const int tid = threadIdx.x, lane = tid & 63;
   const int lw = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane % X::MR, lg = lane / X::MR;
@@ -267,7 +277,7 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
   uint32_t q_off[T::PER], do_off[T::PER];
   FarBias far{0, 0, 0.f, 0.f};
   {
-    const GradArgs a = grad_args();
+    const GradArgs a = grad_args<true>();
     if (a.g.cuts && tid == 0) a.io.cut[2 * l] = a.io.cut[2 * l + 1] = int4{0, 0, 0, 0};
     uint64_t share;
     wk = grad_start<QT>(a.g, l, P, &share);
@@ -293,7 +303,7 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
     uint64_t unit_end;
     GradPiece pc;
     {
-      const GradArgs a = grad_args();
+      const GradArgs a = grad_args<true>();
       pc = grad_piece<QT>(a.g, wk, &unit_end);
     }
     if (pc.tb > pc.ta) {
@@ -309,7 +319,7 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
       int next_head = head, next_tile = tile;
       uint64_t next_q, next_do, next_stat;
       auto seek = [&]() {
-        const GradArgs a = grad_args();
+        const GradArgs a = grad_args<true>();
         const int64_t tok = (int64_t)wk.q.q0 + (first + next_tile) * QT;
         const int qh = wk.h * a.g.G + next_head;
         next_q = first_lane_u64((uint64_t)(uintptr_t)a.io.q + (uint64_t)(tok * a.io.q_tok + qh * a.io.q_head) * 2u);
@@ -337,7 +347,7 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
       __syncthreads();                                 // the piece before is read
       const float* table = nullptr;                    // the bias of the present head
       {
-        const GradArgs a = grad_args();
+        const GradArgs a = grad_args<true>();
         const Seq& q = wk.q;
         const int n0 = wk.b * kGradRows;
         const uint32_t v_stride = (uint32_t)a.io.v_tok * 2u;
@@ -377,7 +387,7 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
         }
       }
       // rows before this one see none of the wave's keys, those from it on all of them
-      const bool causal = grad_args().g.causal;
+      const bool causal = grad_args<true>().g.causal;
       const int from = key0 < wk.q.lk ? (causal ? key0 - off : 0) : 0x7fffffff;
       const int whole_from = causal ? key0 + 31 - off : 0;
       for (int st = 0; left > 0; --left, st ^= 1) {
@@ -386,7 +396,7 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
         const int row0 = (first + tile) * QT;
         if constexpr (BIAS) {
           if (tile == 0) {
-            const GradArgs a = grad_args();
+            const GradArgs a = grad_args<true>();
             table = a.io.table + (int64_t)(wk.h * a.g.G + head) * a.io.bias_pitch;
             far_bias(far, table);
           }
@@ -465,7 +475,7 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
         columns_product<D, QT / X::KC>(qt, op, dk, cbase);
       }
       __builtin_amdgcn_s_waitcnt(0);                   // V, where nothing saw the unit
-      const GradArgs a = grad_args();
+      const GradArgs a = grad_args<true>();
       const bool whole = pc.ta == 0 && pc.tb == pc.n;
       const int slot = 2 * l + (pc.ta == 0 ? 1 : 0);
       const int n0 = wk.b * kGradRows;
@@ -485,7 +495,7 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
         }
       }
     }
-    const GradArgs a = grad_args();
+    const GradArgs a = grad_args<true>();
     grad_on<QT>(a.g, wk, unit_end);
   }
 }
@@ -550,15 +560,19 @@ __device__ __forceinline__ void add_diagonals(const typename Mma<D>::Acc (*x)[Mm
 }
 
 template <int D, bool BIAS>
-__global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void row_grad_kernel(GradArgs) {
+constexpr int row_lds() {
+  return 4 * GradTile<D, KT>::BYTES + (BIAS ? 4 * (256 + kBiasPitch) * 4 : 0);
+}
+
+template <int D, bool BIAS>
+__device__ __forceinline__ void row_grad(unsigned char* lds, int group, int P) {
   using X = Mma<D>;
   constexpr int NT = KT / X::MR;
   using T = GradTile<D, KT>;
-  __shared__ __attribute__((aligned(1024))) unsigned char ring[4 * T::BYTES];       // K, V of two stages
-  __shared__ __attribute__((aligned(16))) float block[BIAS ? 4 : 1][BIAS ? 256 : 4];
-  __shared__ float sums[BIAS ? 4 : 1][BIAS ? kBiasPitch : 1];
-  const int P = gridDim.x;
-  const int l = (blockIdx.x & 7) * (P >> 3) + (blockIdx.x >> 3);
+  unsigned char* const ring = lds;                     // K, V of two stages
+  float(*const block)[256] = (float(*)[256])(lds + 4 * T::BYTES);
+  float(*const sums)[kBiasPitch] = (float(*)[kBiasPitch])(lds + 4 * T::BYTES + 4 * 256 * 4);
+  const int l = (group & 7) * (P >> 3) + (group >> 3);
   const int tid = threadIdx.x, lane = tid & 63;
   const int lw = __builtin_amdgcn_readfirstlane(tid >> 6);
   GradWalk wk;
@@ -568,7 +582,7 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
   float far_lo = 0.f, far_hi = 0.f;      // the lane's sums of dS beyond the table's ends
   uint32_t k_stride, v_stride;
   {
-    const GradArgs a = grad_args();
+    const GradArgs a = grad_args<false>();
     if (a.g.cuts && tid == 0) a.io.cut[2 * l] = a.io.cut[2 * l + 1] = int4{0, 0, 0, 0};
     uint64_t share;
     wk = grad_start<0>(a.g, l, P, &share);
@@ -576,7 +590,7 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
     k_stride = (uint32_t)a.io.k_tok * 2u;
     v_stride = (uint32_t)a.io.v_tok * 2u;
     if constexpr (BIAS) {
-      if (blockIdx.x == 0 && tid == 0) {
+      if (group == 0 && tid == 0) {
         a.io.line[0] = wk.head;
         a.io.line[1] = share;
       }
@@ -596,7 +610,7 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
   auto flush = [&](int until) {
     if constexpr (BIAS) {
       if (sum_head >= until) return;
-      const GradArgs a = grad_args();
+      const GradArgs a = grad_args<false>();
       const int pitch = a.io.bias_pitch;
       for (; sum_head < until; ++sum_head) {
 #pragma unroll
@@ -635,7 +649,7 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
     uint64_t unit_end;
     GradPiece pc;
     {
-      const GradArgs a = grad_args();
+      const GradArgs a = grad_args<false>();
       pc = grad_piece<KT>(a.g, wk, &unit_end);
     }
     if (pc.tb > pc.ta) {
@@ -660,7 +674,7 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
       const float* table = nullptr;
       int least_pos = 0;                               // place of the wave's first query among the keys
       {
-        const GradArgs a = grad_args();
+        const GradArgs a = grad_args<false>();
         const Seq& q = wk.q;
         const int kvh = wk.h / a.g.GS, head0 = wk.h % a.g.GS * a.g.GH;       // the unit's heads within the group
         const int heads = min(a.g.GH, a.g.G - head0);
@@ -785,7 +799,7 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
         as_operand<D, NT>(dp, op);
         columns_product<D, KT / X::KC>(kt, op, dq, cbase);
       }
-      const GradArgs a = grad_args();
+      const GradArgs a = grad_args<false>();
       const bool whole = pc.ta == 0 && pc.tb == pc.n;
       const int slot = 2 * l + (pc.ta == 0 ? 1 : 0);
       const int kvh = wk.h / a.g.GS, head0 = wk.h % a.g.GS * a.g.GH;
@@ -805,19 +819,34 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
           store_part<D>(dq, qc, a.io.part + ((size_t)slot * kGradRows + r) * D, lg);
       }
     }
-    const GradArgs a = grad_args();
+    const GradArgs a = grad_args<false>();
     grad_on<0>(a.g, wk, unit_end);
   }
   if constexpr (BIAS) flush(last_head + 1);
 }
 
+// One launch for both: the workgroups of dK and dV, which take longer, come first, and those of dQ start as they end.
+template <int D, bool BIAS>
+__global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void grad_kernel(GradBoth) {
+  constexpr int LDS = key_lds<D>() > row_lds<D, BIAS>() ? key_lds<D>() : row_lds<D, BIAS>();
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[LDS];
+  const int keys_p = grad_args<true>().P;
+  if ((int)blockIdx.x < keys_p) key_grad<D, BIAS>(lds, blockIdx.x, keys_p);
+  else row_grad<D, BIAS>(lds, blockIdx.x - keys_p, gridDim.x - keys_p);
+}
+
 // ------------------------------------------------------------------------------------------------
 // Joins the pieces of a unit that several stretches share, in the order of the stretches (as seq_merge_kernel,
-// but sums alone).  Workgroup (l, y, z) joins rows [16 y, 16 y + 16) of array z.
+// but sums alone).  Workgroup (l, y) joins rows [16 y, 16 y + 16) of the unit of stretch l: dK where y < 8 and dV
+// behind, for l below the number of the stretches of keys; dQ for the others.
 template <int D>
-__global__ __launch_bounds__(256) void grad_merge_kernel(GradIo io, int GH, int P) {
+__global__ __launch_bounds__(256) void grad_merge_kernel(GradIo keys, GradIo rows, int keys_p, int rows_p, int rows_gh) {
   constexpr int TPR = 16, W = D / TPR;
-  const int l0 = blockIdx.x, A = gridDim.z;
+  const bool of_keys = (int)blockIdx.x < keys_p;
+  const GradIo& io = of_keys ? keys : rows;
+  const int l0 = of_keys ? blockIdx.x : blockIdx.x - keys_p, P = of_keys ? keys_p : rows_p;
+  const int A = of_keys ? 2 : 1, GH = of_keys ? 1 : rows_gh, array = blockIdx.y / 8;
+  if (array >= A) return;
   const int lane = threadIdx.x & 63;
   const int4 u = io.cut[2 * l0 + 1];
   if (u.w == 0) return;
@@ -832,7 +861,7 @@ __global__ __launch_bounds__(256) void grad_merge_kernel(GradIo io, int GH, int 
     }
     n += 64;
   }
-  const int r = blockIdx.y * 16 + threadIdx.x / TPR, part = threadIdx.x % TPR;
+  const int r = blockIdx.y % 8 * 16 + threadIdx.x / TPR, part = threadIdx.x % TPR;
   const int token = r / GH, head = r - token * GH;
   if (token >= u.y || head >= u.w) return;
   float acc[W];
@@ -847,7 +876,7 @@ __global__ __launch_bounds__(256) void grad_merge_kernel(GradIo io, int GH, int 
       const size_t slot = i == 0 ? 2 * l0 + 1 : 2 * (l0 + i);
 #pragma unroll
       for (int e = 0; e < W / 4; ++e)
-        x[j][e] = *(const f32x4*)(io.part + ((slot * A + blockIdx.z) * kGradRows + r) * D + part * W + 4 * e);
+        x[j][e] = *(const f32x4*)(io.part + ((slot * A + array) * kGradRows + r) * D + part * W + 4 * e);
     }
 #pragma unroll
     for (int j = 0; j < BATCH; ++j) {
@@ -856,7 +885,7 @@ __global__ __launch_bounds__(256) void grad_merge_kernel(GradIo io, int GH, int 
       for (int e = 0; e < W; ++e) acc[e] += x[j][e / 4][e % 4];
     }
   }
-  const bool second = blockIdx.z == 1;
+  const bool second = array == 1;
   const float f = second ? 1.0f : io.scale;
   uint16_t* dst = (second ? io.out1 : io.out0) + (int64_t)(u.x + token) * (second ? io.out1_tok : io.out0_tok) +
                   (int64_t)(u.z + head) * (second ? io.out1_head : io.out0_head) + part * W;
@@ -995,20 +1024,16 @@ static hipError_t launch_grad(const GradCall& c, hipStream_t st) {
                      const_cast<float2*>(c.rows_io.stat), c.Tq, c.rows_g.Hq, groups, c.bias, c.rows_io.bias_pitch,
                      const_cast<float*>(c.rows_io.table)};
     hipLaunchKernelGGL((grad_prep_kernel<D>), dim3(groups + (c.has_bias ? c.rows_g.Hq : 0)), dim3(256), 0, st, p);
-    const GradArgs a{c.rows_g, c.rows_io};
-    if (c.has_bias) hipLaunchKernelGGL((row_grad_kernel<D, true>), dim3(c.rows_p), dim3(kGradThreads), 0, st, a);
-    else hipLaunchKernelGGL((row_grad_kernel<D, false>), dim3(c.rows_p), dim3(kGradThreads), 0, st, a);
-    if (c.rows_g.cuts)
-      hipLaunchKernelGGL((grad_merge_kernel<D>), dim3(c.rows_p, kGradRows / 16, 1), dim3(256), 0, st, c.rows_io,
-                         c.rows_g.GH, c.rows_p);
   }
-  if (c.keys) {
-    const GradArgs a{c.keys_g, c.keys_io};
-    if (c.has_bias) hipLaunchKernelGGL((key_grad_kernel<D, true>), dim3(c.keys_p), dim3(kGradThreads), 0, st, a);
-    else hipLaunchKernelGGL((key_grad_kernel<D, false>), dim3(c.keys_p), dim3(kGradThreads), 0, st, a);
-    if (c.keys_g.cuts)
-      hipLaunchKernelGGL((grad_merge_kernel<D>), dim3(c.keys_p, kGradRows / 16, 2), dim3(256), 0, st, c.keys_io, 1,
-                         c.keys_p);
+  const int keys_p = c.keys ? c.keys_p : 0, rows_p = c.rows ? c.rows_p : 0;
+  if (keys_p + rows_p > 0) {
+    const GradBoth a{{c.keys_g, c.keys_io, keys_p}, {c.rows_g, c.rows_io, rows_p}};
+    if (c.has_bias) hipLaunchKernelGGL((grad_kernel<D, true>), dim3(keys_p + rows_p), dim3(kGradThreads), 0, st, a);
+    else hipLaunchKernelGGL((grad_kernel<D, false>), dim3(keys_p + rows_p), dim3(kGradThreads), 0, st, a);
+    const int keys_cut = c.keys_g.cuts ? keys_p : 0, rows_cut = c.rows_g.cuts ? rows_p : 0;
+    if (keys_cut + rows_cut > 0)
+      hipLaunchKernelGGL((grad_merge_kernel<D>), dim3(keys_cut + rows_cut, keys_cut ? 16 : 8), dim3(256), 0, st, c.keys_io,
+                         c.rows_io, keys_cut, rows_cut, c.rows_g.GH);
   }
   if (c.has_bias) {
     const DistArgs d{c.rows_io.dist, c.rows_io.line, c.bias.bucket, c.dweight, c.bias.bf16, c.bias.buckets, c.bias.lo,
