@@ -159,7 +159,7 @@ struct GradWalk {
   uint64_t pos, end;       // the stretch still to do
   uint64_t unit0;          // where the present unit starts
   uint64_t head;           // weight of a head
-  uint32_t snap, small;    // as in Walk
+  uint32_t snap, small;    // as in Walk, but borders in units of up to 5/4 shares go to the nearest end
   int h, s, j, b;          // head group, sequence, place of the run among the sequence's, run
   Seq q;
   GradLine line;
@@ -167,7 +167,7 @@ struct GradWalk {
 };
 
 __device__ __forceinline__ uint32_t grad_near(const GradWalk& w, uint64_t weight) {
-  return weight <= w.small ? w.small / 4 : w.snap;
+  return weight <= w.small ? w.small * 2 / 5 : w.snap;
 }
 
 // The part of the present unit that the stretch covers: inner tiles [ta, tb) of n, none if ta == tb.  A unit
@@ -248,7 +248,7 @@ __device__ __forceinline__ GradWalk grad_start(const GradGeom& g, int l, int P, 
   w.pos = first_lane_u64((uint64_t)(uint32_t)l * share);
   w.end = w.pos + share < total ? w.pos + share : total;
   w.snap = !g.cuts ? ~0u : (uint32_t)(share / 64 < g.extra ? share / 64 : g.extra);
-  w.small = g.cuts && share < g.whole ? 2 * (uint32_t)share : 0;
+  w.small = g.cuts && share < g.whole ? (uint32_t)share * 5 / 4 : 0;
   w.h = w.s = w.j = w.b = 0;
   w.unit0 = 0;
   w.q = Seq{0, 0, 0, 0};

@@ -140,7 +140,7 @@ int device_workgroups(int per_cu) {
 }
 
 // The gradients' units, and where nothing is cut: inner axes of at most kGradWhole rows.
-constexpr uint32_t kGradExtra = 256, kGradShare = 512;
+constexpr uint32_t kGradExtra = 512, kGradShare = 512;
 constexpr int kGradWhole = 512, kGradPerCu = 2;
 
 GradGeom grad_geom(const la_seqs& s, bool keys, bool bias) {
@@ -159,7 +159,7 @@ GradGeom grad_geom(const la_seqs& s, bool keys, bool bias) {
   g.NH = s.Hkv * g.GS;
   g.causal = s.causal;
   g.extra = kGradExtra;
-  g.whole = 2 * kGradExtra;
+  g.whole = 4096;
   g.min_share = kGradShare;
   g.cuts = (keys ? (double)s.Tq * g.G : (double)s.Tk) > kGradWhole;
   return g;
@@ -172,12 +172,6 @@ int grad_workgroups(const GradGeom& g, bool keys) {
   const double shares = ceil(units * (inner + g.extra) / g.min_share);
   const int most = kMaxWorkgroups * kGradPerCu, want = shares < most ? (int)shares : most;
   return (want + 7) / 8 * 8;
-}
-
-// A workgroup of 256 threads takes the statistics of 16 tokens by 16 heads, and one more lays out each head's
-// bias; a grid has at most 2^32 - 1 threads along an axis.
-bool bad_grad_rows(const la_seqs& s) {
-  return (int64_t)ceil_div(s.Tq, 16) * ceil_div(s.Hq, 16) + s.Hq >= 1 << 24;
 }
 
 bool bad_bias(const la_rel_bias* b) {
@@ -430,7 +424,7 @@ la_status la_kv4_attn(const la_seqs* seqs, const la_kv4* kv, int32_t max_q, cons
 }
 
 size_t la_prompt_bwd_ws_bytes(const la_seqs* seqs, const la_rel_bias* bias) {
-  if (check_seqs(seqs) != LA_OK || bad_grad_rows(*seqs) || (bias && bad_bias(bias)) || seqs->S == 0) return 0;
+  if (check_seqs(seqs) != LA_OK || (bias && bad_bias(bias)) || seqs->S == 0) return 0;
   return grad_layout(*seqs, bias, nullptr).bytes;
 }
 
@@ -442,7 +436,6 @@ la_status la_prompt_attn_bwd(const la_seqs* seqs, const la_prompt_grads* grads, 
   la_status st = check_seqs(seqs);
   if (st != LA_OK) return st;
   if (!grads || isnan(scale) || isinf(scale)) return LA_ERR_ARG;
-  if (bad_grad_rows(*seqs)) return LA_ERR_SHAPE;
   if (bias) {
     st = check_bias(bias, bucket, weight);
     if (st != LA_OK) return st;

@@ -404,7 +404,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   w.scale_log2 = scale_log2;
   PieceState<D> st;
   typename std::conditional<BIAS, WaveBias<D>, int>::type wb;
-  int bias_lo = 0, bias_hi = 0;
+  int bias_lo = 0, bias_hi = 0, table_head = -1;       // table_head: the first head of the tables in LDS
   if constexpr (BIAS) {
     const SeqArgs a = fresh_args();
     bias_lo = a.bias.lo;
@@ -440,9 +440,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
           src.prime(a.io, wk, wk.kvh, pc.ta, pc.tb, IS_G1 ? s0 + VOFF : s0, IS_G1 ? nullptr : s1);
           start_rows<D>(st, w, a.g, a.io, wk, r_off, c, lg);
           if constexpr (BIAS) {
-            // the waves read no table of the piece before any more: its last iteration ended with a barrier
-            fill_bias(table, a, wk);
-            __syncthreads();
+            // consecutive units mostly have the same heads; the waves read no table of the piece before any more, as
+            // its last iteration ended with a barrier
+            const int heads = unit_head0(a.g, wk);
+            if (heads != table_head) {
+              table_head = heads;
+              fill_bias(table, a, wk);
+              __syncthreads();
+            }
             start_bias<D>(wb, table, a, wk, r_off, c, lg);
           }
           const int open = a.g.causal ? max(0, wk.q.lk - wk.q.lq + wk.b * a.g.TB + 1) : wk.q.lk;

@@ -17,6 +17,9 @@
 namespace la {
 namespace {
 
+// four words at any word's address
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+
 constexpr int kGradThreads = 256;        // four waves, each with 32 of a unit's 128 rows
 
 // A tile of ROWS rows of D bf16 in LDS that is read both ways: as operands along d (16 bytes of MR rows) and
@@ -410,25 +413,29 @@ __device__ __forceinline__ void key_grad(unsigned char* lds, int block, int P) {
         const unsigned char* qt = ring + st * (2 * T::BYTES);
         const unsigned char* dt = qt + T::BYTES;
         typename X::Acc s[NT][X::QT], dp[NT][X::QT];
-        rows_product<D, NT>(qt, kreg, s, rbase);
         float to_log2 = scale_log2, shift = 0.f;
+        rows_product<D, NT>(qt, kreg, s, rbase);
         if constexpr (BIAS) {
           const TileBias bias = tile_bias(far, key0 - (row0 + QT - 1 + off), key0 + 31 - (row0 + off));
           shift = bias.far;
           if (bias.near) {
             to_log2 = 1.0f;
             const float* at0 = table + (key0 + c - (row0 + 4 * lg + 3 + off) - far.lo + kBiasPad);
+            f32x4u b[NT][X::QT][X::AR / 4];
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
               for (int kc = 0; kc < X::QT; ++kc)
 #pragma unroll
-                for (int i = 0; i < X::AR; i += 4) {
-                  const float* at = at0 + (X::MR * kc - X::MR * t - X::acc_row(i));
+                for (int i = 0; i < X::AR; i += 4)
+                  b[t][kc][i / 4] = *(const f32x4u*)(at0 + (X::MR * kc - X::MR * t - X::acc_row(i)));
 #pragma unroll
-                  for (int j = 0; j < 4; ++j)
-                    s[t][kc][i + j] = __builtin_fmaf(s[t][kc][i + j], scale_log2, at[3 - j]);
-                }
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+              for (int kc = 0; kc < X::QT; ++kc)
+#pragma unroll
+                for (int i = 0; i < X::AR; ++i)
+                  s[t][kc][i] = __builtin_fmaf(s[t][kc][i], scale_log2, b[t][kc][i / 4][3 - i % 4]);
           }
         }
         tiles_product<D, NT>(dt, vtile + (w0 >> 6) * TV::BYTES + (w0 & 63) * (2 * D), dp, rbase, rbase);
@@ -503,65 +510,93 @@ __device__ __forceinline__ void key_grad(unsigned char* lds, int block, int P) {
 // ------------------------------------------------------------------------------------------------
 // dQ, and the bias' gradient
 
-// Adds a wave's tile of dS to its sums by distance, `sums`, which start at distance lo - kBiasPad: X[t][c] is the
-// product's accumulator, key rows by query columns.
+// Blocks of 16 x 16 that are in LDS at once, of each wave: all five where there is room for two workgroups of a CU.
+template <int D>
+constexpr int diagonal_blocks() {
+  return D == 128 ? 1 : 5;
+}
+
+// Sum over the lanes l, l ^ 16, l ^ 32 and l ^ 48, in all of them.
+__device__ __forceinline__ float sum_quarters(float x) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const auto s = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const uint32_t v = __builtin_bit_cast(uint32_t, __builtin_bit_cast(float, (uint32_t)s[0]) +
+                                                      __builtin_bit_cast(float, (uint32_t)s[1]));
+  const auto t = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return __builtin_bit_cast(float, (uint32_t)t[0]) + __builtin_bit_cast(float, (uint32_t)t[1]);
+}
+
+// Adds a wave's tile of dS to its sums by distance, `sums`, which start at distance lo - kBiasPad: x[t][c] is the
+// product's accumulator, key rows by query columns; `first` is the place of distance 0 of the tile's first pair.
 //
-// The blocks of 16 keys by 16 queries whose keys are as far ahead of their queries are added first, then each
-// is laid into LDS row by row (a query's 16 keys) and its diagonals are summed: lane j of quarter h takes key
-// (j + r) mod 16 of the queries r = 4 h .. 4 h + 3, which lie at distance j where j + r < 16, else j - 16.
+// The blocks of 16 keys by 16 queries whose keys are as far ahead of their queries are added first (block e has 16 e
+// keys more than queries, from -1 to 3).  Each is laid into LDS row by row (a query's 16 keys) and its diagonals
+// are summed: lane j of quarter h takes key (j + r) mod 16 of the queries r = 4 h .. 4 h + 3, which lie at distance
+// j where j + r < 16, else j - 16.  So distance 16 m + j of the tile is what lies ahead in block m and behind in m + 1.
 template <int D>
 __device__ __forceinline__ void add_diagonals(const typename Mma<D>::Acc (*x)[Mma<D>::QT], float* block, float* sums,
                                               int first, int lane) {
   using X = Mma<D>;
-  // 16 x 16 blocks of the 64 keys and 32 queries: block e has 16 (kt - qt) = 16 e, e from -1 to 3
+  constexpr int NB = diagonal_blocks<D>();
+  const int j = lane & 15, quarter = lane >> 4;
+  float at[6] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};        // distances 16 (m - 2) + j
 #pragma unroll
-  for (int e = -1; e < 4; ++e) {
-    if constexpr (X::MR == 16) {
-      f32x4 y = e >= 0 ? x[e][0] : x[0][1];
-      if (e >= 0 && e < 3) y += x[e + 1][1];
-      *(f32x4*)(block + 16 * (lane & 15) + 4 * (lane >> 4)) = y;
-    } else {
-      // lanes 0..15 and 32..47 hold the columns of qt = 0, the others those of qt = 1; registers 8 (kt & 1) + 4 u + v
-      // of accumulator kt / 2 hold key 8 u + 4 (lane / 32) + v of key block kt.  A column's own block is e + qt.
-      const int qt = (lane >> 4) & 1;
+  for (int e0 = -1; e0 < 4; e0 += NB) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
-        const int k0 = e, k1 = e + 1;
+    for (int e = e0; e < 4 && e < e0 + NB; ++e) {
+      float* to = block + 256 * (e - e0);
+      if constexpr (X::MR == 16) {
+        f32x4 y = e >= 0 ? x[e][0] : x[0][1];
+        if (e >= 0 && e < 3) y += x[e + 1][1];
+        *(f32x4*)(to + 16 * j + 4 * quarter) = y;
+      } else {
+        // lanes of even quarters hold the columns of the first 16 queries, the others those of the second; registers
+        // 8 (kt & 1) + 4 u + v of accumulator kt / 2 hold key 8 u + 4 (lane / 32) + v of key block kt, which is
+        // e for the first queries and e + 1 for the second
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          const float mine0 = k0 >= 0 ? x[k0 >> 1][0][8 * (k0 & 1) + 4 * u + v] : 0.f;
-          const float mine1 = k1 < 4 ? x[(k1 & 3) >> 1][0][8 * (k1 & 1) + 4 * u + v] : 0.f;
-          y[v] = qt ? mine1 : mine0;
+        for (int u = 0; u < 2; ++u) {
+          f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
+          const int k0 = e, k1 = e + 1;
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            if (k1 < 4) {
+              const uint32_t z = __builtin_bit_cast(uint32_t, (float)x[(k1 & 3) >> 1][0][8 * (k1 & 1) + 4 * u + v]);
+              const auto s = __builtin_amdgcn_permlane16_swap(z, z, false, false);
+              y[v] = __builtin_bit_cast(float, (uint32_t)s[1]);          // the odd quarter's, in both
+            }
+            if (k0 >= 0) y[v] += x[(k0 & 3) >> 1][0][8 * (k0 & 1) + 4 * u + v];
+          }
+          if ((quarter & 1) == 0) *(f32x4*)(to + 16 * j + 8 * u + 4 * (lane >> 5)) = y;
         }
-#pragma unroll
-        for (int v = 0; v < 4; ++v) y[v] += __shfl_xor(y[v], 16);
-        if (qt == 0) *(f32x4*)(block + 16 * (lane & 15) + 8 * u + 4 * (lane >> 5)) = y;
       }
     }
     lds_order();
-    const int j = lane & 15, quarter = lane >> 4;
-    float ahead = 0.f, behind = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = 4 * quarter + i;
-      const float v = block[16 * r + ((j + r) & 15)];
-      if (j + r < 16) ahead += v;
-      else behind += v;
+    for (int e = e0; e < 4 && e < e0 + NB; ++e) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = 4 * quarter + i;
+        const float v = block[256 * (e - e0) + 16 * r + ((j + r) & 15)];
+        at[e + 2] += j + r < 16 ? v : 0.f;
+        at[e + 1] += j + r < 16 ? 0.f : v;
+      }
     }
     lds_order();
-    ahead += __shfl_xor(ahead, 16);
-    ahead += __shfl_xor(ahead, 32);
-    behind += __shfl_xor(behind, 16);
-    behind += __shfl_xor(behind, 32);
-    if (lane < 32) sums[first + 16 * e + (lane < 16 ? j : j - 16)] += lane < 16 ? ahead : behind;
-    lds_order();
   }
+#pragma unroll
+  for (int m = 0; m < 6; ++m) at[m] = sum_quarters(at[m]);
+  // quarter h writes segments h and, for the last two, 4 + h
+  const float a = quarter == 0 ? at[0] : quarter == 1 ? at[1] : quarter == 2 ? at[2] : at[3];
+  const float b = quarter == 0 ? at[4] : at[5];
+  float* p = sums + (first - 32 + lane);
+  p[0] += a;
+  if (quarter < 2) p[64] += b;
+  lds_order();
 }
 
 template <int D, bool BIAS>
 constexpr int row_lds() {
-  return 4 * GradTile<D, KT>::BYTES + (BIAS ? 4 * (256 + kBiasPitch) * 4 : 0);
+  return 4 * GradTile<D, KT>::BYTES + (BIAS ? 4 * (256 * diagonal_blocks<D>() + kBiasPitch) * 4 : 0);
 }
 
 template <int D, bool BIAS>
@@ -570,8 +605,9 @@ __device__ __forceinline__ void row_grad(unsigned char* lds, int group, int P) {
   constexpr int NT = KT / X::MR;
   using T = GradTile<D, KT>;
   unsigned char* const ring = lds;                     // K, V of two stages
-  float(*const block)[256] = (float(*)[256])(lds + 4 * T::BYTES);
-  float(*const sums)[kBiasPitch] = (float(*)[kBiasPitch])(lds + 4 * T::BYTES + 4 * 256 * 4);
+  constexpr int BLOCK = 256 * diagonal_blocks<D>();
+  float(*const block)[BLOCK] = (float(*)[BLOCK])(lds + 4 * T::BYTES);
+  float(*const sums)[kBiasPitch] = (float(*)[kBiasPitch])(lds + 4 * T::BYTES + 4 * BLOCK * 4);
   const int l = (group & 7) * (P >> 3) + (group >> 3);
   const int tid = threadIdx.x, lane = tid & 63;
   const int lw = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -738,9 +774,9 @@ __device__ __forceinline__ void row_grad(unsigned char* lds, int group, int P) {
         if (key0 >= wave_keys) continue;
         const unsigned char* kt = ring + st * (2 * T::BYTES);
         typename X::Acc s[NT][X::QT], dp[NT][X::QT];
-        rows_product<D, NT>(kt, qreg, s, rbase);
         float to_log2 = scale_log2, shift = 0.f;
         bool near = false;
+        rows_product<D, NT>(kt, qreg, s, rbase);
         if constexpr (BIAS) {
           const TileBias bias = tile_bias(far, key0 - (least_pos + 31), key0 + 63 - least_pos);
           shift = bias.far;
@@ -748,13 +784,21 @@ __device__ __forceinline__ void row_grad(unsigned char* lds, int group, int P) {
           if (near) {
             to_log2 = 1.0f;
             const float* at = table + (key0 + 4 * lg - (least_pos + c) - far.lo + kBiasPad);
+            f32x4u b[NT][X::QT][X::AR / 4];
+#pragma unroll
+            for (int qc = 0; qc < X::QT; ++qc)
+#pragma unroll
+              for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < X::AR; i += 4)
+                  b[t][qc][i / 4] = *(const f32x4u*)(at + (X::MR * t + X::acc_row(i) - X::MR * qc));
 #pragma unroll
             for (int qc = 0; qc < X::QT; ++qc)
 #pragma unroll
               for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int i = 0; i < X::AR; ++i)
-                  s[t][qc][i] = __builtin_fmaf(s[t][qc][i], scale_log2, at[X::MR * t + X::acc_row(i) - X::MR * qc]);
+                  s[t][qc][i] = __builtin_fmaf(s[t][qc][i], scale_log2, b[t][qc][i / 4][i % 4]);
           }
         }
         rows_product<D, NT>(kt + T::BYTES, doreg, dp, rbase);
@@ -836,17 +880,62 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
 }
 
 // ------------------------------------------------------------------------------------------------
+// The gradient of the bias' weights: a workgroup adds the sums by distance of one bucket (and of every `step`-th from
+// there) of a head, over the workgroups of dQ that met the head and the distances of the bucket (what lies beyond the
+// ends belongs to them), in 64 bits and a fixed order.  A wave has every fourth workgroup, a lane every 64th distance.
+struct DistArgs {
+  const float* dist;
+  const uint64_t* line;
+  SeqBias bias;
+  void* dweight;
+  int pitch, Hq, P, empty;
+  int groups;              // workgroups of a head
+};
+__device__ __forceinline__ void dist_merge(const DistArgs& a, int h, int first, int step) {
+  __shared__ double part[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint64_t head = a.empty ? 0 : a.line[0], share = a.empty ? 1 : a.line[1];
+  const int l0 = (int)(head * (uint32_t)h / share);
+  const int l1 = head == 0 ? l0 - 1 : min((int)((head * ((uint32_t)h + 1ull) - 1) / share), a.P - 1);
+  for (int64_t b = first; b < a.bias.buckets; b += step) {
+    double x = 0.0;
+    for (int i = lane; i < a.pitch; i += 64) {
+      if (a.bias.bucket[min(max(i - kBiasPad, 0), a.bias.hi - a.bias.lo)] != b) continue;
+#pragma unroll 16
+      for (int l = l0 + wave; l <= l1; l += 4) x += a.dist[(size_t)(l + h) * a.pitch + i];
+    }
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
+    if (lane == 0) part[wave] = x;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      const float y = (float)((part[0] + part[1]) + (part[2] + part[3]));
+      const size_t at = (size_t)b * a.Hq + h;
+      if (a.bias.bf16) ((uint16_t*)a.dweight)[at] = (uint16_t)(pack_bf16x2(y, 0.f) & 0xffffu);
+      else ((float*)a.dweight)[at] = y;
+    }
+    __syncthreads();
+  }
+}
+
 // Joins the pieces of a unit that several stretches share, in the order of the stretches (as seq_merge_kernel,
-// but sums alone).  Workgroup (l, y) joins rows [16 y, 16 y + 16) of the unit of stretch l: dK where y < 8 and dV
-// behind, for l below the number of the stretches of keys; dQ for the others.
+// but sums alone).  A workgroup joins 16 rows of an array (dK, dV or dQ) of the unit of one stretch.  In front of
+// them (the longest chains) are those of the weights' gradient.
 template <int D>
-__global__ __launch_bounds__(256) void grad_merge_kernel(GradIo keys, GradIo rows, int keys_p, int rows_p, int rows_gh) {
+__global__ __launch_bounds__(256) void grad_merge_kernel(GradIo keys, GradIo rows, DistArgs dist, int keys_p, int rows_p,
+                                                         int rows_gh) {
   constexpr int TPR = 16, W = D / TPR;
-  const bool of_keys = (int)blockIdx.x < keys_p;
+  const int dists = dist.Hq * dist.groups;
+  if ((int)blockIdx.x < dists) {
+    dist_merge(dist, blockIdx.x / dist.groups, blockIdx.x % dist.groups, dist.groups);
+    return;
+  }
+  const int block = blockIdx.x - dists;
+  const bool of_keys = block < 16 * keys_p;
   const GradIo& io = of_keys ? keys : rows;
-  const int l0 = of_keys ? blockIdx.x : blockIdx.x - keys_p, P = of_keys ? keys_p : rows_p;
-  const int A = of_keys ? 2 : 1, GH = of_keys ? 1 : rows_gh, array = blockIdx.y / 8;
-  if (array >= A) return;
+  const int y = of_keys ? block % 16 : block % 8, array = y / 8;
+  const int l0 = of_keys ? block / 16 : (block - 16 * keys_p) / 8, P = of_keys ? keys_p : rows_p;
+  const int A = of_keys ? 2 : 1, GH = of_keys ? 1 : rows_gh;
   const int lane = threadIdx.x & 63;
   const int4 u = io.cut[2 * l0 + 1];
   if (u.w == 0) return;
@@ -861,7 +950,7 @@ __global__ __launch_bounds__(256) void grad_merge_kernel(GradIo keys, GradIo row
     }
     n += 64;
   }
-  const int r = blockIdx.y % 8 * 16 + threadIdx.x / TPR, part = threadIdx.x % TPR;
+  const int r = y % 8 * 16 + threadIdx.x / TPR, part = threadIdx.x % TPR;
   const int token = r / GH, head = r - token * GH;
   if (token >= u.y || head >= u.w) return;
   float acc[W];
@@ -895,14 +984,16 @@ __global__ __launch_bounds__(256) void grad_merge_kernel(GradIo keys, GradIo row
 }
 
 // ------------------------------------------------------------------------------------------------
-// What both kernels need of a row: lse in base 2, and delta.  Workgroups behind the rows' lay out the bias.
+// What both walks need of a row: lse in base 2, and delta; and the bias by distance.  Bound by reading o and do.
+constexpr int kPrepTokens = 2;           // 4 and 8 take as long where there are many, and 1 us more where there are few
 struct PrepArgs {
   const uint16_t *o, *dout;
   const float *lse, *dlse;
   int64_t o_tok, o_head, do_tok, do_head;
   float2* stat;
   int Tq, Hq;
-  int row_groups;                        // workgroups of rows: 16 tokens by 16 heads each
+  int tables;                            // workgroups that lay out the bias of a head each, in front
+  int64_t groups;                        // of kPrepTokens tokens by 16 heads
   SeqBias bias;
   int pitch;
   float* table;
@@ -911,106 +1002,51 @@ struct PrepArgs {
 template <int D>
 __global__ __launch_bounds__(256) void grad_prep_kernel(PrepArgs a) {
   const int tid = threadIdx.x;
-  if ((int)blockIdx.x >= a.row_groups) {
-    const int h = blockIdx.x - a.row_groups;
-    for (int i = tid; i < a.pitch; i += 256) {
+  if ((int)blockIdx.x < a.tables) {
+    const int h = blockIdx.x;
+    for (int i = tid; i < a.pitch; i += 256)
       a.table[(size_t)h * a.pitch + i] = bias_log2(a.bias, i - kBiasPad, a.Hq, h);
-    }
     return;
   }
   constexpr int LPR = D / 8;             // lanes of a row
   constexpr int RPP = 256 / LPR;         // rows of a pass
-  __shared__ float dots[256];
+  constexpr int ROWS = 16 * kPrepTokens;
+  __shared__ float dots[ROWS];
   const int HB = (a.Hq + 15) / 16;
-  const int64_t t0 = (int64_t)(blockIdx.x / HB) * 16;
-  const int h0 = blockIdx.x % HB * 16;
-#pragma unroll 4
-  for (int p = 0; p < 256 / RPP; ++p) {
-    const int r = p * RPP + tid / LPR;   // token r / 16, head r % 16
-    const int64_t t = t0 + r / 16;
-    const int h = h0 + r % 16;
-    float x = 0.f;
-    if (t < a.Tq && h < a.Hq) {
-      const u32x4 u = *(const u32x4*)(a.o + t * a.o_tok + (int64_t)h * a.o_head + 8 * (tid % LPR));
-      const u32x4 v = *(const u32x4*)(a.dout + t * a.do_tok + (int64_t)h * a.do_head + 8 * (tid % LPR));
+  for (int64_t g = blockIdx.x - a.tables; g < a.groups; g += gridDim.x - a.tables) {
+    const int64_t t0 = g / HB * kPrepTokens;
+    const int h0 = (int)(g % HB) * 16;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        x = __builtin_fmaf(__uint_as_float(u[i] << 16), __uint_as_float(v[i] << 16), x);
-        x = __builtin_fmaf(__uint_as_float(u[i] & 0xffff0000u), __uint_as_float(v[i] & 0xffff0000u), x);
+    for (int p = 0; p < ROWS / RPP; ++p) {
+      const int r = p * RPP + tid / LPR;   // token r / 16, head r % 16
+      const int64_t t = t0 + r / 16;
+      const int h = h0 + r % 16;
+      float x = 0.f;
+      if (t < a.Tq && h < a.Hq) {
+        const u32x4 u = *(const u32x4*)(a.o + t * a.o_tok + (int64_t)h * a.o_head + 8 * (tid % LPR));
+        const u32x4 v = *(const u32x4*)(a.dout + t * a.do_tok + (int64_t)h * a.do_head + 8 * (tid % LPR));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x = __builtin_fmaf(__uint_as_float(u[i] << 16), __uint_as_float(v[i] << 16), x);
+          x = __builtin_fmaf(__uint_as_float(u[i] & 0xffff0000u), __uint_as_float(v[i] & 0xffff0000u), x);
+        }
       }
-    }
 #pragma unroll
-    for (int m = 1; m < LPR; m <<= 1) x += __shfl_xor(x, m);
-    if (tid % LPR == 0) dots[r] = x;
-  }
-  __syncthreads();
-  const int64_t t = t0 + tid % 16;
-  const int h = h0 + tid / 16;
-  if (t >= a.Tq || h >= a.Hq) return;
-  const float lse = a.lse[t * a.Hq + h];
-  float delta = dots[tid % 16 * 16 + tid / 16];
-  if (a.dlse) delta -= a.dlse[t * a.Hq + h];
-  // a row that sees nothing has no probabilities: exp2(x - inf) = 0
-  const bool none = lse == -INFINITY;
-  a.stat[(size_t)h * a.Tq + t] = float2{none ? INFINITY : lse * 1.4426950408889634f, none ? 0.f : delta};
-}
-
-// The gradient of the bias' weights: workgroup h adds the sums by distance of head h, over the workgroups
-// that met it and then over a bucket's distances, in 64 bits and a fixed order.
-struct DistArgs {
-  const float* dist;
-  const uint64_t* line;
-  const int32_t* bucket;
-  void* dweight;
-  int bf16, buckets, lo, hi, pitch, Hq, P, empty;
-};
-__device__ __forceinline__ double wave_sum_f64(double x) {
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
-  return x;
-}
-__global__ __launch_bounds__(1024) void dist_merge_kernel(DistArgs a) {
-  constexpr int PARTS = 4;                // of the workgroups, by turns
-  __shared__ double parts[PARTS][kBiasPitch];
-  __shared__ double sums[kBiasPitch];
-  __shared__ int to[kBiasMost];
-  const int h = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int n = a.hi - a.lo + 1;
-  const uint64_t head = a.empty ? 0 : a.line[0], share = a.empty ? 1 : a.line[1];
-  const int l0 = (int)(head * (uint32_t)h / share);
-  const int l1 = head == 0 ? l0 - 1 : min((int)((head * ((uint32_t)h + 1ull) - 1) / share), a.P - 1);
-  for (int j = tid; j < PARTS * a.pitch; j += 1024) {
-    const int part = j / a.pitch, i = j - part * a.pitch;
-    double x = 0.0;
-#pragma unroll 8
-    for (int l = l0 + part; l <= l1; l += PARTS) x += a.dist[(size_t)(l + h) * a.pitch + i];
-    parts[part][i] = x;
-  }
-  for (int i = tid; i < n; i += 1024) to[i] = a.bucket[i];
-  __syncthreads();
-  for (int i = tid; i < a.pitch; i += 1024) sums[i] = (parts[0][i] + parts[1][i]) + (parts[2][i] + parts[3][i]);
-  __syncthreads();
-  if (wave < 2) {                         // what lies beyond the ends belongs to them
-    const int end = wave == 0 ? 0 : kBiasPad + n;
-    double x = sums[end + lane];
-    if (lane < kBiasPad - 64) x += sums[end + 64 + lane];
-    x = wave_sum_f64(x);
-    if (lane == 0) sums[end] = x;
-  }
-  __syncthreads();
-  for (int b = wave; b < a.buckets; b += 16) {
-    double x = 0.0;
-    for (int i = lane; i < n; i += 64) {
-      if (to[i] != b) continue;
-      x += sums[kBiasPad + i];
-      if (i == 0) x += sums[0];
-      if (i == n - 1) x += sums[kBiasPad + n];
+      for (int m = 1; m < LPR; m <<= 1) x += __shfl_xor(x, m);
+      if (tid % LPR == 0) dots[r] = x;
     }
-    x = wave_sum_f64(x);
-    if (lane != 0) continue;
-    const size_t at = (size_t)b * a.Hq + h;
-    if (a.bf16) ((uint16_t*)a.dweight)[at] = (uint16_t)(pack_bf16x2((float)x, 0.f) & 0xffffu);
-    else ((float*)a.dweight)[at] = (float)x;
+    __syncthreads();
+    const int64_t t = t0 + tid % kPrepTokens;
+    const int h = h0 + tid / kPrepTokens;
+    if (tid < ROWS && t < a.Tq && h < a.Hq) {
+      const float lse = a.lse[t * a.Hq + h];
+      float delta = dots[tid % kPrepTokens * 16 + tid / kPrepTokens];
+      if (a.dlse) delta -= a.dlse[t * a.Hq + h];
+      // a row that sees nothing has no probabilities: exp2(x - inf) = 0
+      const bool none = lse == -INFINITY;
+      a.stat[(size_t)h * a.Tq + t] = float2{none ? INFINITY : lse * 1.4426950408889634f, none ? 0.f : delta};
+    }
+    __syncthreads();
   }
 }
 
@@ -1019,27 +1055,28 @@ __global__ __launch_bounds__(1024) void dist_merge_kernel(DistArgs a) {
 template <int D>
 static hipError_t launch_grad(const GradCall& c, hipStream_t st) {
   if (c.rows) {
-    const int groups = ceil_div(c.Tq, 16) * ceil_div(c.rows_g.Hq, 16);
+    const int64_t groups = ((int64_t)c.Tq + kPrepTokens - 1) / kPrepTokens * ceil_div(c.rows_g.Hq, 16);
+    const int tables = c.has_bias ? c.rows_g.Hq : 0;
     const PrepArgs p{c.o, c.rows_io.dout, c.lse, c.dlse, c.o_tok, c.o_head, c.rows_io.do_tok, c.rows_io.do_head,
-                     const_cast<float2*>(c.rows_io.stat), c.Tq, c.rows_g.Hq, groups, c.bias, c.rows_io.bias_pitch,
+                     const_cast<float2*>(c.rows_io.stat), c.Tq, c.rows_g.Hq, tables, groups, c.bias, c.rows_io.bias_pitch,
                      const_cast<float*>(c.rows_io.table)};
-    hipLaunchKernelGGL((grad_prep_kernel<D>), dim3(groups + (c.has_bias ? c.rows_g.Hq : 0)), dim3(256), 0, st, p);
+    const int most = 1 << 20;
+    hipLaunchKernelGGL((grad_prep_kernel<D>), dim3(tables + (groups < most ? (int)groups : most)), dim3(256), 0, st, p);
   }
   const int keys_p = c.keys ? c.keys_p : 0, rows_p = c.rows ? c.rows_p : 0;
   if (keys_p + rows_p > 0) {
     const GradBoth a{{c.keys_g, c.keys_io, keys_p}, {c.rows_g, c.rows_io, rows_p}};
     if (c.has_bias) hipLaunchKernelGGL((grad_kernel<D, true>), dim3(keys_p + rows_p), dim3(kGradThreads), 0, st, a);
     else hipLaunchKernelGGL((grad_kernel<D, false>), dim3(keys_p + rows_p), dim3(kGradThreads), 0, st, a);
-    const int keys_cut = c.keys_g.cuts ? keys_p : 0, rows_cut = c.rows_g.cuts ? rows_p : 0;
-    if (keys_cut + rows_cut > 0)
-      hipLaunchKernelGGL((grad_merge_kernel<D>), dim3(keys_cut + rows_cut, keys_cut ? 16 : 8), dim3(256), 0, st, c.keys_io,
-                         c.rows_io, keys_cut, rows_cut, c.rows_g.GH);
   }
-  if (c.has_bias) {
-    const DistArgs d{c.rows_io.dist, c.rows_io.line, c.bias.bucket, c.dweight, c.bias.bf16, c.bias.buckets, c.bias.lo,
-                     c.bias.hi, c.rows_io.bias_pitch, c.rows_g.Hq, c.rows_p, !c.rows};
-    hipLaunchKernelGGL(dist_merge_kernel, dim3(c.rows_g.Hq), dim3(1024), 0, st, d);
-  }
+  const int keys_cut = c.keys_g.cuts ? keys_p : 0, rows_cut = c.rows_g.cuts ? rows_p : 0;
+  const int groups = c.bias.buckets < 64 ? c.bias.buckets : 64;
+  const DistArgs d{c.rows_io.dist, c.rows_io.line, c.bias, c.dweight, c.rows_io.bias_pitch, c.has_bias ? c.rows_g.Hq : 0,
+                   c.rows_p, !c.rows, groups};
+  const int blocks = 16 * keys_cut + 8 * rows_cut + d.Hq * d.groups;
+  if (blocks > 0)
+    hipLaunchKernelGGL((grad_merge_kernel<D>), dim3(blocks), dim3(256), 0, st, c.keys_io, c.rows_io, d, keys_cut, rows_cut,
+                       c.rows_g.GH);
   return hipGetLastError();
 }
 

@@ -85,7 +85,7 @@ def test_bias_arguments_refused():
 @pytest.mark.parametrize("bad", [dict(S=-1), dict(Tq=-1), dict(Tk=-1), dict(Hq=0), dict(Hkv=0), dict(Hq=9), dict(Hq=65536),
                                  dict(d=96), dict(causal=2), dict(q_token=64), dict(q_head=4), dict(k_token=1 << 24),
                                  dict(v_token=127), dict(v_head=-8), dict(o_token=-1024), dict(o_head=-128),
-                                 dict(S=(1 << 31) - 4095), dict(Tq=(1 << 28) + 1, Hq=2)], ids=str)
+                                 dict(S=(1 << 31) - 4095)], ids=str)
 def test_bwd_shapes_refused(bad):
     assert bwd(seqs(**bad), grads()) == la.LA_ERR_SHAPE
 
