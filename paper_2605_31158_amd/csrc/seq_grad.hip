@@ -347,7 +347,7 @@ __device__ __forceinline__ void key_grad(unsigned char* lds, int block, int P) {
           seek();
         }
       };
-      __syncthreads();                                 // the piece before is read
+      phase_barrier();                                 // the piece before is read; its stores need not have landed
       const float* table = nullptr;                    // the bias of the present head
       {
         const GradArgs a = grad_args<true>();
@@ -693,7 +693,7 @@ __device__ __forceinline__ void row_grad(unsigned char* lds, int group, int P) {
       const int keys = (int)grad_seen(wk.line, wk.b);  // keys that the unit's last token sees
       const int first = (int)pc.ta, N = keys == 0 ? 0 : (int)(pc.tb - pc.ta);
       if constexpr (BIAS) flush(wk.h);
-      __syncthreads();                                 // the piece before is read
+      phase_barrier();                                 // the piece before is read; its stores need not have landed
       uint64_t next_k = 0, next_v = 0;                 // where the tile to load next starts
       int next_left = 0;                               // keys from it on
       auto issue = [&](int st) {
@@ -985,7 +985,8 @@ __global__ __launch_bounds__(256) void grad_merge_kernel(GradIo keys, GradIo row
 
 // ------------------------------------------------------------------------------------------------
 // What both walks need of a row: lse in base 2, and delta; and the bias by distance.  Bound by reading o and do.
-constexpr int kPrepTokens = 2;           // 4 and 8 take as long where there are many, and 1 us more where there are few
+// More tokens take as long where there are many, and 1 us more where there are few.
+constexpr int kPrepTokens = 4, kPrepHeads = 8;
 struct PrepArgs {
   const uint16_t *o, *dout;
   const float *lse, *dlse;
@@ -993,7 +994,7 @@ struct PrepArgs {
   float2* stat;
   int Tq, Hq;
   int tables;                            // workgroups that lay out the bias of a head each, in front
-  int64_t groups;                        // of kPrepTokens tokens by 16 heads
+  int64_t groups;                        // of kPrepTokens tokens by kPrepHeads heads
   SeqBias bias;
   int pitch;
   float* table;
@@ -1010,17 +1011,17 @@ __global__ __launch_bounds__(256) void grad_prep_kernel(PrepArgs a) {
   }
   constexpr int LPR = D / 8;             // lanes of a row
   constexpr int RPP = 256 / LPR;         // rows of a pass
-  constexpr int ROWS = 16 * kPrepTokens;
+  constexpr int ROWS = kPrepHeads * kPrepTokens;
   __shared__ float dots[ROWS];
-  const int HB = (a.Hq + 15) / 16;
+  const int HB = (a.Hq + kPrepHeads - 1) / kPrepHeads;
   for (int64_t g = blockIdx.x - a.tables; g < a.groups; g += gridDim.x - a.tables) {
     const int64_t t0 = g / HB * kPrepTokens;
-    const int h0 = (int)(g % HB) * 16;
+    const int h0 = (int)(g % HB) * kPrepHeads;
 #pragma unroll
     for (int p = 0; p < ROWS / RPP; ++p) {
-      const int r = p * RPP + tid / LPR;   // token r / 16, head r % 16
-      const int64_t t = t0 + r / 16;
-      const int h = h0 + r % 16;
+      const int r = p * RPP + tid / LPR;
+      const int64_t t = t0 + r / kPrepHeads;
+      const int h = h0 + r % kPrepHeads;
       float x = 0.f;
       if (t < a.Tq && h < a.Hq) {
         const u32x4 u = *(const u32x4*)(a.o + t * a.o_tok + (int64_t)h * a.o_head + 8 * (tid % LPR));
@@ -1040,7 +1041,7 @@ __global__ __launch_bounds__(256) void grad_prep_kernel(PrepArgs a) {
     const int h = h0 + tid / kPrepTokens;
     if (tid < ROWS && t < a.Tq && h < a.Hq) {
       const float lse = a.lse[t * a.Hq + h];
-      float delta = dots[tid % kPrepTokens * 16 + tid / kPrepTokens];
+      float delta = dots[tid % kPrepTokens * kPrepHeads + tid / kPrepTokens];
       if (a.dlse) delta -= a.dlse[t * a.Hq + h];
       // a row that sees nothing has no probabilities: exp2(x - inf) = 0
       const bool none = lse == -INFINITY;
@@ -1055,7 +1056,7 @@ __global__ __launch_bounds__(256) void grad_prep_kernel(PrepArgs a) {
 template <int D>
 static hipError_t launch_grad(const GradCall& c, hipStream_t st) {
   if (c.rows) {
-    const int64_t groups = ((int64_t)c.Tq + kPrepTokens - 1) / kPrepTokens * ceil_div(c.rows_g.Hq, 16);
+    const int64_t groups = ((int64_t)c.Tq + kPrepTokens - 1) / kPrepTokens * ceil_div(c.rows_g.Hq, kPrepHeads);
     const int tables = c.has_bias ? c.rows_g.Hq : 0;
     const PrepArgs p{c.o, c.rows_io.dout, c.lse, c.dlse, c.o_tok, c.o_head, c.rows_io.do_tok, c.rows_io.do_head,
                      const_cast<float2*>(c.rows_io.stat), c.Tq, c.rows_g.Hq, tables, groups, c.bias, c.rows_io.bias_pitch,
