@@ -32,7 +32,7 @@ struct GradTile {
   static constexpr int BYTES = ROWS * STRIDE;
   static constexpr int PER = BYTES / 4096;             // 1 KiB loads of each of the four waves
   __device__ static constexpr int swz(int r) {
-    return D == 128 ? ((r & 7) << 1) | ((r >> 3) & 1) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+    return D == 128 ? (r & 7) << 1 : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
   }
 };
 
