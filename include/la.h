@@ -387,8 +387,9 @@ la_status la_prompt_attn(const la_seqs* seqs, const void* q, const void* k, cons
  * i + lk - lq among its sequence's keys, and key n at distance n - that place,
  *   bias[h] = weight[bucket[clamp(distance, lo, hi) - lo]][h].
  * What the buckets are is the caller's: one for every distance, or ever wider ones.  A bucket outside
- * [0, buckets) has no bias (and takes no gradient).  A weight of -inf hides its distances; +inf and NaN are not
- * supported. */
+ * [0, buckets) has no bias (and takes no gradient).  A weight of -inf hides its distances; finite weights beyond
+ * +-2^24 (a type's lowest value as a mask) count as +-2^24; +inf and NaN are not supported.  A positive scale below
+ * 2^-60 is LA_ERR_ARG with a bias. */
 typedef struct la_rel_bias {
   int32_t lo, hi;            /* lo <= hi <= lo + 512, both within +-2^20 */
   int32_t buckets;           /* rows of the weights: 1 to 2^20 */

@@ -145,8 +145,9 @@ constexpr int kSgMfma = 0x008;
 constexpr int kSgDsRead = 0x100;
 
 // S^T = K Q^T for one 64-key tile: accumulators [MR keys][MR queries].  The K operand reads run
-// AHEAD operands ahead of their use, so LDS latency overlaps the matrix pipeline.
-template <int D>
+// AHEAD operands ahead of their use, so LDS latency overlaps the matrix pipeline.  ADD: it is added to what the
+// accumulators hold (a relative bias).
+template <int D, bool ADD = false>
 __device__ __forceinline__ void qk_tile(const unsigned char* __restrict__ kb,
                                         const bf16x8 (*qreg)[Mma<D>::QT],
                                         typename Mma<D>::Acc (*sacc)[Mma<D>::QT], int kbase) {
@@ -163,7 +164,8 @@ __device__ __forceinline__ void qk_tile(const unsigned char* __restrict__ kb,
 #pragma unroll
     for (int qt = 0; qt < X::QT; ++qt)
 #pragma unroll
-      for (int i = 0; i < X::AR; ++i) sacc[kt][qt][i] = 0.f;
+      for (int i = 0; i < X::AR; ++i)
+        if constexpr (!ADD) sacc[kt][qt][i] = 0.f;
 #pragma unroll
   for (int i = 0; i < NO; ++i)
 #pragma unroll

@@ -215,8 +215,12 @@ GradLayout grad_layout(const la_seqs& s, const la_rel_bias* bias, void* ws) {
   return w;
 }
 
-la_status check_bias(const la_rel_bias* bias, const int32_t* bucket, const void* weight) {
+// The logits are formed as scale (q.k + bias / scale): the quotient of the largest bias is finite above this scale.
+constexpr float kBiasScale = 0x1p-60f;
+
+la_status check_bias(const la_rel_bias* bias, const int32_t* bucket, const void* weight, float scale) {
   if (bad_bias(bias)) return LA_ERR_SHAPE;
+  if (scale > 0.0f && scale < kBiasScale) return LA_ERR_ARG;
   if (bias->dtype != LA_DTYPE_F32 && bias->dtype != LA_DTYPE_BF16) return LA_ERR_ARG;
   const uintptr_t word = bias->dtype == LA_DTYPE_F32 ? 3u : 1u;
   if (!bucket || !weight || ((uintptr_t)bucket & 3u) || ((uintptr_t)weight & word)) return LA_ERR_ARG;
@@ -340,7 +344,7 @@ la_status la_prompt_attn_bias(const la_seqs* seqs, const la_rel_bias* bias, cons
   if (((uintptr_t)cu_q | (uintptr_t)cu_k | (uintptr_t)lse) & 3u) return LA_ERR_ARG;
   SeqBias b{};
   if (bias) {
-    st = check_bias(bias, bucket, weight);
+    st = check_bias(bias, bucket, weight, scale);
     if (st != LA_OK) return st;
     b = SeqBias{bucket, weight, bias->dtype == LA_DTYPE_BF16, bias->buckets, bias->lo, bias->hi};
   }
@@ -437,7 +441,7 @@ la_status la_prompt_attn_bwd(const la_seqs* seqs, const la_prompt_grads* grads, 
   if (st != LA_OK) return st;
   if (!grads || isnan(scale) || isinf(scale)) return LA_ERR_ARG;
   if (bias) {
-    st = check_bias(bias, bucket, weight);
+    st = check_bias(bias, bucket, weight, scale);
     if (st != LA_OK) return st;
     if (!dweight || ((uintptr_t)dweight & (bias->dtype == LA_DTYPE_F32 ? 3u : 1u))) return LA_ERR_ARG;
   }

@@ -290,73 +290,61 @@ template <int D>
 struct WaveBias {
   using X = Mma<D>;
   int at[X::QT];                     // index of key 0's distance in the table, of this lane's first key
+  int row[X::QT];                    // the row's table
   float lo[X::QT], hi[X::QT];        // beyond the ends
   int first, last;                   // the first and last place of the wave's rows among the keys
 };
 
+// Where the wave's rows lie; the tables are whole behind the barrier that follows.
 template <int D>
-__device__ __forceinline__ void start_bias(WaveBias<D>& wb, float (*table)[kBiasPitch], const SeqArgs& a, const Walk& wk,
-                                           int r_off, int c, int lg) {
+__device__ __forceinline__ void start_bias(WaveBias<D>& wb, const SeqArgs& a, const Walk& wk, int r_off, int c, int lg) {
   using X = Mma<D>;
-  const int off = wk.q.lk - wk.q.lq;
-  int first = 0x7fffffff, last = -0x7fffffff;
-#pragma unroll
-  for (int qt = 0; qt < X::QT; ++qt) {
-    const Row row = unit_row(a.g, wk, r_off + X::MR * qt + c);
-    if (row.ok) {
-      first = min(first, row.token + off);
-      last = max(last, row.token + off);
-    }
-  }
-#pragma unroll
-  for (int m = 1; m < X::MR; m <<= 1) {
-    first = min(first, __shfl_xor(first, m));
-    last = max(last, __shfl_xor(last, m));
-  }
-  wb.first = __builtin_amdgcn_readfirstlane(first);
-  wb.last = __builtin_amdgcn_readfirstlane(last);
-  const int n = a.bias.hi - a.bias.lo;
+  const int off = wk.q.lk - wk.q.lq, t0 = wk.b * a.g.TB;
+  // the tokens of the wave's 32 rows, as unit_row has them
+  const int last = min(a.g.TB, wk.q.lq - t0) - 1;
+  wb.first = off + t0 + min((int)(((uint32_t)r_off * (uint32_t)a.g.gh_magic) >> 16), last);
+  wb.last = off + t0 + min((int)(((uint32_t)(r_off + 31) * (uint32_t)a.g.gh_magic) >> 16), last);
 #pragma unroll
   for (int qt = 0; qt < X::QT; ++qt) {
     const Row row = unit_row(a.g, wk, r_off + X::MR * qt + c);
     const int head = row.ok ? row.head - unit_head0(a.g, wk) : 0;
     // rows that do not exist read the places of one that does
     const int place = row.ok ? row.token + off : wb.first;
-    wb.at[qt] = head * kBiasPitch + 4 * lg + kBiasPad - a.bias.lo - place;
-    wb.lo[qt] = table[head][kBiasPad];
-    wb.hi[qt] = table[head][kBiasPad + n];
+    wb.row[qt] = head * kBiasPitch;
+    wb.at[qt] = wb.row[qt] + 4 * lg + kBiasPad - a.bias.lo - place;
+  }
+}
+// The bias beyond the ends, from the tables.
+template <int D>
+__device__ __forceinline__ void far_bias(WaveBias<D>& wb, const float* table, int distances, float scale_log2) {
+#pragma unroll
+  for (int qt = 0; qt < Mma<D>::QT; ++qt) {
+    wb.lo[qt] = table[wb.row[qt] + kBiasPad] * scale_log2;
+    wb.hi[qt] = table[wb.row[qt] + kBiasPad + distances] * scale_log2;
   }
 }
 
 // The unit's tables, by all threads.
 __device__ __forceinline__ void fill_bias(float (*table)[kBiasPitch], const SeqArgs& a, const Walk& wk) {
   const int heads = unit_heads(a.g, wk), head0 = unit_head0(a.g, wk), n = a.bias.hi - a.bias.lo + 1 + 2 * kBiasPad;
+  const float inv = 1.0f / a.io.scale_log2;
   for (int h = 0; h < heads; ++h)
-    for (int i = threadIdx.x; i < n; i += kThreads) table[h][i] = bias_log2(a.bias, i - kBiasPad, a.g.Hq, head0 + h);
+    for (int i = threadIdx.x; i < n; i += kThreads) table[h][i] = bias_log2(a.bias, i - kBiasPad, a.g.Hq, head0 + h) * inv;
 }
 
-// The bias of a tile: added to the scaled logits (whose scale is 1 then), or the shift of each row.
+// The bias of a tile that needs the table, where the logits are added to.
 template <int D>
-__device__ __forceinline__ float add_bias(const WaveBias<D>& wb, const float* table, typename Mma<D>::Acc (*sacc)[Mma<D>::QT],
-                                          float* shift, int key0, int lo, int hi, float scale_log2) {
+__device__ __forceinline__ void near_bias(const WaveBias<D>& wb, const float* table,
+                                          typename Mma<D>::Acc (*sacc)[Mma<D>::QT], int key0) {
   using X = Mma<D>;
-  const bool left = key0 + 63 - wb.first <= lo, right = key0 - wb.last >= hi;
-  if (left || right) {
-#pragma unroll
-    for (int qt = 0; qt < X::QT; ++qt) shift[qt] = left ? wb.lo[qt] : wb.hi[qt];
-    return scale_log2;
-  }
 #pragma unroll
   for (int qt = 0; qt < X::QT; ++qt) {
-    shift[qt] = 0.f;
     const float* at = table + (wb.at[qt] + key0);
 #pragma unroll
     for (int kt = 0; kt < KT / X::MR; ++kt)
 #pragma unroll
-      for (int i = 0; i < X::AR; ++i)
-        sacc[kt][qt][i] = __builtin_fmaf(sacc[kt][qt][i], scale_log2, at[X::MR * kt + X::acc_row(i)]);
+      for (int i = 0; i < X::AR; ++i) sacc[kt][qt][i] = at[X::MR * kt + X::acc_row(i)];
   }
-  return 1.0f;
 }
 
 // The arguments of seq_attn_kernel, read anew: 50 scalar registers that a piece needs at its ends must
@@ -443,31 +431,45 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
             // consecutive units mostly have the same heads; the waves read no table of the piece before any more, as
             // its last iteration ended with a barrier
             const int heads = unit_head0(a.g, wk);
-            if (heads != table_head) {
-              table_head = heads;
-              fill_bias(table, a, wk);
-              __syncthreads();
-            }
-            start_bias<D>(wb, table, a, wk, r_off, c, lg);
+            if (heads != table_head) fill_bias(table, a, wk);
+            table_head = heads;
+            start_bias<D>(wb, a, wk, r_off, c, lg);
           }
           const int open = a.g.causal ? max(0, wk.q.lk - wk.q.lq + wk.b * a.g.TB + 1) : wk.q.lk;
           key_open = min(open, wk.q.lk) - 63;
         }
         __builtin_amdgcn_s_waitcnt(0);
         phase_barrier();
+        if constexpr (BIAS) far_bias<D>(wb, &table[0][0], bias_hi - bias_lo, w.scale_log2);
         auto m_phase = [&](int i, const unsigned char* kcur, const unsigned char* vprev) {
           const int key0 = 64 * (pc.ta + i);
           if (i > 0 && key0 - 64 < st.seen) pv_tile<D>(vprev, st.pb, st.oacc, w.vbase);
-          if (i < N && key0 < st.seen) qk_tile<D>(kcur, st.qreg, st.sacc, w.kbase);
+          if (i < N && key0 < st.seen) {
+            if constexpr (BIAS) {
+              if (key0 + 63 - wb.first > bias_lo && key0 - wb.last < bias_hi) {
+                near_bias<D>(wb, &table[0][0], st.sacc, key0);
+                qk_tile<D, true>(kcur, st.qreg, st.sacc, w.kbase);
+              } else {
+                qk_tile<D>(kcur, st.qreg, st.sacc, w.kbase);
+              }
+            } else {
+              qk_tile<D>(kcur, st.qreg, st.sacc, w.kbase);
+            }
+          }
         };
         auto v_phase = [&](int i) {
           const int key0 = 64 * (pc.ta + i);
           if (i >= 0 && i < N && key0 < st.seen) {
             if constexpr (BIAS) {
+              const bool left = key0 + 63 - wb.first <= bias_lo, right = key0 - wb.last >= bias_hi;
               float shift[X::QT];
-              const float scale = add_bias<D>(wb, &table[0][0], st.sacc, shift, key0, bias_lo, bias_hi, w.scale_log2);
+#pragma unroll
+              for (int qt = 0; qt < X::QT; ++qt) {
+                const float lo = wb.lo[qt], hi = wb.hi[qt];
+                shift[qt] = left ? lo : (right ? hi : 0.f);
+              }
               if (__builtin_expect(key0 >= key_open, 0)) mask_tile<D>(st.sacc, key0, 0, w);
-              softmax_tile<D, true>(st.sacc, st.pb, st.oacc, st.m_run, st.l_run, scale, shift);
+              softmax_tile<D, true>(st.sacc, st.pb, st.oacc, st.m_run, st.l_run, w.scale_log2, shift);
             } else {
               if (__builtin_expect(key0 >= key_open, 0)) mask_tile<D>(st.sacc, key0, 0, w);
               softmax_tile<D>(st.sacc, st.pb, st.oacc, st.m_run, st.l_run, w.scale_log2);

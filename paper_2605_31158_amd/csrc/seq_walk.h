@@ -25,6 +25,8 @@
 // search over the runs, in registers.
 #pragma once
 
+#include <math.h>
+
 #include "la_internal.h"
 
 namespace la {
@@ -75,12 +77,14 @@ struct SeqBias {
 
 namespace {
 
-// The bias of bucket bucket[i] and head h in base 2.
+// The bias of bucket bucket[i] and head h in base 2.  Finite weights are held to 2^24, far beyond what a weight of zero
+// takes: of larger ones (a type's lowest value as a mask) a logit's rounding would be worth whole factors of 2^128.
 __device__ __forceinline__ float bias_log2(const SeqBias& b, int i, int Hq, int h) {
   const int n = b.bucket[min(max(i, 0), b.hi - b.lo)];
   if (n < 0 || n >= b.buckets) return 0.f;
   const size_t at = (size_t)n * Hq + h;
-  const float w = b.bf16 ? __uint_as_float((uint32_t)((const uint16_t*)b.weight)[at] << 16) : ((const float*)b.weight)[at];
+  float w = b.bf16 ? __uint_as_float((uint32_t)((const uint16_t*)b.weight)[at] << 16) : ((const float*)b.weight)[at];
+  if (fabsf(w) > 16777216.f && w != -INFINITY) w = copysignf(16777216.f, w);
   return w * 1.4426950408889634f;
 }
 

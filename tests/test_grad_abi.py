@@ -68,6 +68,7 @@ def test_bias_arguments_refused():
                 assert call(**{name: None}) == la.LA_ERR_ARG, name
             assert call(bucket=ctypes.c_void_p(4098)) == la.LA_ERR_ARG
             assert call(weight=ctypes.c_void_p(4096 + word)) == la.LA_ERR_ARG
+    assert fwd(seqs(), rel(), scale=1e-20) == la.LA_ERR_ARG and bwd(seqs(), grads(), rel(), scale=1e-20) == la.LA_ERR_ARG
     for call in (lambda b: fwd(seqs(), b), lambda b: bwd(seqs(), grads(), b)):
         assert call(rel(dtype=2)) == la.LA_ERR_ARG and call(rel(dtype=-1)) == la.LA_ERR_ARG
     assert bwd(seqs(), grads(), rel(), dw=None) == la.LA_ERR_ARG

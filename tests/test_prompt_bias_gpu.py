@@ -102,6 +102,35 @@ def test_weights_that_hide_and_buckets_that_are_none(d):
     R.check(o, lse, G.forward(q, k, v, lq, lk, False, bias=b), "buckets outside the weights")
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("low", [-1e9, None], ids=["-1e9", "lowest"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_large_finite_weights_as_masks(d, low, dtype):
+    # where a row sees any other key they are as -inf, to the bit; a row of nothing else stays finite
+    lq, lk = [200, 77], [260, 77]
+    q, k, v = make(lq, lk, 4, 4, d, 27)
+    cu_q, cu_k = R.starts(lq), R.starts(lk)
+    b = rel(4, 28, dtype=dtype)
+    hidden = b._replace(weight=b.weight.clone())
+    for x, value in ((b, torch.finfo(dtype).min if low is None else low), (hidden, -torch.inf)):
+        x.weight[9:16, 0] = x.weight[20:, 0] = x.weight[3, 1] = value
+        x.weight[:, 2] = value
+    do = torch.randn(q.shape, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda").to(torch.bfloat16)
+    got, want = [], []
+    for x, y in ((b, got), (hidden, want)):
+        o, lse = la.prompt_attn(q, k, v, cu_q, cu_k, causal=False, want_lse=True, bias=x)
+        y += [o, lse, *la.prompt_attn_bwd(do, q, k, v, o, lse, cu_q, cu_k, causal=False, bias=x)]
+    for x, y in zip(got, want):
+        assert torch.isfinite(x).all()
+        keep = [h for h in range(4) if h != 2]
+        assert torch.equal(x[:, keep], y[:, keep])
+    for s, (a, n, m) in enumerate(((0, 200, 260), (200, 77, 77))):
+        # some average of the values: of a logit next to 2^24 steps of 2 are left (fp32 has 24 bits), no more
+        v2 = v[260 * s: 260 * s + m, 2].double()
+        o2 = got[0][a: a + n, 2].double()
+        assert bool((o2 <= v2.amax(0) + 2.0 ** -6).all()) and bool((o2 >= v2.amin(0) - 2.0 ** -6).all())
+
+
 def test_large_biases_scales_and_bf16_weights():
     lq = [150, 400]
     q, k, v = make(lq, lq, 4, 2, 128, 21, qscale=1.0)
