@@ -916,7 +916,9 @@ def prompt_attn_bwd(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch
         rel = _rel_bias(bias, dev, Hq)
     if out is None:
         dq = torch.empty_like(q, memory_format=torch.contiguous_format)
-        dk, dv = (torch.empty_like(x, memory_format=torch.contiguous_format) for x in (k, v))
+        dk = torch.empty_like(k, memory_format=torch.contiguous_format)
+        dv = torch.empty_like(v, memory_format=torch.contiguous_format)
+        strides = (Hq * d, d, Hkv * d, d, Hkv * d, d)
         if bias is not None:
             dw = torch.empty_like(bias.weight)
     elif len(out) != (3 if bias is None else 4):
@@ -928,8 +930,9 @@ def prompt_attn_bwd(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch
             if not isinstance(dw, torch.Tensor) or dw.dtype is not bias.weight.dtype or dw.shape != bias.weight.shape \
                     or not dw.is_contiguous() or dw.get_device() != dev:
                 raise ValueError("dweight must be a contiguous tensor like bias.weight")
-    grads = PromptGrads(dt, dh, *_rows("dq", dq, dev, Hq, d, Tq)[3:], *_rows("dk", dk, dev, Hkv, d, Tk)[3:],
-                        *_rows("dv", dv, dev, Hkv, d, Tk)[3:])
+        strides = (*_rows("dq", dq, dev, Hq, d, Tq)[3:], *_rows("dk", dk, dev, Hkv, d, Tk)[3:],
+                   *_rows("dv", dv, dev, Hkv, d, Tk)[3:])
+    grads = PromptGrads(dt, dh, *strides)
     seqs = _seqs(S, Tq, Tk, Hq, Hkv, d, 1 if causal else 0, qt, qh, ot, oh, kt, kh, vt, vh)
     wp, nbytes, ws = _scratch(lib().la_prompt_bwd_ws_bytes(seqs, rel), q, dev, ws)
     _on_device(dev, "la_prompt_attn_bwd", seqs, ctypes.byref(grads), rel, do.data_ptr(), q.data_ptr(), k.data_ptr(),
