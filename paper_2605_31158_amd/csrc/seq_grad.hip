@@ -258,7 +258,8 @@ constexpr int key_lds() {
   return 4 * 64 * 128 + 2 * GradTile<D, 64>::BYTES + 2 * kStatBytes;
 }
 
-template <int D, bool BIAS>
+// ROTATE: a unit's inner tiles start where those of the workgroups beside it are, see below.
+template <int D, bool BIAS, bool ROTATE>
 __device__ __forceinline__ void key_grad(unsigned char* lds, int block, int P) {
   using X = Mma<D>;
   constexpr int QT = D == 128 ? 32 : 64;               // query rows of a tile
@@ -299,6 +300,7 @@ __device__ __forceinline__ void key_grad(unsigned char* lds, int block, int P) {
     }
   }
   const int w0 = 32 * lw;                              // the wave's first key of the unit
+  uint32_t done = 0;                                   // tiles so far
   typename X::Acc dk[D / X::MR][X::QT], dv[D / X::MR][X::QT];
   bf16x8 kreg[D / X::KC][X::QT];
 
@@ -314,10 +316,21 @@ __device__ __forceinline__ void key_grad(unsigned char* lds, int block, int P) {
       const int key0 = wk.b * kGradRows + w0;          // the wave's first key
       const int seen = __builtin_amdgcn_readfirstlane((int)(grad_seen(wk.line, wk.b) / QT));
       const int first = (lq + QT - 1) / QT - seen;     // first query tile that sees a key of the unit
-      // the inner tiles are the `seen` tiles of each head in turn
+      // the inner tiles are the `seen` tiles of each head in turn, from `begin` to the piece's end and then from its
+      // start: workgroups that walk the same queries read the same tiles at the same time
       int64_t left = seen == 0 ? 0 : pc.tb - pc.ta;
-      int head = __builtin_amdgcn_readfirstlane(seen == 0 ? 0 : (int)(pc.ta / seen));       // of the present tile
-      int tile = __builtin_amdgcn_readfirstlane(seen == 0 ? 0 : (int)(pc.ta - (int64_t)head * seen));
+      int64_t begin = pc.ta;
+      if (ROTATE && left > 0 && left < (1 << 30)) {
+        const int nq = seen + first;
+        const uint64_t at = (uint64_t)done % ((uint64_t)nq * wk.line.mult);
+        const int64_t i = (int64_t)(at / (uint32_t)nq) * seen + max((int)(at % (uint32_t)nq) - first, 0);
+        if (i >= pc.ta && i < pc.tb) begin = i;
+        done += (uint32_t)left;
+      }
+      const int seen1 = max(seen, 1);
+      int head = __builtin_amdgcn_readfirstlane((int)(begin / seen1));              // of the present tile
+      int tile = __builtin_amdgcn_readfirstlane((int)(begin % seen1));
+      int to_end = begin == pc.ta ? 0 : (int)(pc.tb - begin);      // tiles to load before the piece's start, if that is due
       // the tile to load next, and where its rows are
       int next_head = head, next_tile = tile;
       uint64_t next_q, next_do, next_stat;
@@ -337,7 +350,12 @@ __device__ __forceinline__ void key_grad(unsigned char* lds, int block, int P) {
         // whole words of 16 bytes: the row behind an odd number of them is masked
         if (lw == 0)
           stat_issue(stat + st * kStatBytes, nullptr, first_lane_u64(next_stat), __builtin_amdgcn_readfirstlane((rows + 1) / 2 * 16u), lane);
-        if (++next_tile < seen) {
+        ++next_tile;
+        if (ROTATE && --to_end == 0) {
+          next_head = (int)(pc.ta / seen1);
+          next_tile = (int)(pc.ta % seen1);
+          seek();
+        } else if (next_tile < seen) {
           next_q += (uint64_t)QT * q_stride;
           next_do += (uint64_t)QT * do_stride;
           next_stat += QT * 8;
@@ -393,21 +411,20 @@ __device__ __forceinline__ void key_grad(unsigned char* lds, int block, int P) {
       const bool causal = grad_args<true>().g.causal;
       const int from = key0 < wk.q.lk ? (causal ? key0 - off : 0) : 0x7fffffff;
       const int whole_from = causal ? key0 + 31 - off : 0;
-      for (int st = 0; left > 0; --left, st ^= 1) {
+      for (int st = 0, table_head = head; left > 0; --left, st ^= 1) {
         __builtin_amdgcn_s_waitcnt(0);
         phase_barrier();
         const int row0 = (first + tile) * QT;
         if constexpr (BIAS) {
-          if (tile == 0) {
+          if (head != table_head) {
+            table_head = head;
             const GradArgs a = grad_args<true>();
             table = a.io.table + (int64_t)(wk.h * a.g.G + head) * a.io.bias_pitch;
             far_bias(far, table);
           }
         }
-        if (++tile == seen) {
-          tile = 0;
-          ++head;
-        }
+        head = next_head;
+        tile = next_tile;
         if (left > 1) issue(st ^ 1);
         if (row0 + (QT - 1) < from) continue;
         const unsigned char* qt = ring + st * (2 * T::BYTES);
@@ -599,7 +616,7 @@ constexpr int row_lds() {
   return 4 * GradTile<D, KT>::BYTES + (BIAS ? 4 * (256 * diagonal_blocks<D>() + kBiasPitch) * 4 : 0);
 }
 
-template <int D, bool BIAS>
+template <int D, bool BIAS, bool ROTATE>
 __device__ __forceinline__ void row_grad(unsigned char* lds, int group, int P) {
   using X = Mma<D>;
   constexpr int NT = KT / X::MR;
@@ -678,6 +695,7 @@ __device__ __forceinline__ void row_grad(unsigned char* lds, int group, int P) {
     v_off[i] = grad_slot<D, KT>(lw, i, lane, v_stride);
   }
   const int w0 = 32 * lw;
+  uint32_t done = 0;                                   // tiles so far
   typename X::Acc dq[D / X::MR][X::QT];
   bf16x8 qreg[D / X::KC][X::QT], doreg[D / X::KC][X::QT];
 
@@ -691,7 +709,16 @@ __device__ __forceinline__ void row_grad(unsigned char* lds, int group, int P) {
     if (pc.tb > pc.ta) {
       const int lk = wk.q.lk, off = wk.q.lk - wk.q.lq;
       const int keys = (int)grad_seen(wk.line, wk.b);  // keys that the unit's last token sees
-      const int first = (int)pc.ta, N = keys == 0 ? 0 : (int)(pc.tb - pc.ta);
+      const int N = keys == 0 ? 0 : (int)(pc.tb - pc.ta);
+      // as in key_grad: from `first` to the piece's end and then from its start
+      int first = (int)pc.ta;
+      if (ROTATE && N > 0) {
+        const int at = (int)(done % (((uint32_t)lk + KT - 1) / KT));
+        if (at >= pc.ta && at < pc.tb) first = at;
+        done += (uint32_t)N;
+      }
+      first = __builtin_amdgcn_readfirstlane(first);
+      int to_end = first == (int)pc.ta ? 0 : (int)pc.tb - first;   // tiles to load before the piece's start, if that is due
       if constexpr (BIAS) flush(wk.h);
       phase_barrier();                                 // the piece before is read; its stores need not have landed
       uint64_t next_k = 0, next_v = 0;                 // where the tile to load next starts
@@ -701,9 +728,11 @@ __device__ __forceinline__ void row_grad(unsigned char* lds, int group, int P) {
         unsigned char* dst = ring + st * (2 * T::BYTES) + lw * (T::BYTES / 4);
         grad_issue<D, KT>(dst, nullptr, first_lane_u64(next_k), __builtin_amdgcn_readfirstlane(rows * k_stride), k_off);
         grad_issue<D, KT>(dst + T::BYTES, nullptr, first_lane_u64(next_v), __builtin_amdgcn_readfirstlane(rows * v_stride), v_off);
-        next_k += (uint64_t)KT * k_stride;
-        next_v += (uint64_t)KT * v_stride;
-        next_left -= KT;
+        int tiles = 1;
+        if (ROTATE && --to_end == 0) tiles = 1 - N;
+        next_k += (uint64_t)((int64_t)tiles * KT * (int64_t)k_stride);
+        next_v += (uint64_t)((int64_t)tiles * KT * (int64_t)v_stride);
+        next_left -= tiles * KT;
       };
       float lse[X::QT], delta[X::QT];
       int limit[X::QT], wave_keys = 0, wave_open = 0x7fffffff;
@@ -766,10 +795,12 @@ __device__ __forceinline__ void row_grad(unsigned char* lds, int group, int P) {
       }
       wave_keys = __builtin_amdgcn_readfirstlane(wave_keys);       // keys that some row of the wave sees
       wave_open = __builtin_amdgcn_readfirstlane(wave_open);       // and that all of them see
-      int key0 = 64 * first;
-      for (int left = N, st = 0; left > 0; --left, st ^= 1, key0 += KT) {
+      int next_key0 = 64 * first;
+      for (int left = N, st = 0; left > 0; --left, st ^= 1) {
         __builtin_amdgcn_s_waitcnt(0);
         phase_barrier();
+        const int key0 = next_key0;
+        next_key0 = lk - next_left;
         if (left > 1) issue(st ^ 1);
         if (key0 >= wave_keys) continue;
         const unsigned char* kt = ring + st * (2 * T::BYTES);
@@ -870,13 +901,13 @@ __device__ __forceinline__ void row_grad(unsigned char* lds, int group, int P) {
 }
 
 // One launch for both: the workgroups of dK and dV, which take longer, come first, and those of dQ start as they end.
-template <int D, bool BIAS>
+template <int D, bool BIAS, bool ROTATE>
 __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void grad_kernel(GradBoth) {
   constexpr int LDS = key_lds<D>() > row_lds<D, BIAS>() ? key_lds<D>() : row_lds<D, BIAS>();
   __shared__ __attribute__((aligned(1024))) unsigned char lds[LDS];
   const int keys_p = grad_args<true>().P;
-  if ((int)blockIdx.x < keys_p) key_grad<D, BIAS>(lds, blockIdx.x, keys_p);
-  else row_grad<D, BIAS>(lds, blockIdx.x - keys_p, gridDim.x - keys_p);
+  if ((int)blockIdx.x < keys_p) key_grad<D, BIAS, ROTATE>(lds, blockIdx.x, keys_p);
+  else row_grad<D, BIAS, ROTATE>(lds, blockIdx.x - keys_p, gridDim.x - keys_p);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -1067,8 +1098,12 @@ static hipError_t launch_grad(const GradCall& c, hipStream_t st) {
   const int keys_p = c.keys ? c.keys_p : 0, rows_p = c.rows ? c.rows_p : 0;
   if (keys_p + rows_p > 0) {
     const GradBoth a{{c.keys_g, c.keys_io, keys_p}, {c.rows_g, c.rows_io, rows_p}};
-    if (c.has_bias) hipLaunchKernelGGL((grad_kernel<D, true>), dim3(keys_p + rows_p), dim3(kGradThreads), 0, st, a);
-    else hipLaunchKernelGGL((grad_kernel<D, false>), dim3(keys_p + rows_p), dim3(kGradThreads), 0, st, a);
+    const dim3 grid(keys_p + rows_p), block(kGradThreads);
+    // the rotated walk is for calls without a mask and a bias: a 480P chunk over its context 1740 -> 1615 us; with a
+    // mask it takes as long or 1.5 % longer, with a bias its variables cost more than it gains (d 128: 435 -> 486)
+    if (c.has_bias) hipLaunchKernelGGL((grad_kernel<D, true, false>), grid, block, 0, st, a);
+    else if (c.keys_g.causal) hipLaunchKernelGGL((grad_kernel<D, false, false>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((grad_kernel<D, false, true>), grid, block, 0, st, a);
   }
   const int keys_cut = c.keys_g.cuts ? keys_p : 0, rows_cut = c.rows_g.cuts ? rows_p : 0;
   const int groups = c.bias.buckets < 64 ? c.bias.buckets : 64;

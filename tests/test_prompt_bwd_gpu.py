@@ -71,6 +71,23 @@ def test_against_64_bits(case, biased):
         assert torch.equal(x, y)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("form", [([2500], [3000], 16, 16), ([1300, 200], [2300, 900], 32, 16), ([3000, 1], [150, 4000], 18, 9)],
+                         ids=str)
+@pytest.mark.parametrize("causal", [False, True])
+def test_several_units_to_a_workgroup(form, d, causal):
+    # more units of 128 rows than workgroups: without a mask a unit's walk starts in the middle and wraps
+    lq, lk, Hq, Hkv = form
+    q, k, v = make(lq, lk, Hq, Hkv, d, 95)
+    cu_q, cu_k = R.starts(lq), R.starts(lk)
+    o, lse = left(q, k, v, lq, lk, causal)
+    do = grad_of(q, 96)
+    got = la.prompt_attn_bwd(do, q, k, v, o, lse, cu_q, cu_k, causal=causal)
+    G.check(got, G.backward(do, q, k, v, o, lse, lq, lk, causal), f"{form} d {d} causal {causal}")
+    for x, y in zip(got, la.prompt_attn_bwd(do, q, k, v, o, lse, cu_q, cu_k, causal=causal)):
+        assert torch.equal(x, y)
+
+
 BIASES = [
     # (buckets, reach, both, weights)
     (8, 16, False, torch.float32),
