@@ -6,7 +6,24 @@
 //
 // Two walks over the pairs, so that no sum needs atomics and results repeat bit for bit: key_grad holds 128 keys of a
 // key head and goes over the queries that see them (four products, dK and dV in registers), row_grad holds 128 packed
-// query rows and goes over their keys (three, dQ in registers).
+// query rows and goes over their keys (three, dQ in registers).  Seven products instead of five: dQ summed from the
+// first walk would be one fp32 row for each of a head's runs of keys, and dS stored for a product of its own 2 bytes a
+// pair, both more time in memory than the two products take.  Of a workgroup's four waves each has 32 of the 128 rows;
+// two workgroups run on a CU, one of each walk, so that one's exponentials lie under the other's products without a
+// barrier between them.  S and dP of a tile stay in registers, as they lie in them they are the operands of the
+// products that follow; Q and dO, or K and V, come by asynchronous loads into two stages of LDS, one barrier a tile.
+//
+// P and dS are rounded to bf16 (by at most 2^-8 of themselves) as operands, which run at 16 times fp32's rate; dS is
+// formed from P before its rounding, and the bias' gradient sums it unrounded.  Relative rms error against 64 bits
+// 0.0024, of which the result's own rounding makes 0.0017.
+//
+// Bound, where sequences are long, by the card's power: 8192 causal tokens, 16 heads over 4, d 128, take 781 us, 1.23
+// PFLOP/s over seven products (0.88 over the five that are needed) where a large bf16 product of random data
+// reaches 1.36 to 1.38 (the matrix pipeline is 55 % busy, as it is there); half the vector instructions in the
+// loops, or fewer LDS conflicts, moved it by 1 to 3 %.  d 64 does the same vector work for half the products: 468 us,
+// 1.03 PFLOP/s.  Short sequences: a unit costs 3.5 us beside its tiles (Q, dO or K, V, the first tile, the results), a
+// tile of 64 by 128 pairs 2.1 us where two walks share a CU, and the start (finding the stretch) 2.5: 48 prompts of 1
+// to 300 tokens, 16 heads over 4, d 64, 32 us.
 #include <math.h>
 
 #include <type_traits>
@@ -24,7 +41,10 @@ constexpr int kGradThreads = 256;        // four waves, each with 32 of a unit's
 
 // A tile of ROWS rows of D bf16 in LDS that is read both ways: as operands along d (16 bytes of MR rows) and
 // transposed, as operands along the rows (chunks of 2 MR bytes of 4 rows a lane group).  The 16-byte slots of
-// row r are permuted by an exclusive or with swz(r), for which both spread over all 64 banks.
+// row r are permuted by an exclusive or with swz(r), for which both spread over all 64 banks.  (A 16-byte read takes
+// lanes 0-3, 12-15 and 20-27 at once, then 4-11, 16-19 and 28-31, and so on: rows r and r + 8 of one 16-lane group
+// never meet, so that three bits do.  With the row's fourth bit as the lowest there are 0.59 conflicts an access and
+// 3 % more time.)
 template <int D, int ROWS>
 struct GradTile {
   static constexpr int STRIDE = D * 2;
@@ -258,7 +278,10 @@ constexpr int key_lds() {
   return 4 * 64 * 128 + 2 * GradTile<D, 64>::BYTES + 2 * kStatBytes;
 }
 
-// ROTATE: a unit's inner tiles start where those of the workgroups beside it are, see below.
+// ROTATE: a unit's inner tiles start where those of the workgroups beside it are.  Bound by power and the products (see
+// above); what it reads beside them is a tile of Q and dO for 128 keys, 16 KB for 4.2 MFLOP at d 128, which the L2
+// has to serve: without a mask all units are alike, and with the walks out of step a 480P chunk over its context (16
+// heads) read 8.6 GB from beyond the L2, in step 2.0.
 template <int D, bool BIAS, bool ROTATE>
 __device__ __forceinline__ void key_grad(unsigned char* lds, int block, int P) {
   using X = Mma<D>;
@@ -346,10 +369,12 @@ __device__ __forceinline__ void key_grad(unsigned char* lds, int block, int P) {
         const uint32_t rows = (uint32_t)min(lq - (first + next_tile) * QT, QT);
         unsigned char* dst = ring + st * (2 * T::BYTES) + lw * (T::BYTES / 4);
         grad_issue<D, QT>(dst, nullptr, first_lane_u64(next_q), __builtin_amdgcn_readfirstlane(rows * q_stride), q_off);
-        grad_issue<D, QT>(dst + T::BYTES, nullptr, first_lane_u64(next_do), __builtin_amdgcn_readfirstlane(rows * do_stride), do_off);
+        grad_issue<D, QT>(dst + T::BYTES, nullptr, first_lane_u64(next_do),
+                          __builtin_amdgcn_readfirstlane(rows * do_stride), do_off);
         // whole words of 16 bytes: the row behind an odd number of them is masked
         if (lw == 0)
-          stat_issue(stat + st * kStatBytes, nullptr, first_lane_u64(next_stat), __builtin_amdgcn_readfirstlane((rows + 1) / 2 * 16u), lane);
+          stat_issue(stat + st * kStatBytes, nullptr, first_lane_u64(next_stat),
+                     __builtin_amdgcn_readfirstlane((rows + 1) / 2 * 16u), lane);
         ++next_tile;
         if (ROTATE && --to_end == 0) {
           next_head = (int)(pc.ta / seen1);
@@ -616,6 +641,7 @@ constexpr int row_lds() {
   return 4 * GradTile<D, KT>::BYTES + (BIAS ? 4 * (256 * diagonal_blocks<D>() + kBiasPitch) * 4 : 0);
 }
 
+// As key_grad, with 32 KB of K and V (d 128) for 6.3 MFLOP.
 template <int D, bool BIAS, bool ROTATE>
 __device__ __forceinline__ void row_grad(unsigned char* lds, int group, int P) {
   using X = Mma<D>;
@@ -727,7 +753,8 @@ __device__ __forceinline__ void row_grad(unsigned char* lds, int group, int P) {
         const uint32_t rows = (uint32_t)min(next_left, KT);
         unsigned char* dst = ring + st * (2 * T::BYTES) + lw * (T::BYTES / 4);
         grad_issue<D, KT>(dst, nullptr, first_lane_u64(next_k), __builtin_amdgcn_readfirstlane(rows * k_stride), k_off);
-        grad_issue<D, KT>(dst + T::BYTES, nullptr, first_lane_u64(next_v), __builtin_amdgcn_readfirstlane(rows * v_stride), v_off);
+        grad_issue<D, KT>(dst + T::BYTES, nullptr, first_lane_u64(next_v),
+                          __builtin_amdgcn_readfirstlane(rows * v_stride), v_off);
         int tiles = 1;
         if (ROTATE && --to_end == 0) tiles = 1 - N;
         next_k += (uint64_t)((int64_t)tiles * KT * (int64_t)k_stride);
@@ -900,7 +927,9 @@ __device__ __forceinline__ void row_grad(unsigned char* lds, int group, int P) {
   if constexpr (BIAS) flush(last_head + 1);
 }
 
-// One launch for both: the workgroups of dK and dV, which take longer, come first, and those of dQ start as they end.
+// One launch for both walks, the workgroups of dK and dV, which take longer, in front: with as many of either as there
+// are CUs every CU gets one of each (one after the other 836 us for 8192 tokens as above, together 780; one prompt of
+// 77 tokens, 16 heads, d 64, 27 and 10).
 template <int D, bool BIAS, bool ROTATE>
 __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void grad_kernel(GradBoth) {
   constexpr int LDS = key_lds<D>() > row_lds<D, BIAS>() ? key_lds<D>() : row_lds<D, BIAS>();
@@ -1015,7 +1044,8 @@ __global__ __launch_bounds__(256) void grad_merge_kernel(GradIo keys, GradIo row
 }
 
 // ------------------------------------------------------------------------------------------------
-// What both walks need of a row: lse in base 2, and delta; and the bias by distance.  Bound by reading o and do.
+// What both walks need of a row: lse in base 2, and delta; and the bias by distance.  Bound by reading o and do: 67 MB
+// (8192 tokens, 16 heads, d 128) in 12.2 us, 5.5 TB/s.
 // More tokens take as long where there are many, and 1 us more where there are few.
 constexpr int kPrepTokens = 4, kPrepHeads = 8;
 struct PrepArgs {
