@@ -295,7 +295,7 @@ struct SeqArgs {
 template <int D>
 struct WaveBias {
   using X = Mma<D>;
-  int at[X::QT];                     // index of key 0's distance in the table, of this lane's first key
+  uint32_t at[X::QT];                // index of key 0's distance in the tables, for this lane's first key (mod 2^32)
   int row[X::QT];                    // the row's table
   float lo[X::QT], hi[X::QT];        // beyond the ends
   int first, last;                   // the first and last place of the wave's rows among the keys
@@ -317,7 +317,7 @@ __device__ __forceinline__ void start_bias(WaveBias<D>& wb, const SeqArgs& a, co
     // rows that do not exist read the places of one that does
     const int place = row.ok ? row.token + off : wb.first;
     wb.row[qt] = head * kBiasPitch;
-    wb.at[qt] = wb.row[qt] + 4 * lg + kBiasPad - a.bias.lo - place;
+    wb.at[qt] = (uint32_t)(wb.row[qt] + 4 * lg + kBiasPad - a.bias.lo) - (uint32_t)place;
   }
 }
 // The bias beyond the ends, from the tables.
@@ -345,7 +345,7 @@ __device__ __forceinline__ void near_bias(const WaveBias<D>& wb, const float* ta
   using X = Mma<D>;
 #pragma unroll
   for (int qt = 0; qt < X::QT; ++qt) {
-    const float* at = table + (wb.at[qt] + key0);
+    const float* at = table + (int)(wb.at[qt] + (uint32_t)key0);
 #pragma unroll
     for (int kt = 0; kt < KT / X::MR; ++kt)
 #pragma unroll
