@@ -88,7 +88,8 @@ struct SeqGeom;
 struct SeqIo;
 struct CacheGeom;
 struct SeqBias;
-hipError_t launch_prompt_attn(const SeqGeom& g, const SeqIo& io, const SeqBias* bias, int d, int P, hipStream_t st);
+hipError_t launch_prompt_attn(const SeqGeom& g, const SeqIo& io, const SeqBias* bias, int d, int rows, int P,
+                              hipStream_t st);
 // Attention over a 4-bit cache: sequences of many query rows, and of few.
 hipError_t launch_cache_tokens(const SeqGeom& g, const SeqIo& io, const CacheGeom& cg, int d, int rows, int P,
                                hipStream_t st);

@@ -235,9 +235,28 @@ la_status check_bias(const la_rel_bias* bias, const int32_t* bucket, const void*
   return LA_OK;
 }
 
-// The units of a call over whole prompts; with a bias those of at most kBiasHeads heads, whose tables are in LDS.
-SeqGeom prompt_geom(const la_seqs& s, const la_rel_bias* bias) {
-  return seq_geom(s, kRows, s.Tk, kRowsExtra, 2 * kRowsExtra, kRowsShare, kRowsWhole, bias ? kBiasHeads : kRows);
+// How a call over whole prompts is made.  With a bias, sequences of up to kBiasKeys keys on average go to the kernel of
+// 128 rows (bias_rows_kernel), whose starts and ends cost less, and longer ones to that of 256: d 64, 16 heads, 20 prompts
+// of 100 tokens 16 against 21 us, 16 of 60 to 512 24.5 against 33, 6 of 1024 60 either way, 4 of 2048 104 against 99; d
+// 128, 8 of 512 32.5 against 34, 4 of 2048 142 against 135, 8192 causal tokens 270 against 248.  A unit has at most
+// kBiasHeads heads then, whose tables are in LDS.
+constexpr int kBiasKeys = 1024, kBiasWhole = 512, kBiasPerCu = 2;
+constexpr uint32_t kBiasExtra = 512, kBiasSnap = 2048, kBiasShare = 256;
+struct PromptPlan {
+  SeqGeom g;
+  int rows, most;          // packed rows of a unit; workgroups (before the device's limit)
+};
+PromptPlan prompt_plan(const la_seqs& s, const la_rel_bias* bias) {
+  PromptPlan p{};
+  if (bias && s.Tk <= (int64_t)kBiasKeys * s.S) {
+    p.g = seq_geom(s, kBiasRows, s.Tk, kBiasExtra, kBiasSnap, kBiasShare, kBiasWhole, kBiasHeads);
+    p.rows = kBiasRows;
+  } else {
+    p.g = seq_geom(s, kRows, s.Tk, kRowsExtra, 2 * kRowsExtra, kRowsShare, kRowsWhole, bias ? kBiasHeads : kRows);
+    p.rows = kRows;
+  }
+  p.most = workgroups(p.g, s.Tk, kMaxWorkgroups * (p.rows == kRows ? 1 : kBiasPerCu));
+  return p;
 }
 
 bool bad_kv4(const la_kv4* kv) {
@@ -321,8 +340,8 @@ size_t la_prompt_ws_bytes(const la_seqs* seqs) { return la_prompt_bias_ws_bytes(
 
 size_t la_prompt_bias_ws_bytes(const la_seqs* seqs, const la_rel_bias* bias) {
   if (check_seqs(seqs) != LA_OK || (bias && bad_bias(bias)) || seqs->S == 0 || seqs->Tq == 0) return 0;
-  const SeqGeom g = prompt_geom(*seqs, bias);
-  return part_layout(g, workgroups(g, seqs->Tk, kMaxWorkgroups), kRows, seqs->d, nullptr).bytes;
+  const PromptPlan p = prompt_plan(*seqs, bias);
+  return part_layout(p.g, p.most, p.rows, seqs->d, nullptr).bytes;
 }
 
 la_status la_prompt_attn(const la_seqs* seqs, const void* q, const void* k, const void* v, const int32_t* cu_q,
@@ -356,18 +375,17 @@ la_status la_prompt_attn_bias(const la_seqs* seqs, const la_rel_bias* bias, cons
     if (st != LA_OK) return st;
     b = SeqBias{bucket, weight, bias->dtype == LA_DTYPE_BF16, bias->buckets, bias->lo, bias->hi};
   }
-  SeqGeom g = prompt_geom(*seqs, bias);
-  g.cu_q = cu_q;
-  g.ks = cu_k;
-  const int most = workgroups(g, seqs->Tk, kMaxWorkgroups);
-  const PartLayout w = part_layout(g, most, kRows, seqs->d, ws);
+  PromptPlan p = prompt_plan(*seqs, bias);
+  p.g.cu_q = cu_q;
+  p.g.ks = cu_k;
+  const PartLayout w = part_layout(p.g, p.most, p.rows, seqs->d, ws);
   if (w.bytes > 0 && (!ws || ws_bytes < w.bytes || ((uintptr_t)ws & 255u))) return LA_ERR_WORKSPACE;
   SeqIo io = seq_io(*seqs, q, o, lse, scale);
   io.k = (const uint16_t*)k;
   io.v = (const uint16_t*)v;
   set_parts(&io, w);
-  const int have = device_workgroups(1);
-  const hipError_t e = launch_prompt_attn(g, io, bias ? &b : nullptr, seqs->d, most < have ? most : have,
+  const int have = device_workgroups(p.rows == kRows ? 1 : kBiasPerCu);
+  const hipError_t e = launch_prompt_attn(p.g, io, bias ? &b : nullptr, seqs->d, p.rows, p.most < have ? p.most : have,
                                           (hipStream_t)stream);
   return e == hipSuccess ? LA_OK : LA_ERR_HIP;
 }

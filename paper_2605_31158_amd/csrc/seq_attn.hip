@@ -240,7 +240,7 @@ __device__ __forceinline__ void start_rows(PieceState<D>& st, WaveCtx& w, const 
 }
 
 // Ends a piece: bf16 rows (and lse) where the piece is the whole unit, else the partial.
-template <int D>
+template <int D, int R = QR>
 __device__ __forceinline__ void end_rows(const PieceState<D>& st, const SeqGeom& g, const SeqIo& io, const Walk& wk,
                                          const Piece& pc, int slot0, int r_off, int c, int lg) {
   using X = Mma<D>;
@@ -265,7 +265,7 @@ __device__ __forceinline__ void end_rows(const PieceState<D>& st, const SeqGeom&
         io.lse[(int64_t)(wk.q.q0 + row.token) * g.Hq + row.head] =
             l == 0.f ? -INFINITY : (st.m_run[qt] + log2f(l)) * 0.69314718055994531f;
     } else {
-      const size_t prow = (size_t)slot * QR + r;
+      const size_t prow = (size_t)slot * R + r;
       float* po = io.part_o + prow * D + 4 * lg;
 #pragma unroll
       for (int dt = 0; dt < D / X::MR; ++dt) {
@@ -331,11 +331,12 @@ __device__ __forceinline__ void far_bias(WaveBias<D>& wb, const float* table, in
 }
 
 // The unit's tables, by all threads.
+template <int THREADS>
 __device__ __forceinline__ void fill_bias(float (*table)[kBiasPitch], const SeqArgs& a, const Walk& wk) {
   const int heads = unit_heads(a.g, wk), head0 = unit_head0(a.g, wk), n = a.bias.hi - a.bias.lo + 1 + 2 * kBiasPad;
   const float inv = 1.0f / a.io.scale_log2;
   for (int h = 0; h < heads; ++h)
-    for (int i = threadIdx.x; i < n; i += kThreads) table[h][i] = bias_log2(a.bias, i - kBiasPad, a.g.Hq, head0 + h) * inv;
+    for (int i = threadIdx.x; i < n; i += THREADS) table[h][i] = bias_log2(a.bias, i - kBiasPad, a.g.Hq, head0 + h) * inv;
 }
 
 // The bias of a tile that needs the table, where the logits are added to.
@@ -437,7 +438,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
             // consecutive units mostly have the same heads; the waves read no table of the piece before any more, as
             // its last iteration ended with a barrier
             const int heads = unit_head0(a.g, wk);
-            if (heads != table_head) fill_bias(table, a, wk);
+            if (heads != table_head) fill_bias<kThreads>(table, a, wk);
             table_head = heads;
             start_bias<D>(wb, a, wk, r_off, c, lg);
           }
@@ -516,6 +517,108 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   };
   if (wave >= 4) run(std::true_type{});
   else run(std::false_type{});
+}
+
+// The same with a bias for units of 128 rows: four waves of 32 rows and two stages of tiles, two workgroups to a CU,
+// which cover each other's starts and ends, and a softmax by the other's products, without taking turns.  For short
+// sequences (prompt_plan): 16 of 60 to 512 tokens, 16 heads, d 64, 20.5 us where units of 256 rows take 28.5, the
+// next token of 8 over 500 to 1000 keys 13 instead of 17.  Long ones are 6 to 9 % faster by the larger units.
+constexpr int kBiasThreads = 256;
+template <int D>
+__global__ __launch_bounds__(kBiasThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void bias_rows_kernel(SeqArgs) {
+  using T = Tile<D>;
+  using X = Mma<D>;
+  __shared__ __attribute__((aligned(1024))) unsigned char ring[4 * T::BYTES];     // K of two stages, V of two
+  __shared__ float table[kBiasHeads][kBiasPitch];
+  const int P = gridDim.x;
+  const int lambda = (blockIdx.x & 7) * (P >> 3) + (blockIdx.x >> 3);
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int lw = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c = lane % X::MR, lg = lane / X::MR;
+  const int r_off = lw * QW;
+  Walk wk;
+  WaveCtx w;
+  RowTiles<D, false> ks;
+  RowTiles<D, true> vs;
+  int bias_lo, bias_hi;
+  {
+    const SeqArgs a = fresh_args();
+    if (a.g.cuts && tid == 0) a.io.cut[2 * lambda] = a.io.cut[2 * lambda + 1] = int4{0, 0, 0, 0};
+    wk = start_walk<false>(a.g, lambda, P);
+    if (!wk.more()) return;
+    w.scale_log2 = a.io.scale_log2;
+    bias_lo = a.bias.lo;
+    bias_hi = a.bias.hi;
+    ks.init(a.io, a.cg, lw, lane);
+    vs.init(a.io, a.cg, lw, lane);
+  }
+  w.kbase = c * T::STRIDE + 16 * (lg ^ T::kswz(c));
+  {
+    const int vrow = 4 * lg + ((lane & 15) >> 2);
+    w.vbase = vrow * T::STRIDE + 2 * X::MR * T::vswz(vrow) + (X::MR == 32 ? 2 * (lane & 16) : 0) + 8 * (lane & 3);
+  }
+  w.g4 = 4 * lg;
+  PieceState<D> st;
+  WaveBias<D> wb;
+  int table_head = -1;
+  while (wk.more()) {
+    uint64_t unit_end;
+    Piece pc;
+    {
+      const SeqArgs a = fresh_args();
+      pc = walk_piece(a.g, wk, &unit_end);
+    }
+    const int N = pc.tb - pc.ta;
+    if (N > 0) {
+      int key_open;
+      phase_barrier();                                 // the piece before is read
+      {
+        const SeqArgs a = fresh_args();
+        ks.prime(a.io, wk, wk.kvh, pc.ta, pc.tb, ring, nullptr);
+        vs.prime(a.io, wk, wk.kvh, pc.ta, pc.tb, ring + 2 * T::BYTES, nullptr);
+        start_rows<D>(st, w, a.g, a.io, wk, r_off, c, lg);
+        const int heads = unit_head0(a.g, wk);
+        if (heads != table_head) fill_bias<kBiasThreads>(table, a, wk);
+        table_head = heads;
+        start_bias<D>(wb, a, wk, r_off, c, lg);
+        const int open = a.g.causal ? max(0, wk.q.lk - wk.q.lq + wk.b * a.g.TB + 1) : wk.q.lk;
+        key_open = min(open, wk.q.lk) - 63;
+      }
+      for (int i = 0; i < N; ++i) {
+        __builtin_amdgcn_s_waitcnt(0);
+        phase_barrier();
+        if (i == 0) far_bias<D>(wb, &table[0][0], bias_hi - bias_lo, w.scale_log2);
+        const unsigned char* kt = ring + (i & 1) * T::BYTES;
+        const unsigned char* vt = kt + 2 * T::BYTES;
+        if (i + 1 < N) {
+          ks.issue(ring + (~i & 1) * T::BYTES);
+          vs.issue(ring + (2 + (~i & 1)) * T::BYTES);
+        }
+        const int key0 = 64 * (pc.ta + i);
+        if (key0 >= st.seen) continue;
+        const bool left = key0 + 63 - wb.first <= bias_lo, right = key0 - wb.last >= bias_hi;
+        if (!left && !right) {
+          near_bias<D>(wb, &table[0][0], st.sacc, key0);
+          qk_tile<D, true>(kt, st.qreg, st.sacc, w.kbase);
+        } else {
+          qk_tile<D>(kt, st.qreg, st.sacc, w.kbase);
+        }
+        float shift[X::QT];
+#pragma unroll
+        for (int qt = 0; qt < X::QT; ++qt) {
+          const float lo = wb.lo[qt], hi = wb.hi[qt];
+          shift[qt] = left ? lo : (right ? hi : 0.f);
+        }
+        if (__builtin_expect(key0 >= key_open, 0)) mask_tile<D>(st.sacc, key0, 0, w);
+        softmax_tile<D, true>(st.sacc, st.pb, st.oacc, st.m_run, st.l_run, w.scale_log2, shift);
+        pv_tile<D>(vt, st.pb, st.oacc, w.vbase);
+      }
+      const SeqArgs a = fresh_args();
+      end_rows<D, kBiasRows>(st, a.g, a.io, wk, pc, 2 * lambda, r_off, c, lg);
+    }
+    const SeqArgs a = fresh_args();
+    walk_on<false>(a.g, wk, unit_end);
+  }
 }
 
 // Joins the pieces of a unit that several stretches share: o = sum 2^(m_s - m) O_s / sum 2^(m_s - m) l_s,
@@ -640,8 +743,18 @@ static hipError_t launch_rows(const SeqGeom& g, const SeqIo& io, const CacheGeom
   return hipGetLastError();
 }
 
-hipError_t launch_prompt_attn(const SeqGeom& g, const SeqIo& io, const SeqBias* bias, int d, int P, hipStream_t st) {
+template <int D>
+static hipError_t launch_bias_rows(const SeqGeom& g, const SeqIo& io, const SeqBias& bias, int P, hipStream_t st) {
+  hipLaunchKernelGGL((bias_rows_kernel<D>), dim3(P), dim3(kBiasThreads), 0, st, SeqArgs{g, io, CacheGeom{}, bias});
+  if (g.cuts) launch_merge<D, kBiasRows>(g, io, P, st);
+  return hipGetLastError();
+}
+
+hipError_t launch_prompt_attn(const SeqGeom& g, const SeqIo& io, const SeqBias* bias, int d, int rows, int P,
+                              hipStream_t st) {
   const CacheGeom none{};
+  if (bias && rows == kBiasRows)
+    return d == 128 ? launch_bias_rows<128>(g, io, *bias, P, st) : launch_bias_rows<64>(g, io, *bias, P, st);
   if (bias)
     return d == 128 ? launch_rows<128, false, true>(g, io, none, P, st, *bias)
                     : launch_rows<64, false, true>(g, io, none, P, st, *bias);

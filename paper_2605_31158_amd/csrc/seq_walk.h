@@ -66,7 +66,7 @@ struct SeqIo {
 constexpr int kBiasPad = 96;
 constexpr int kBiasMost = 513;                              // distances
 constexpr int kBiasPitch = kBiasMost + 2 * kBiasPad;
-constexpr int kBiasHeads = 8;                               // of a unit of la_prompt_attn_bias
+constexpr int kBiasHeads = 4, kBiasRows = 128;              // of a unit of la_prompt_attn_bias
 
 // A learned bias by relative position (la_rel_bias).
 struct SeqBias {

@@ -41,6 +41,13 @@ CASES = [
     ([130], [2100], 6, 2, 64, False, 64, 256, True),
     ([2500], None, 2, 1, 128, True, 32, 128, False),
     ([2100], None, 2, 2, 64, False, 32, 128, True),           # units are cut
+    # more than 1024 keys to a sequence: the kernel of 256 rows at its edges too
+    ([1], [1500], 4, 2, 128, True, 32, 128, False),
+    ([1, 300, 2], [4000, 5, 0], 6, 3, 64, False, 32, 128, True),
+    ([333, 1], [1100, 2000], 14, 2, 128, True, 32, 512, False),
+    ([257, 0, 64], [1281, 3000, 64], 9, 1, 64, True, 16, 60, True),
+    ([1024], None, 2, 1, 64, False, 32, 128, True),           # the last average of the one kernel, and the
+    ([1025], None, 2, 1, 64, False, 32, 128, True),           # first of the other
 ]
 
 
