@@ -19,9 +19,9 @@
 //
 // A relative bias costs where a tile lies within its reach: its accumulators start from the bias instead of 0 (read
 // from LDS, in units of q.k), while the tiles beyond have one number a row, by which the maximum they are formed
-// against is moved.  16 prompts of 60 to 512 tokens, 16 heads, d 64, 28.5 us (without a bias 26.2), 8192 causal tokens as
-// below 225 (221); added behind the product it was 32.6 and 251 (copies of the logits where the two kinds of tiles
-// meet), and two calls of the softmax, one for each kind, spill.
+// against is moved.  16 prompts of 60 to 512 tokens, 16 heads, d 64, take 28.5 us here (without a bias 26.2; short
+// sequences go to bias_rows_kernel), 8192 causal tokens as below 225 (221); added behind the product it was 32.6 and
+// 251 (copies of the logits where the two kinds of tiles meet), and two calls of the softmax, one for each kind, spill.
 //
 // Differences from attn.hip: the tiles of a piece are consecutive, so nothing is read to know the
 // next one (no records); K and V rows have a stride; and the loop ends with the piece, so a piece
