@@ -338,3 +338,79 @@ def test_two_streams():
     for w, runs in zip(want, got):
         for r in runs:
             assert all(torch.equal(x, y) for x, y in zip(w, r))
+
+
+def test_two_graphs_share_scratch():
+    # two captured calls of different sizes and kinds with one scratch, replayed in turn with eager work between
+    ws = torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+    st = torch.cuda.Stream()
+    calls = []
+    for n, (lq, lk, H, K, d, causal, form) in enumerate([([700, 90], [700, 90], 4, 4, 64, False, (32, 128, True)),
+                                                          ([130, 1, 900], [300, 40, 900], 6, 2, 128, True, None)]):
+        q, k, v = make(lq, lk, H, K, d, 110 + n)
+        bias = None if form is None else rel(H, 120 + n, *form)
+        cu_q, cu_k = R.starts(lq), R.starts(lk)
+        o, lse = left(q, k, v, lq, lk, causal, bias=bias)
+        do = grad_of(q, 130 + n)
+        outs = tuple(torch.empty_like(x) for x in (q, k, v)) + (() if bias is None else (torch.empty_like(bias.weight),))
+
+        def call(out=None, ws=None, a=(do, q, k, v, o, lse, cu_q, cu_k), causal=causal, bias=bias):
+            return la.prompt_attn_bwd(*a, causal=causal, bias=bias, ws=ws, out=out)
+
+        st.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(st):
+            call(outs, ws)
+        st.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=st):
+            call(outs, ws)
+        calls.append((graph, call, do, outs))
+    for i in range(6):
+        graph, call, do, outs = calls[i % 2]
+        do.copy_(grad_of(do, 140 + i))
+        ws[::4097].fill_(i)                                   # what the other call left there does not matter
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, y in zip(outs, call()):
+            assert torch.equal(x, y), i
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_everything_at_once(d):
+    # a bias, the gradient of lse, one gradient row for all heads, columns of one buffer, a scale, keys past the queries
+    lq, lk, H, K = [90, 3, 200], [300, 50, 200], 6, 3
+    q, k, v = make(lq, lk, H, K, d, 150, qscale=1.0)
+    bias = rel(H, 151, 32, 200, True, torch.bfloat16)
+    o, lse = left(q, k, v, lq, lk, False, 0.2, bias)
+    do = grad_of(q, 152)[:, :1].expand(sum(lq), H, d)
+    dlse = torch.randn(lse.shape, generator=torch.Generator(device="cuda").manual_seed(8), device="cuda")
+    kv = torch.cat([k, v], 1)
+    grads = torch.empty_like(kv)
+    outs = (torch.empty((H, sum(lq), d), dtype=torch.bfloat16, device="cuda").transpose(0, 1), grads[:, :K], grads[:, K:],
+            torch.empty_like(bias.weight))
+    got = la.prompt_attn_bwd(do, q, kv[:, :K], kv[:, K:], o, lse, R.starts(lq), R.starts(lk), causal=False, scale=0.2,
+                             bias=bias, dlse=dlse, out=outs)
+    G.check(got, G.backward(do, q, k, v, o, lse, lq, lk, False, 0.2, bias, dlse), "everything")
+
+
+def test_refusals():
+    q, k, v = make([40], [40], 4, 2, 64, 160)
+    cu = R.starts([40])
+    o, lse = la.prompt_attn(q, k, v, cu, want_lse=True)
+    b = rel(4, 161)
+    good = dict(do=q, q=q, k=k, v=v, o=o, lse=lse, cu_q=cu)
+    la.prompt_attn_bwd(**good)
+    for bad in (dict(do=q[:39]), dict(do=q.float()), dict(o=o[:, :2]), dict(lse=lse[:, :2]), dict(lse=lse.double()),
+                dict(lse=lse.t().contiguous().t()), dict(dlse=lse[:20]), dict(k=k[:, :, :32]), dict(v=v[:30]), dict(cu_q=cu.long()),
+                dict(do=q[:, :, :1].expand(40, 4, 64)), dict(out=(q, k)), dict(out=(q, k, v[:30])), dict(bias=b, out=(q, k, v)),
+                dict(bias=b, out=(q, k, v, b.weight[:4])), dict(bias=b._replace(weight=b.weight[:, :2])),
+                dict(bias=b._replace(weight=b.weight.half())), dict(bias=b._replace(weight=b.weight.t())),
+                dict(bias=b._replace(bucket=b.bucket.long())), dict(bias=b._replace(bucket=b.bucket.cpu())),
+                dict(bias=b._replace(bucket=torch.zeros(514, dtype=torch.int32, device="cuda"))),
+                dict(bias=b._replace(lo=1 << 21)), dict(ws=torch.empty(16, dtype=torch.uint8))):
+        with pytest.raises((TypeError, ValueError)):
+            la.prompt_attn_bwd(**{**good, **bad})
+    for bad in (dict(ws=torch.empty(256, dtype=torch.uint8, device="cuda")), dict(scale=float("nan")),
+                dict(bias=b._replace(lo=(1 << 20) - 3)), dict(bias=b, scale=1e-30)):
+        with pytest.raises(la.LaError):
+            la.prompt_attn_bwd(**{**good, **bad})
