@@ -139,16 +139,17 @@ int device_workgroups(int per_cu) {
   return (p < 8 ? 8 : (p > kMaxWorkgroups ? kMaxWorkgroups : p)) * per_cu;
 }
 
-// The gradients' units (seq_grad.hip): what starting and ending one costs and the smallest share of a workgroup, in
-// rows of the inner axis; below kGradSnap a share ends at the nearest end of a unit of up to 5/4 shares; and nothing is
-// cut where the inner axis has at most kGradWhole rows.  16 prompts of 60 to 512 tokens (16 heads, d 64) 63 us with an
-// extra of 512, 70 with 256 or 768; five of 100 to 2100 (12 heads over 4) 115 with a snap of 2048, 120 with 4096, 119
-// with none.
+// The gradients' units (seq_grad.hip): what starting and ending one costs (of keys, and of query rows) and the
+// smallest share of a workgroup, in rows of the inner axis; below kGradSnap a share ends at the nearest end of a unit of
+// up to 5/4 shares; and nothing is cut where the inner axis has at most kGradWhole rows.  Chosen over 98 calls, 90 of
+// them drawn: all three at 512 are 3.2 % slower (48 prompts of 1 to 300 tokens, 16 heads over 4, d 64,
+// 39.5 us, with these 36.4), extras of 256 for both 2.2 %, a smallest share of 256 or 144 0.9 %; a snap of 4096 or none costs five prompts of 100 to
+// 2100 (12 heads over 4, a bias) 120 instead of 115.
 // A CU runs one workgroup of dK and dV and one of dQ at a time: 256 of each instead of 512 have half the cuts, and two
 // kinds on a CU cover each other better than two of one kind that start together (the prompts above 73 -> 63 us and
 // 130 -> 121; six of 150 to 3300, 24 heads over 8, d 128, 493 -> 466; a 480P chunk over its context 1806 -> 1765; one
 // of 8192, 16 heads over 4, 818 either way).
-constexpr uint32_t kGradExtra = 512, kGradShare = 512, kGradSnap = 2048;
+constexpr uint32_t kGradKeysExtra = 256, kGradRowsExtra = 512, kGradShare = 192, kGradSnap = 2048;
 constexpr int kGradWhole = 512, kGradPerCu = 1;
 
 GradGeom grad_geom(const la_seqs& s, bool keys, bool bias) {
@@ -166,7 +167,7 @@ GradGeom grad_geom(const la_seqs& s, bool keys, bool bias) {
   g.TB = kGradRows / g.GH;
   g.NH = s.Hkv * g.GS;
   g.causal = s.causal;
-  g.extra = kGradExtra;
+  g.extra = keys ? kGradKeysExtra : kGradRowsExtra;
   g.whole = kGradSnap;
   g.min_share = kGradShare;
   g.cuts = (keys ? (double)s.Tq * g.G : (double)s.Tk) > kGradWhole;
