@@ -80,11 +80,14 @@ SeqGeom seq_geom(const la_seqs& s, int rows, int kcap, uint32_t extra, uint32_t 
   return g;
 }
 
+double most_units(const SeqGeom& g) {
+  return (double)g.Hkv * g.GS * ((double)g.Tq / g.TB + (g.S < g.Tq ? g.S : g.Tq));
+}
+
 // Workgroups worth starting: no more than smallest shares of the most work there can be (sequences of
 // at most kcap keys, kall in all).
 int workgroups(const SeqGeom& g, int64_t kall, int most) {
-  const double units = (double)g.Hkv * g.GS * ((double)g.Tq / g.TB + (g.S < g.Tq ? g.S : g.Tq));
-  const double shares = ceil(units * ((double)kall + g.extra) / g.min_share);
+  const double shares = ceil(most_units(g) * ((double)kall + g.extra) / g.min_share);
   const int want = shares < most ? (int)shares : most;
   return (want + 7) / 8 * 8;
 }
@@ -142,9 +145,9 @@ int device_workgroups(int per_cu) {
 // The gradients' units (seq_grad.hip): what starting and ending one costs (of keys, and of query rows) and the
 // smallest share of a workgroup, in rows of the inner axis; below kGradSnap a share ends at the nearest end of a unit of
 // up to 5/4 shares; and nothing is cut where the inner axis has at most kGradWhole rows.  Chosen over 98 calls, 90 of
-// them drawn: all three at 512 are 3.2 % slower (48 prompts of 1 to 300 tokens, 16 heads over 4, d 64,
-// 39.5 us, with these 36.4), extras of 256 for both 2.2 %, a smallest share of 256 or 144 0.9 %; a snap of 4096 or none costs five prompts of 100 to
-// 2100 (12 heads over 4, a bias) 120 instead of 115.
+// them drawn: all three at 512 are 3.2 % slower (48 prompts of 1 to 300 tokens, 16 heads over 4, d 64, 39.5 us, with
+// these 36.4), extras of 256 for both 2.2 %, a smallest share of 256 or 144 0.9 %; a snap of 4096 or none costs five
+// prompts of 100 to 2100 (12 heads over 4, a bias) 120 instead of 115.
 // A CU runs one workgroup of dK and dV and one of dQ at a time: 256 of each instead of 512 have half the cuts, and two
 // kinds on a CU cover each other better than two of one kind that start together (the prompts above 73 -> 63 us and
 // 130 -> 121; six of 150 to 3300, 24 heads over 8, d 128, 493 -> 466; a 480P chunk over its context 1806 -> 1765; one
@@ -238,10 +241,14 @@ la_status check_bias(const la_rel_bias* bias, const int32_t* bucket, const void*
 
 // How a call over whole prompts is made.  With a bias, sequences of up to kBiasKeys keys on average go to the kernel of
 // 128 rows (bias_rows_kernel), whose starts and ends cost less, and longer ones to that of 256: d 64, 16 heads, 20 prompts
-// of 100 tokens 16 against 21 us, 16 of 60 to 512 24.5 against 33, 6 of 1024 60 either way, 4 of 2048 104 against 99; d
-// 128, 8 of 512 32.5 against 34, 4 of 2048 142 against 135, 8192 causal tokens 270 against 248.  A unit has at most
-// kBiasHeads heads then, whose tables are in LDS.
-constexpr int kBiasKeys = 1024, kBiasWhole = 512, kBiasPerCu = 2;
+// of 100 tokens 11 against 19 us, 16 of 256 15 against 17, 4 of 1024 30 either way, 6 of 1024 54 against 52, 4 of 2048 93
+// against 89; d 128, 8 of 512 27.5 against 32, 4 of 2048 140 against 132, 8192 causal tokens 270 against 230.  A unit has
+// at most kBiasHeads heads then, whose tables are in LDS.
+// Its units are not cut in calls of up to kBiasWhole keys, or kBiasWholeShort where many short sequences are likely
+// to fill the GPU with whole units: a mean of 512 keys and 256 units, or of 256 keys.  That saves the join: 16 prompts of
+// 60 to 512 tokens 26.5 -> 21 us, 20 of 100 13 -> 11, 8 of 512 (d 128) 29.5 -> 27.5; but one of 3900 with 7 of 28 and 4
+// heads would take 71 instead of 41, one of 4000 with 3 of 32 75 instead of 41.
+constexpr int kBiasKeys = 1024, kBiasWhole = 1024, kBiasWholeShort = 4096, kBiasPerCu = 2;
 constexpr uint32_t kBiasExtra = 512, kBiasSnap = 2048, kBiasShare = 256;
 struct PromptPlan {
   SeqGeom g;
@@ -251,6 +258,8 @@ PromptPlan prompt_plan(const la_seqs& s, const la_rel_bias* bias) {
   PromptPlan p{};
   if (bias && s.Tk <= (int64_t)kBiasKeys * s.S) {
     p.g = seq_geom(s, kBiasRows, s.Tk, kBiasExtra, kBiasSnap, kBiasShare, kBiasWhole, kBiasHeads);
+    const double mean = (double)s.Tk / s.S, units = most_units(p.g);
+    if (s.Tk <= kBiasWholeShort && (mean <= 256 || (mean <= 512 && units >= 256))) p.g.cuts = 0;
     p.rows = kBiasRows;
   } else {
     p.g = seq_geom(s, kRows, s.Tk, kRowsExtra, 2 * kRowsExtra, kRowsShare, kRowsWhole, bias ? kBiasHeads : kRows);

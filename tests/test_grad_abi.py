@@ -56,7 +56,7 @@ BAD_BIAS = [dict(lo=1, hi=0), dict(lo=-256, hi=257), dict(lo=-(1 << 20) - 1, hi=
 def test_bias_refused(bad):
     assert fwd(seqs(), rel(**bad)) == la.LA_ERR_SHAPE
     assert bwd(seqs(), grads(), rel(**bad)) == la.LA_ERR_SHAPE
-    assert la.lib().la_prompt_bias_ws_bytes(ref(seqs(Tk=2000)), ref(rel(**bad))) == 0
+    assert la.lib().la_prompt_bias_ws_bytes(ref(seqs(Tk=20000)), ref(rel(**bad))) == 0
     assert la.lib().la_prompt_bwd_ws_bytes(ref(seqs()), ref(rel(**bad))) == 0
 
 
@@ -73,7 +73,7 @@ def test_bias_arguments_refused():
         assert call(rel(dtype=2)) == la.LA_ERR_ARG and call(rel(dtype=-1)) == la.LA_ERR_ARG
     assert bwd(seqs(), grads(), rel(), dw=None) == la.LA_ERR_ARG
     assert bwd(seqs(), grads(), rel(), dw=ctypes.c_void_p(4098)) == la.LA_ERR_ARG
-    s = seqs(Tk=2000)
+    s = seqs(Tk=20000)
     need = la.lib().la_prompt_bias_ws_bytes(ref(s), ref(rel()))
     assert need > 0
     assert fwd(s, rel(), ws=None) == la.LA_ERR_WORKSPACE and fwd(s, rel(), nbytes=need - 1) == la.LA_ERR_WORKSPACE
