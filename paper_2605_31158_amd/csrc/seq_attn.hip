@@ -521,7 +521,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 
 // The same with a bias for units of 128 rows: four waves of 32 rows and two stages of tiles, two workgroups to a CU,
 // which cover each other's starts and ends, and a softmax by the other's products, without taking turns.  For short
-// sequences (prompt_plan): 16 of 60 to 512 tokens, 16 heads, d 64, 20.5 us where units of 256 rows take 28.5, the
+// sequences (prompt_plan): 16 of 60 to 512 tokens, 16 heads, d 64, 21 us where units of 256 rows take 28.5, the
 // next token of 8 over 500 to 1000 keys 13 instead of 17.  Long ones are 6 to 9 % faster by the larger units.
 constexpr int kBiasThreads = 256;
 template <int D>

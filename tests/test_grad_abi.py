@@ -61,6 +61,16 @@ def test_bias_refused(bad):
 
 
 @cpu_only
+def test_bias_scratch():
+    # none where no unit is cut: few keys, or up to 4096 in short sequences that fill the GPU with whole units
+    need = lambda **kw: la.lib().la_prompt_bias_ws_bytes(ref(seqs(**kw)), ref(rel()))   # noqa: E731
+    assert need(S=1, Tq=1024, Tk=1024) == 0 < need(S=1, Tq=1025, Tk=1025)
+    assert need(S=16, Tq=100, Tk=4096) == 0 < need(S=16, Tq=100, Tk=4097)
+    assert need(S=8, Tq=4096, Tk=4096, Hq=16, Hkv=16) == 0 < need(S=8, Tq=4096, Tk=4096, Hq=2, Hkv=2)
+    assert need(S=7, Tq=4096, Tk=4096, Hq=16, Hkv=16) > 0
+
+
+@cpu_only
 def test_bias_arguments_refused():
     for dtype, word in ((0, 2), (1, 1)):
         for call in (lambda **kw: fwd(seqs(), rel(dtype=dtype), **kw), lambda **kw: bwd(seqs(), grads(), rel(dtype=dtype), **kw)):

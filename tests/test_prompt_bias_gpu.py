@@ -48,6 +48,12 @@ CASES = [
     ([257, 0, 64], [1281, 3000, 64], 9, 1, 64, True, 16, 60, True),
     ([1024], None, 2, 1, 64, False, 32, 128, True),           # the last average of the one kernel, and the
     ([1025], None, 2, 1, 64, False, 32, 128, True),           # first of the other
+    # several short sequences: whole units up to 4096 keys where those are many or short, cut ones else
+    ([64] * 40, None, 2, 1, 64, False, 32, 128, True),
+    ([1900] + [28] * 7, None, 16, 16, 64, False, 32, 128, True),
+    ([1900] + [28] * 7, None, 2, 1, 64, True, 32, 128, False),
+    ([512] * 8, None, 16, 16, 128, True, 32, 128, False),
+    ([512] * 7 + [513], None, 16, 4, 128, False, 32, 128, True),
 ]
 
 
