@@ -951,6 +951,7 @@ struct DistArgs {
   int pitch, Hq, P, empty;
   int groups;              // workgroups of a head
 };
+constexpr int kDistChunks = (kBiasMost + 2 * kBiasPad + 63) / 64;
 __device__ __forceinline__ void dist_merge(const DistArgs& a, int h, int first, int step) {
   __shared__ double part[4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -959,10 +960,17 @@ __device__ __forceinline__ void dist_merge(const DistArgs& a, int h, int first, 
   const int l1 = head == 0 ? l0 - 1 : min((int)((head * ((uint32_t)h + 1ull) - 1) / share), a.P - 1);
   for (int64_t b = first; b < a.bias.buckets; b += step) {
     double x = 0.0;
-    for (int i = lane; i < a.pitch; i += 64) {
-      if (a.bias.bucket[min(max(i - kBiasPad, 0), a.bias.hi - a.bias.lo)] != b) continue;
+    uint32_t mine = 0;       // bit c: distance lane + 64 c is of the bucket (all loads at once, not one behind the other)
+#pragma unroll
+    for (int c = 0; c < kDistChunks; ++c) {
+      const int i = lane + 64 * c;
+      const bool hit = a.bias.bucket[min(max(i - kBiasPad, 0), a.bias.hi - a.bias.lo)] == b;
+      mine |= hit && i < a.pitch ? 1u << c : 0;
+    }
+    for (; mine; mine &= mine - 1) {
+      const float* at = a.dist + (size_t)h * a.pitch + lane + 64 * __builtin_ctz(mine);
 #pragma unroll 16
-      for (int l = l0 + wave; l <= l1; l += 4) x += a.dist[(size_t)(l + h) * a.pitch + i];
+      for (int l = l0 + wave; l <= l1; l += 4) x += at[(size_t)l * a.pitch];
     }
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
