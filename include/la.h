@@ -388,8 +388,9 @@ la_status la_prompt_attn(const la_seqs* seqs, const void* q, const void* k, cons
  *   bias[h] = weight[bucket[clamp(distance, lo, hi) - lo]][h].
  * What the buckets are is the caller's: one for every distance, or ever wider ones.  A bucket outside
  * [0, buckets) has no bias (and takes no gradient).  A weight of -inf hides its distances; finite weights beyond
- * +-2^24 (a type's lowest value as a mask) count as +-2^24; +inf and NaN are not supported.  A positive scale below
- * 2^-60 is LA_ERR_ARG with a bias. */
+ * +-2^14 (-1e9 or a type's lowest value as a mask) count as +-2^14, which hides where other logits are within 16000 of
+ * those hidden, and where a row sees nothing else leaves it the softmax of its q.k; +inf and NaN are not supported.  A
+ * positive scale below 2^-60 is LA_ERR_ARG with a bias. */
 typedef struct la_rel_bias {
   int32_t lo, hi;            /* lo <= hi <= lo + 512, both within +-2^20 */
   int32_t buckets;           /* rows of the weights: 1 to 2^20 */
@@ -408,8 +409,9 @@ la_status la_prompt_attn_bias(const la_seqs* seqs, const la_rel_bias* bias, cons
  * delta = do.o - dlse and dS = P (do.v - delta) over the pairs that see each other,
  *   dq = scale dS k,   dk = scale dS^T q,   dv = P^T do   (dk and dv summed over the query heads of a key head),
  *   dweight[b][h] = the sum of dS over the pairs of bucket b and head h, over all sequences.
- * The probabilities are recomputed from q, k and lse; they and dS are rounded to bf16 for their products, sums
- * are fp32 (dweight's 64 bits between workgroups) and in a fixed order: results repeat bit for bit on one device. */
+ * The probabilities are recomputed from q, k and lse, whose rounding moves a row's by up to 0.2 % where |lse| is 2^14 (in
+ * proportion elsewhere); they and dS are rounded to bf16 for their products, sums are fp32 (dweight's 64 bits between
+ * workgroups) and in a fixed order: results repeat bit for bit on one device. */
 typedef struct la_prompt_grads {
   int64_t do_token, do_head;   /* strides in elements, as in la_seqs: those of do may be a broadcast's (head 0) */
   int64_t dq_token, dq_head;

@@ -67,6 +67,7 @@ constexpr int kBiasPad = 96;
 constexpr int kBiasMost = 513;                              // distances
 constexpr int kBiasPitch = kBiasMost + 2 * kBiasPad;
 constexpr int kBiasHeads = 4, kBiasRows = 128;              // of a unit of la_prompt_attn_bias
+constexpr float kBiasWeight = 16384.f;                      // the largest finite weight
 
 // A learned bias by relative position (la_rel_bias).
 struct SeqBias {
@@ -77,14 +78,17 @@ struct SeqBias {
 
 namespace {
 
-// The bias of bucket bucket[i] and head h in base 2.  Finite weights are held to 2^24, far beyond what a weight of zero
-// takes: of larger ones (a type's lowest value as a mask) a logit's rounding would be worth whole factors of 2^128.
+// The bias of bucket bucket[i] and head h in base 2.  Finite weights are held to 2^14 (a type's lowest value as a mask, or
+// -1e9): a row that sees nothing but such keys has all of it in its logits and in its lse, and must still tell the logits
+// apart and get its probabilities back from the lse, of which the gradients have one float.  Next to 2^14 that float's
+// half step is worth 0.1 % of a probability, the logits' the same; next to 2^24 both are worth whole factors (row sums of
+// P from 0.25 to 4).  As a mask 2^14 is enough for logits that lie up to 16000 apart.
 __device__ __forceinline__ float bias_log2(const SeqBias& b, int i, int Hq, int h) {
   const int n = b.bucket[min(max(i, 0), b.hi - b.lo)];
   if (n < 0 || n >= b.buckets) return 0.f;
   const size_t at = (size_t)n * Hq + h;
   float w = b.bf16 ? __uint_as_float((uint32_t)((const uint16_t*)b.weight)[at] << 16) : ((const float*)b.weight)[at];
-  if (fabsf(w) > 16777216.f && w != -INFINITY) w = copysignf(16777216.f, w);
+  if (fabsf(w) > kBiasWeight && w != -INFINITY) w = copysignf(kBiasWeight, w);
   return w * 1.4426950408889634f;
 }
 
