@@ -429,8 +429,8 @@ size_t la_prompt_bwd_ws_bytes(const la_seqs* seqs, const la_rel_bias* bias);
  *   dq [Tq, Hq, d], dk, dv [Tk, Hkv, d]  bf16, not overlapping each other or an input.  Rows that no sequence
  *           covers are not written; keys that no query sees get zeros.
  *   dweight [buckets, Hq] in the weights' type, with a bias: written whole.
- * A query that sees no key (lse = -inf) has no gradients and gives none.  Kernel launches only: a caller may
- * capture the call; calls that may overlap need a ws each. */
+ * A query that sees no key (lse = -inf) has no gradients and gives none, whatever its rows of do and dlse hold (NaN, say).
+ * Kernel launches only: a caller may capture the call; calls that may overlap need a ws each. */
 la_status la_prompt_attn_bwd(const la_seqs* seqs, const la_prompt_grads* grads, const la_rel_bias* bias,
                              const void* dout, const void* q, const void* k, const void* v, const void* o,
                              const float* lse, const float* dlse, const int32_t* cu_q, const int32_t* cu_k,

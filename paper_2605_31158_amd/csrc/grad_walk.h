@@ -42,7 +42,7 @@ struct GradIo {
   float* part;             // [2 P][arrays][128][d]: sums of the piece that a stretch starts in (0) or ends in (1)
   int4* cut;               // [2 P]: the unit whose piece a slot holds, or w = 0
   float scale, scale_log2;
-  const float* table;      // [Hq][bias_pitch]: the bias times log2 e by distance - (bias_lo - kBiasPad)
+  const float* table;      // [Hq][bias_pitch]: the bias times log2 e by distance - (bias_lo - kBiasPad); first, whether any is -inf
   int bias_lo, bias_hi, bias_pitch;
   float* dist;             // [P + NH][bias_pitch]: the sums of dS of workgroup l and head h by distance, in l + h
   uint64_t* line;          // a head's weight, and a share

@@ -249,6 +249,7 @@ __device__ __forceinline__ GradArgs grad_args() {
 struct FarBias {
   int lo, hi;              // the first and last distance of the table
   float at_lo, at_hi;      // the bias there and beyond
+  bool hides;              // some distance's bias is -inf
 };
 struct TileBias {
   bool near;
@@ -257,6 +258,7 @@ struct TileBias {
 __device__ __forceinline__ void far_bias(FarBias& b, const float* table) {
   b.at_lo = table[kBiasPad];
   b.at_hi = table[kBiasPad + b.hi - b.lo];
+  b.hides = __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, table[0])) != 0;
 }
 __device__ __forceinline__ TileBias tile_bias(const FarBias& b, int least, int most) {
   if (most <= b.lo) return TileBias{false, b.at_lo};
@@ -302,7 +304,7 @@ __device__ __forceinline__ void key_grad(unsigned char* lds, int block, int P) {
   float scale_log2;
   uint32_t q_stride, do_stride;
   uint32_t q_off[T::PER], do_off[T::PER];
-  FarBias far{0, 0, 0.f, 0.f};
+  FarBias far{0, 0, 0.f, 0.f, false};
   {
     const GradArgs a = grad_args<true>();
     if (a.g.cuts && tid == 0) a.io.cut[2 * l] = a.io.cut[2 * l + 1] = int4{0, 0, 0, 0};
@@ -452,8 +454,18 @@ __device__ __forceinline__ void key_grad(unsigned char* lds, int block, int P) {
         tile = next_tile;
         if (left > 1) issue(st ^ 1);
         if (row0 + (QT - 1) < from) continue;
-        const unsigned char* qt = ring + st * (2 * T::BYTES);
-        const unsigned char* dt = qt + T::BYTES;
+        unsigned char* const qt = ring + st * (2 * T::BYTES);
+        unsigned char* const dt = qt + T::BYTES;
+        // Rows that see nothing take no part, whatever q and do hold there: 0 times NaN would.  They come from the mask or
+        // from weights of -inf.  (Every wave clears them before it reads, all of them to the same zeros.)
+        if (!ROTATE && __builtin_expect(far.hides || row0 + off < 0, 0)) {
+          const float lse = *(const float*)(stat + st * kStatBytes + 8 * (lane & (QT - 1)));
+          for (uint64_t none = __ballot(lse == INFINITY && lane < QT); none; none &= none - 1) {
+            const int at = __builtin_ctzll(none) * T::STRIDE + 16 * lane;
+            if (lane < T::SLOTS) *(u32x4*)(qt + at) = *(u32x4*)(dt + at) = u32x4{0u, 0u, 0u, 0u};
+          }
+          lds_order();
+        }
         typename X::Acc s[NT][X::QT], dp[NT][X::QT];
         float to_log2 = scale_log2, shift = 0.f;
         rows_product<D, NT>(qt, kreg, s, rbase);
@@ -656,7 +668,7 @@ __device__ __forceinline__ void row_grad(unsigned char* lds, int group, int P) {
   const int lw = __builtin_amdgcn_readfirstlane(tid >> 6);
   GradWalk wk;
   float scale_log2;
-  FarBias far{0, 0, 0.f, 0.f};
+  FarBias far{0, 0, 0.f, 0.f, false};
   int sum_head = 0, last_head = 0;       // the heads whose sums this workgroup writes
   float far_lo = 0.f, far_hi = 0.f;      // the lane's sums of dS beyond the table's ends
   uint32_t k_stride, v_stride;
@@ -806,6 +818,11 @@ __device__ __forceinline__ void row_grad(unsigned char* lds, int group, int P) {
           if (ok) z = a.io.stat[(uint64_t)head * (uint32_t)a.g.Tq + (uint64_t)tok];
           lse[qc] = z.x;
           delta[qc] = z.y;
+          // as in key_grad: rows that see nothing
+          if (!ROTATE && z.x == INFINITY) {
+#pragma unroll
+            for (int ks = 0; ks < D / X::KC; ++ks) qreg[ks][qc] = doreg[ks][qc] = bf16x8{};
+          }
           limit[qc] = ok ? (a.g.causal ? max(0, min(lk, off + token + 1)) : lk) : 0x7fffffff;
           wave_keys = max(wave_keys, ok ? limit[qc] : 0);
           wave_open = min(wave_open, limit[qc]);
@@ -1074,8 +1091,15 @@ __global__ __launch_bounds__(256) void grad_prep_kernel(PrepArgs a) {
   const int tid = threadIdx.x;
   if ((int)blockIdx.x < a.tables) {
     const int h = blockIdx.x;
-    for (int i = tid; i < a.pitch; i += 256)
-      a.table[(size_t)h * a.pitch + i] = bias_log2(a.bias, i - kBiasPad, a.Hq, h);
+    float* const table = a.table + (size_t)h * a.pitch;
+    bool hides = false;
+    for (int i = tid; i < a.pitch; i += 256) {
+      const float x = bias_log2(a.bias, i - kBiasPad, a.Hq, h);
+      hides |= x == -INFINITY;
+      if (i > 0) table[i] = x;
+    }
+    const int any = __syncthreads_or(hides);
+    if (tid == 0) table[0] = any ? 1.0f : 0.f;         // no tile reads the first three
     return;
   }
   constexpr int LPR = D / 8;             // lanes of a row
