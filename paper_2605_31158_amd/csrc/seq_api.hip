@@ -244,11 +244,17 @@ la_status check_bias(const la_rel_bias* bias, const int32_t* bucket, const void*
 // of 100 tokens 11 against 19 us, 16 of 256 15 against 17, 4 of 1024 30 either way, 6 of 1024 54 against 52, 4 of 2048 93
 // against 89; d 128, 8 of 512 27.5 against 32, 4 of 2048 140 against 132, 8192 causal tokens 270 against 230.  A unit has
 // at most kBiasHeads heads then, whose tables are in LDS.
-// Its units are not cut in calls of up to kBiasWhole keys, or kBiasWholeShort where many short sequences are likely
-// to fill the GPU with whole units: a mean of 512 keys and 256 units, or of 256 keys.  That saves the join: 16 prompts of
-// 60 to 512 tokens 26.5 -> 21 us, 20 of 100 13 -> 11, 8 of 512 (d 128) 29.5 -> 27.5; but one of 3900 with 7 of 28 and 4
-// heads would take 71 instead of 41, one of 4000 with 3 of 32 75 instead of 41.
-constexpr int kBiasKeys = 1024, kBiasWhole = 1024, kBiasWholeShort = 4096, kBiasPerCu = 2;
+// Its units are not cut in calls of up to kBiasWhole keys, which saves the join.  Up to kBiasWholeShort keys it goes by
+// how uneven the work can be, as the lengths are on the GPU: one sequence may have nearly all keys, and its units walk 60
+// tiles, 50 to 70 us.  With a mean of up to 256 keys, units are whole up to kBiasWholeMost keys (20 prompts of 100 tokens, 4
+// heads, 14.4 -> 9.7 us; one of 1900 with 7 of 28, 4 heads, would take 31 instead of 26).  Beyond, where there is a run of
+// queries for every 16 keys, as 8 heads have: then the long sequence has many units too (16 prompts of 60 to 512 tokens, 16
+// heads, 25 -> 21 us, 8 heads 22 -> 17; one of 3800 among 15 of 10 60 to 90 -> 69 to 79, with 8 heads 44 to 58 -> 71).  With
+// fewer they are cut: that one with 4 heads takes 31 to 38 us instead of 52 to 72, 16 single tokens, of which one has 3900
+// keys, 17 instead of 50, for 2 to 4 us more in even batches (16 over 250 keys 10.6 -> 13).  A mean of up to 512 keys asks
+// for 256 units too (8 of 512, 8 heads, d 128, 33 -> 25).  Calls of more keys are cut: whole units would save 1.5 to 4 us in
+// even batches (32 prompts of 60 to 512 tokens 34 -> 32, 64 60 -> 56).
+constexpr int kBiasKeys = 1024, kBiasWhole = 1024, kBiasWholeMost = 2048, kBiasWholeShort = 4096, kBiasPerCu = 2;
 constexpr uint32_t kBiasExtra = 512, kBiasSnap = 2048, kBiasShare = 256;
 struct PromptPlan {
   SeqGeom g;
@@ -258,8 +264,10 @@ PromptPlan prompt_plan(const la_seqs& s, const la_rel_bias* bias) {
   PromptPlan p{};
   if (bias && s.Tk <= (int64_t)kBiasKeys * s.S) {
     p.g = seq_geom(s, kBiasRows, s.Tk, kBiasExtra, kBiasSnap, kBiasShare, kBiasWhole, kBiasHeads);
-    const double mean = (double)s.Tk / s.S, units = most_units(p.g);
-    if (s.Tk <= kBiasWholeShort && (mean <= 256 || (mean <= 512 && units >= 256))) p.g.cuts = 0;
+    const double mean = (double)s.Tk / s.S, runs = (double)p.g.Hkv * p.g.GS * p.g.Tq / p.g.TB;
+    const bool fill = s.Tk <= kBiasWholeShort && 16 * runs >= s.Tk;
+    if ((s.Tk <= kBiasWholeMost && mean <= 256) || (fill && (mean <= 256 || (mean <= 512 && most_units(p.g) >= 256))))
+      p.g.cuts = 0;
     p.rows = kBiasRows;
   } else {
     p.g = seq_geom(s, kRows, s.Tk, kRowsExtra, 2 * kRowsExtra, kRowsShare, kRowsWhole, bias ? kBiasHeads : kRows);
