@@ -251,9 +251,11 @@ la_status check_bias(const la_rel_bias* bias, const int32_t* bucket, const void*
 // queries for every 16 keys, as 8 heads have: then the long sequence has many units too (16 prompts of 60 to 512 tokens, 16
 // heads, 25 -> 21 us, 8 heads 22 -> 17; one of 3800 among 15 of 10 60 to 90 -> 69 to 79, with 8 heads 44 to 58 -> 71).  With
 // fewer they are cut: that one with 4 heads takes 31 to 38 us instead of 52 to 72, 16 single tokens, of which one has 3900
-// keys, 17 instead of 50, for 2 to 4 us more in even batches (16 over 250 keys 10.6 -> 13).  A mean of up to 512 keys asks
-// for 256 units too (8 of 512, 8 heads, d 128, 33 -> 25).  Calls of more keys are cut: whole units would save 1.5 to 4 us in
-// even batches (32 prompts of 60 to 512 tokens 34 -> 32, 64 60 -> 56).
+// keys, 17 instead of 50, for 2 to 4 us more in even batches (16 over 250 keys 10.6 -> 13).  Continuations of a few queries
+// (more than one a sequence, fewer than a sixteenth of the keys) are whole: 6 a sequence over 256 keys, 8 heads over 2, d 128,
+// take 13.7 us instead of 15.8, but 71 instead of 22 where one sequence has nearly all keys.  A mean of up to 512 keys asks for 256 units too (8 of 512, 8 heads, d 128, 33 -> 25).
+// Calls of more keys are cut: whole units would save 1.5 to 4 us in even batches (32 prompts of 60 to 512 tokens 34 -> 32,
+// 64 60 -> 56).
 constexpr int kBiasKeys = 1024, kBiasWhole = 1024, kBiasWholeMost = 2048, kBiasWholeShort = 4096, kBiasPerCu = 2;
 constexpr uint32_t kBiasExtra = 512, kBiasSnap = 2048, kBiasShare = 256;
 struct PromptPlan {
@@ -265,9 +267,9 @@ PromptPlan prompt_plan(const la_seqs& s, const la_rel_bias* bias) {
   if (bias && s.Tk <= (int64_t)kBiasKeys * s.S) {
     p.g = seq_geom(s, kBiasRows, s.Tk, kBiasExtra, kBiasSnap, kBiasShare, kBiasWhole, kBiasHeads);
     const double mean = (double)s.Tk / s.S, runs = (double)p.g.Hkv * p.g.GS * p.g.Tq / p.g.TB;
-    const bool fill = s.Tk <= kBiasWholeShort && 16 * runs >= s.Tk;
-    if ((s.Tk <= kBiasWholeMost && mean <= 256) || (fill && (mean <= 256 || (mean <= 512 && most_units(p.g) >= 256))))
-      p.g.cuts = 0;
+    const bool fill = 16 * runs >= s.Tk, few = s.Tq > s.S && 16 * (int64_t)s.Tq < s.Tk;
+    const bool whole = mean <= 256 ? s.Tk <= kBiasWholeMost || fill || few : mean <= 512 && fill && most_units(p.g) >= 256;
+    if (s.Tk <= kBiasWholeShort && whole) p.g.cuts = 0;
     p.rows = kBiasRows;
   } else {
     p.g = seq_geom(s, kRows, s.Tk, kRowsExtra, 2 * kRowsExtra, kRowsShare, kRowsWhole, bias ? kBiasHeads : kRows);
