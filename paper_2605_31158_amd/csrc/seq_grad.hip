@@ -24,6 +24,7 @@
 // 1.03 PFLOP/s.  Short sequences: a unit costs 3.5 us beside its tiles (Q, dO or K, V, the first tile, the results), a
 // tile of 64 by 128 pairs 2.1 us where two walks share a CU, and the start (finding the stretch) 2.5: 48 prompts of 1
 // to 300 tokens, 16 heads over 4, d 64, 26 us.
+#include <limits.h>
 #include <math.h>
 
 #include <type_traits>
@@ -957,9 +958,11 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
 }
 
 // ------------------------------------------------------------------------------------------------
-// The gradient of the bias' weights: a workgroup adds the sums by distance of one bucket (and of every `step`-th from
-// there) of a head, over the workgroups of dQ that met the head and the distances of the bucket (what lies beyond the
-// ends belongs to them), in 64 bits and a fixed order.  A wave has every fourth workgroup, a lane every 64th distance.
+// The gradient of the bias' weights: a workgroup adds the sums by distance of one bucket of a head, over the workgroups
+// of dQ that met the head and the distances of the bucket (what lies beyond the ends belongs to them), in 64 bits and a
+// fixed order.  A wave has every fourth workgroup, a lane every 64th distance.  Of more than kDistGroups buckets it has
+// every `step`-th that some distance names, at most 513 in all; the others were set to 0 by the call's first launch (two
+// prompts of 300 and 77 tokens, 16 heads, 2^20 buckets: 13.3 ms with each bucket's distances looked for, so 0.074).
 struct DistArgs {
   const float* dist;
   const uint64_t* line;
@@ -969,13 +972,32 @@ struct DistArgs {
   int groups;              // workgroups of a head
 };
 constexpr int kDistChunks = (kBiasMost + 2 * kBiasPad + 63) / 64;
+constexpr int kDistGroups = 64;
 __device__ __forceinline__ void dist_merge(const DistArgs& a, int h, int first, int step) {
   __shared__ double part[4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const uint64_t head = a.empty ? 0 : a.line[0], share = a.empty ? 1 : a.line[1];
   const int l0 = (int)(head * (uint32_t)h / share);
   const int l1 = head == 0 ? l0 - 1 : min((int)((head * ((uint32_t)h + 1ull) - 1) / share), a.P - 1);
-  for (int64_t b = first; b < a.bias.buckets; b += step) {
+  int name[kDistChunks];     // the buckets of the workgroup among the lane's distances
+  if (a.bias.buckets > step) {
+#pragma unroll
+    for (int c = 0; c < kDistChunks; ++c) {
+      const int b = a.bias.bucket[min(max(lane + 64 * c - kBiasPad, 0), a.bias.hi - a.bias.lo)];
+      name[c] = b >= 0 && b < a.bias.buckets && b % step == first ? b : INT_MAX;
+    }
+  }
+  // the one behind b
+  auto next = [&](int b) {
+    if (a.bias.buckets <= step) return INT_MAX;
+    int x = INT_MAX;
+#pragma unroll
+    for (int c = 0; c < kDistChunks; ++c) x = min(x, name[c] > b ? name[c] : INT_MAX);
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) x = min(x, __shfl_xor(x, m));
+    return __builtin_amdgcn_readfirstlane(x);
+  };
+  for (int b = a.bias.buckets <= step ? first : next(-1); b < a.bias.buckets; b = next(b)) {
     double x = 0.0;
     uint32_t mine = 0;       // bit c: distance lane + 64 c is of the bucket (all loads at once, not one behind the other)
 #pragma unroll
@@ -1069,7 +1091,8 @@ __global__ __launch_bounds__(256) void grad_merge_kernel(GradIo keys, GradIo row
 }
 
 // ------------------------------------------------------------------------------------------------
-// What both walks need of a row: lse in base 2, and delta; and the bias by distance.  Bound by reading o and do: 67 MB
+// What both walks need of a row: lse in base 2, and delta; and the bias by distance, and zeros for its gradient where not
+// every bucket is written later.  Bound by reading o and do: 67 MB
 // (8192 tokens, 16 heads, d 128) in 12.2 us, 5.5 TB/s.
 // More tokens take as long where there are many, and 1 us more where there are few.
 constexpr int kPrepTokens = 4, kPrepHeads = 8;
@@ -1079,7 +1102,10 @@ struct PrepArgs {
   int64_t o_tok, o_head, do_tok, do_head;
   float2* stat;
   int Tq, Hq;
-  int tables;                            // workgroups that lay out the bias of a head each, in front
+  int clears;                            // workgroups that clear the weights' gradient, in front
+  int64_t zeros;                         // its values
+  void* dweight;
+  int tables;                            // workgroups that lay out the bias of a head each, behind them
   int64_t groups;                        // of kPrepTokens tokens by kPrepHeads heads
   SeqBias bias;
   int pitch;
@@ -1089,8 +1115,16 @@ struct PrepArgs {
 template <int D>
 __global__ __launch_bounds__(256) void grad_prep_kernel(PrepArgs a) {
   const int tid = threadIdx.x;
-  if ((int)blockIdx.x < a.tables) {
-    const int h = blockIdx.x;
+  if ((int)blockIdx.x < a.clears) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + tid; i < a.zeros; i += (int64_t)a.clears * 256) {
+      if (a.bias.bf16) ((uint16_t*)a.dweight)[i] = 0;
+      else ((float*)a.dweight)[i] = 0.f;
+    }
+    return;
+  }
+  const int block = blockIdx.x - a.clears, blocks = gridDim.x - a.clears;
+  if (block < a.tables) {
+    const int h = block;
     float* const table = a.table + (size_t)h * a.pitch;
     bool hides = false;
     for (int i = tid; i < a.pitch; i += 256) {
@@ -1107,7 +1141,7 @@ __global__ __launch_bounds__(256) void grad_prep_kernel(PrepArgs a) {
   constexpr int ROWS = kPrepHeads * kPrepTokens;
   __shared__ float dots[ROWS];
   const int HB = (a.Hq + kPrepHeads - 1) / kPrepHeads;
-  for (int64_t g = blockIdx.x - a.tables; g < a.groups; g += gridDim.x - a.tables) {
+  for (int64_t g = block - a.tables; g < a.groups; g += blocks - a.tables) {
     const int64_t t0 = g / HB * kPrepTokens;
     const int h0 = (int)(g % HB) * kPrepHeads;
 #pragma unroll
@@ -1148,14 +1182,17 @@ __global__ __launch_bounds__(256) void grad_prep_kernel(PrepArgs a) {
 
 template <int D>
 static hipError_t launch_grad(const GradCall& c, hipStream_t st) {
-  if (c.rows) {
-    const int64_t groups = ((int64_t)c.Tq + kPrepTokens - 1) / kPrepTokens * ceil_div(c.rows_g.Hq, kPrepHeads);
-    const int tables = c.has_bias ? c.rows_g.Hq : 0;
+  const int64_t zeros = c.has_bias && c.bias.buckets > kDistGroups ? (int64_t)c.bias.buckets * c.rows_g.Hq : 0;
+  if (c.rows || zeros > 0) {
+    const int64_t groups =
+        c.rows ? ((int64_t)c.Tq + kPrepTokens - 1) / kPrepTokens * ceil_div(c.rows_g.Hq, kPrepHeads) : 0;
+    const int tables = c.rows && c.has_bias ? c.rows_g.Hq : 0;
+    const int clears = (int)(zeros < 1024 * 1024 ? (zeros + 1023) / 1024 : 1024);
     const PrepArgs p{c.o, c.rows_io.dout, c.lse, c.dlse, c.o_tok, c.o_head, c.rows_io.do_tok, c.rows_io.do_head,
-                     const_cast<float2*>(c.rows_io.stat), c.Tq, c.rows_g.Hq, tables, groups, c.bias, c.rows_io.bias_pitch,
-                     const_cast<float*>(c.rows_io.table)};
+                     const_cast<float2*>(c.rows_io.stat), c.Tq, c.rows_g.Hq, clears, zeros, c.dweight, tables, groups, c.bias,
+                     c.rows_io.bias_pitch, const_cast<float*>(c.rows_io.table)};
     const int most = 1 << 20;
-    hipLaunchKernelGGL((grad_prep_kernel<D>), dim3(tables + (groups < most ? (int)groups : most)), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((grad_prep_kernel<D>), dim3(clears + tables + (groups < most ? (int)groups : most)), dim3(256), 0, st, p);
   }
   const int keys_p = c.keys ? c.keys_p : 0, rows_p = c.rows ? c.rows_p : 0;
   if (keys_p + rows_p > 0) {
@@ -1168,7 +1205,7 @@ static hipError_t launch_grad(const GradCall& c, hipStream_t st) {
     else hipLaunchKernelGGL((grad_kernel<D, false, true>), grid, block, 0, st, a);
   }
   const int keys_cut = c.keys_g.cuts ? keys_p : 0, rows_cut = c.rows_g.cuts ? rows_p : 0;
-  const int groups = c.bias.buckets < 64 ? c.bias.buckets : 64;
+  const int groups = c.bias.buckets < kDistGroups ? c.bias.buckets : kDistGroups;
   const DistArgs d{c.rows_io.dist, c.rows_io.line, c.bias, c.dweight, c.rows_io.bias_pitch, c.has_bias ? c.rows_g.Hq : 0,
                    c.rows_p, !c.rows, groups};
   const int blocks = 16 * keys_cut + 8 * rows_cut + d.Hq * d.groups;
