@@ -960,9 +960,10 @@ __global__ __launch_bounds__(kGradThreads) __attribute__((amdgpu_waves_per_eu(2,
 // ------------------------------------------------------------------------------------------------
 // The gradient of the bias' weights: a workgroup adds the sums by distance of one bucket of a head, over the workgroups
 // of dQ that met the head and the distances of the bucket (what lies beyond the ends belongs to them), in 64 bits and a
-// fixed order.  A wave has every fourth workgroup, a lane every 64th distance.  Of more than kDistGroups buckets it has
-// every `step`-th that some distance names, at most 513 in all; the others were set to 0 by the call's first launch (two
-// prompts of 300 and 77 tokens, 16 heads, 2^20 buckets: 13.3 ms with each bucket's distances looked for, so 0.074).
+// fixed order, and then every `step`-th bucket from there.  A wave has every fourth workgroup, a lane every 64th distance.
+// Where there are more buckets than distances it goes through those that some distance names; the others were set to 0 by
+// the call's first launch (two prompts of 300 and 77 tokens, 16 heads, 2^20 buckets: 13.3 ms with each bucket's distances
+// looked for, so 0.074; 4096 buckets 97 -> 61 us, but 513 49 -> 55).
 struct DistArgs {
   const float* dist;
   const uint64_t* line;
@@ -973,6 +974,7 @@ struct DistArgs {
 };
 constexpr int kDistChunks = (kBiasMost + 2 * kBiasPad + 63) / 64;
 constexpr int kDistGroups = 64;
+__host__ __device__ __forceinline__ bool by_name(const SeqBias& b) { return b.buckets > kBiasMost; }
 __device__ __forceinline__ void dist_merge(const DistArgs& a, int h, int first, int step) {
   __shared__ double part[4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -980,7 +982,7 @@ __device__ __forceinline__ void dist_merge(const DistArgs& a, int h, int first, 
   const int l0 = (int)(head * (uint32_t)h / share);
   const int l1 = head == 0 ? l0 - 1 : min((int)((head * ((uint32_t)h + 1ull) - 1) / share), a.P - 1);
   int name[kDistChunks];     // the buckets of the workgroup among the lane's distances
-  if (a.bias.buckets > step) {
+  if (by_name(a.bias)) {
 #pragma unroll
     for (int c = 0; c < kDistChunks; ++c) {
       const int b = a.bias.bucket[min(max(lane + 64 * c - kBiasPad, 0), a.bias.hi - a.bias.lo)];
@@ -989,7 +991,7 @@ __device__ __forceinline__ void dist_merge(const DistArgs& a, int h, int first, 
   }
   // the one behind b
   auto next = [&](int b) {
-    if (a.bias.buckets <= step) return INT_MAX;
+    if (!by_name(a.bias)) return b + step;
     int x = INT_MAX;
 #pragma unroll
     for (int c = 0; c < kDistChunks; ++c) x = min(x, name[c] > b ? name[c] : INT_MAX);
@@ -997,7 +999,7 @@ __device__ __forceinline__ void dist_merge(const DistArgs& a, int h, int first, 
     for (int m = 1; m < 64; m <<= 1) x = min(x, __shfl_xor(x, m));
     return __builtin_amdgcn_readfirstlane(x);
   };
-  for (int b = a.bias.buckets <= step ? first : next(-1); b < a.bias.buckets; b = next(b)) {
+  for (int b = by_name(a.bias) ? next(-1) : first; b < a.bias.buckets; b = next(b)) {
     double x = 0.0;
     uint32_t mine = 0;       // bit c: distance lane + 64 c is of the bucket (all loads at once, not one behind the other)
 #pragma unroll
@@ -1182,7 +1184,7 @@ __global__ __launch_bounds__(256) void grad_prep_kernel(PrepArgs a) {
 
 template <int D>
 static hipError_t launch_grad(const GradCall& c, hipStream_t st) {
-  const int64_t zeros = c.has_bias && c.bias.buckets > kDistGroups ? (int64_t)c.bias.buckets * c.rows_g.Hq : 0;
+  const int64_t zeros = c.has_bias && by_name(c.bias) ? (int64_t)c.bias.buckets * c.rows_g.Hq : 0;
   if (c.rows || zeros > 0) {
     const int64_t groups =
         c.rows ? ((int64_t)c.Tq + kPrepTokens - 1) / kPrepTokens * ceil_div(c.rows_g.Hq, kPrepHeads) : 0;

@@ -37,7 +37,7 @@ def test_starts_held_to_the_rows(starts, lengths, d, biased):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
-@pytest.mark.parametrize("buckets", [64, 65, 513, 5000, 1 << 20])
+@pytest.mark.parametrize("buckets", [64, 65, 513, 514, 5000, 1 << 20])
 def test_many_buckets(buckets, dtype):
     # few of them are named by a distance, the same one by several; the others' gradient is 0, written in every call
     lq, lk = [300, 1, 77], [340, 40, 77]
