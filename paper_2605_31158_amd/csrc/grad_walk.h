@@ -160,7 +160,7 @@ struct GradWalk {
   uint64_t pos, end;       // the stretch still to do
   uint64_t unit0;          // where the present unit starts
   uint64_t head;           // weight of a head
-  uint32_t snap, small;    // as in Walk, but borders in units of up to 5/4 shares go to the nearest end
+  uint32_t snap, small;    // as in Walk, but in units of up to 5/4 shares a border within half a share of an end goes there
   int h, s, j, b;          // head group, sequence, place of the run among the sequence's, run
   Seq q;
   GradLine line;

@@ -143,9 +143,9 @@ int device_workgroups(int per_cu) {
 }
 
 // The gradients' units (seq_grad.hip): what starting and ending one costs (of keys, and of query rows) and the
-// smallest share of a workgroup, in rows of the inner axis; below kGradSnap a share ends at the nearest end of a unit of
-// up to 5/4 shares; and nothing is cut where the inner axis has at most kGradWhole rows.  Chosen over 98 calls, 90 of
-// them drawn: all three at 512 are 3.2 % slower (48 prompts of 1 to 300 tokens, 16 heads over 4, d 64, 39.5 us, with
+// smallest share of a workgroup, in rows of the inner axis; shares below kGradSnap end at the end of a unit of up to 5/4
+// shares that lies within half a share; and nothing is cut where the inner axis has at most kGradWhole rows.  Chosen over
+// 98 calls, 90 of them drawn: all three at 512 are 3.2 % slower (48 prompts of 1 to 300 tokens, 16 heads over 4, d 64, 39.5 us, with
 // these 36.4), extras of 256 for both 2.2 %, a smallest share of 256 or 144 0.9 %; a snap of 4096 or none costs five
 // prompts of 100 to 2100 (12 heads over 4, a bias) 120 instead of 115.
 // A CU runs one workgroup of dK and dV and one of dQ at a time: 256 of each instead of 512 have half the cuts, and two
@@ -253,9 +253,9 @@ la_status check_bias(const la_rel_bias* bias, const int32_t* bucket, const void*
 // fewer they are cut: that one with 4 heads takes 31 to 38 us instead of 52 to 72, 16 single tokens, of which one has 3900
 // keys, 17 instead of 50, for 2 to 4 us more in even batches (16 over 250 keys 10.6 -> 13).  Continuations of a few queries
 // (more than one a sequence, fewer than a sixteenth of the keys) are whole: 6 a sequence over 256 keys, 8 heads over 2, d 128,
-// take 13.7 us instead of 15.8, but 71 instead of 22 where one sequence has nearly all keys.  A mean of up to 512 keys asks for 256 units too (8 of 512, 8 heads, d 128, 33 -> 25).
-// Calls of more keys are cut: whole units would save 1.5 to 4 us in even batches (32 prompts of 60 to 512 tokens 34 -> 32,
-// 64 60 -> 56).
+// take 13.7 us instead of 15.8, but 71 instead of 22 where one sequence has nearly all keys.  A mean of up to 512 keys asks
+// for 256 units too (8 of 512, 8 heads, d 128, 33 -> 25).  Calls of more keys are cut: whole units would save 1.5 to 4 us in
+// even batches (32 prompts of 60 to 512 tokens 34 -> 32, 64 60 -> 56).
 constexpr int kBiasKeys = 1024, kBiasWhole = 1024, kBiasWholeMost = 2048, kBiasWholeShort = 4096, kBiasPerCu = 2;
 constexpr uint32_t kBiasExtra = 512, kBiasSnap = 2048, kBiasShare = 256;
 struct PromptPlan {

@@ -17,9 +17,9 @@
 // formed from P before its rounding, and the bias' gradient sums it unrounded.  Relative rms error against 64 bits
 // 0.0024, of which the result's own rounding makes 0.0017.
 //
-// Bound, where sequences are long, by the card's power: 8192 causal tokens, 16 heads over 4, d 128, take 781 us, 1.23
-// PFLOP/s over seven products (0.88 over the five that are needed) where a large bf16 product of random data
-// reaches 1.36 to 1.38 (the matrix pipeline is 55 % busy, as it is there); half the vector instructions in the
+// Bound, where sequences are long, by the card's power: 8192 causal tokens, 16 heads over 4, d 128, take 780 to
+// 800 us from card to card, 1.20 to 1.23 PFLOP/s over seven products (0.86 to 0.88 over the five that are needed) where a
+// large bf16 product of random data reaches 1.35 to 1.38 (the matrix pipeline is 54 % busy, as it is there); half the vector instructions in the
 // loops, or fewer LDS conflicts, moved it by 1 to 3 %.  d 64 does the same vector work for half the products: 468 us,
 // 1.03 PFLOP/s.  Short sequences: a unit costs 3.5 us beside its tiles (Q, dO or K, V, the first tile, the results), a
 // tile of 64 by 128 pairs 2.1 us where two walks share a CU, and the start (finding the stretch) 2.5: 48 prompts of 1

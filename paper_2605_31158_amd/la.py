@@ -797,7 +797,8 @@ class RelativeBias(NamedTuple):
     lq stands at i + lk - lq) and key n gets weight[bucket[clamp(n - p, lo, hi) - lo], head].
 
     weight  [buckets, Hq], fp32 or bf16, contiguous, on the GPU.  bucket  int32 [hi - lo + 1] on the GPU, at most
-    513 distances (relative_buckets makes the usual ones); a bucket outside the weights' rows has no bias."""
+    513 distances (relative_buckets makes the usual ones); a bucket outside the weights' rows has no bias.  A weight of
+    -inf hides its distances, as finite ones of -2^14 and less do, which count as -2^14."""
     weight: torch.Tensor
     bucket: torch.Tensor
     lo: int
@@ -851,7 +852,8 @@ def prompt_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.T
     q [Tq, Hq, d]; k, v [Tk, Hkv, d] in bf16, Hq a multiple of Hkv; token and head strides are free
     (multiples of 8).  cu_q, cu_k int32 [S + 1] on the GPU: the first row of every sequence (cu_k None:
     cu_q).  Causal: the last query of a sequence sees its last key.  bias: added to the scaled logits.  Rows
-    behind the last sequence are not written (a new output holds anything there)."""
+    behind the last sequence are not written (a new output holds anything there).  No graph is kept for autograd,
+    whatever the inputs ask for: prompt_attn_bwd has the gradients."""
     Tq, Hq, d, qt, qh = _rows("q", q)
     dev = q.get_device()
     Tk, Hkv, _, kt, kh = _rows("k", k, dev, d=d)
