@@ -820,7 +820,7 @@ __device__ __forceinline__ void row_grad(unsigned char* lds, int group, int P) {
           lse[qc] = z.x;
           delta[qc] = z.y;
           // as in key_grad: rows that see nothing
-          if (!ROTATE && z.x == INFINITY) {
+          if (!ROTATE && __builtin_expect(far.hides || off + t0 < 0, 0) && z.x == INFINITY) {
 #pragma unroll
             for (int ks = 0; ks < D / X::KC; ++ks) qreg[ks][qc] = doreg[ks][qc] = bf16x8{};
           }
